@@ -134,9 +134,9 @@ def _product_inputs(case, seed):
 
 
 def _kv_inputs(case, seed, layers, tokens):
-    """K (channels of different size, as rotary embeddings leave them) and V of all sequences, one behind the other."""
+    """K (channels of different size, as rotary embeddings leave them) and V, room for `tokens` of each sequence."""
     g = _generator(seed)
-    shape = (layers, int(tokens), case["kv_heads"], case["hd"])
+    shape = (layers, case["seqs"], int(tokens), case["kv_heads"], case["hd"])
     k = torch.randn(shape, generator=g, device=DEVICE)
     k = (k * (0.3 + 2.0 * torch.rand(case["kv_heads"], case["hd"], generator=g, device=DEVICE))).to(torch.bfloat16)
     v = torch.randn(shape, generator=g, device=DEVICE).to(torch.bfloat16)
@@ -158,11 +158,9 @@ def _paged(sess, k, v, lens, seed):
     table, blocks = wl.make_block_table(wl.rng_for(seed, 3), lens, 16, spare_blocks=3)
     kv = sess.kv_cache(blocks)
     bt = torch.as_tensor(table, device=DEVICE)
-    at = 0
     for s, n in enumerate(int(x) for x in lens):
         if n:
-            kv_layout.write_tokens(kv, bt[s], k[:, at:at + n], v[:, at:at + n])
-        at += n
+            kv_layout.write_tokens(kv, bt[s], k[:, s, :n], v[:, s, :n])
     return kv, bt
 
 
@@ -180,11 +178,10 @@ def prepare(case, seed):
             st["codes"], st["scales"] = _packed(w)
         return st
     a, b = _lengths(case)
-    st["a"], st["b"] = a, b
     i32 = lambda x: torch.as_tensor(x.astype(np.int32), device=DEVICE)
     if case["op"] == "store":
         layers = case["layers"]
-        k, v, _ = _kv_inputs(case, seed, layers, (a + b).sum())
+        k, v, _ = _kv_inputs(case, seed, layers, (a + b).max())
         shape = (layers, case["seqs"], case["hi"], case["kv_heads"], case["hd"])
         st["out"] = [torch.zeros(shape, dtype=torch.bfloat16, device=DEVICE) for _ in range(2)]
         if own:
@@ -193,9 +190,9 @@ def prepare(case, seed):
             st["kv4"] = st["sess"].kv4_cache(st["kv"].shape[2])
             st["first"], st["count"] = i32(a), i32(b)
         else:
-            st["k"], st["v"] = k, v
+            st["k"], st["v"], st["first"], st["count"] = k, v, i32(a).long(), i32(b).long()
         return st
-    k, v, g = _kv_inputs(case, seed, 1, (a + b).sum())
+    k, v, g = _kv_inputs(case, seed, 1, (a + b).max())
     heads = case["kv_heads"] * case["group"]
     st["q"] = torch.randn((case["seqs"], case["window"], heads, case["hd"]), generator=g, device=DEVICE).to(torch.bfloat16)
     st["out"] = torch.zeros_like(st["q"])
@@ -207,7 +204,7 @@ def prepare(case, seed):
         st["lens"], st["valid"] = i32(a), i32(b) if case["ragged"] else None
         st["max_context"] = int((a + b).max())
     else:
-        st["k"], st["v"] = _packed(k[0]), _packed(v[0])
+        st["k"], st["v"], st["lens"], st["valid"] = _packed(k[0]), _packed(v[0]), i32(a).long(), i32(b).long()
     return st
 
 
@@ -236,12 +233,8 @@ def _values(code, scale):
 
 def _packed(x):
     """Two codes to a byte, as a program holds them."""
-    parts = []
-    step = max(1, (1 << 27) // max(1, x[0].numel()))
-    for i in range(0, x.shape[0], step):
-        code, scale = _quantized(x[i:i + step])
-        parts.append((code[..., ::2] | code[..., 1::2] << 4, scale))
-    return torch.cat([p[0] for p in parts]), torch.cat([p[1] for p in parts])
+    code, scale = _quantized(x)
+    return code[..., ::2] | code[..., 1::2] << 4, scale
 
 
 def _unpacked(codes, scales):
@@ -249,23 +242,20 @@ def _unpacked(codes, scales):
 
 
 def _plain_attention(st):
-    case = st["case"]
-    group, out, at = case["group"], st["out"], 0
-    for s in range(case["seqs"]):
-        cached, n = int(st["a"][s]), int(st["b"][s])
-        keys = cached + n
-        if n:
-            k = _unpacked(st["k"][0][at:at + keys], st["k"][1][at:at + keys]).transpose(0, 1)      # [kv head][key][feature]
-            v = _unpacked(st["v"][0][at:at + keys], st["v"][1][at:at + keys]).transpose(0, 1)
-            q = st["q"][s, :n].float().view(n, case["kv_heads"], group, -1).permute(1, 2, 0, 3).reshape(case["kv_heads"], group * n, -1)
-            sc = q @ k.transpose(1, 2).contiguous() / math.sqrt(case["hd"])
-            i = torch.arange(n, device=sc.device).repeat(group)
-            sc = sc.masked_fill(torch.arange(keys, device=sc.device) > cached + i[:, None], -math.inf)
-            p = torch.exp(sc - sc.amax(-1, keepdim=True))
-            o = (p @ v.contiguous()) / p.sum(-1, keepdim=True)
-            out[s, :n] = o.view(case["kv_heads"], group, n, -1).permute(2, 0, 1, 3).reshape(n, case["kv_heads"] * group, -1).to(out.dtype)
-        at += keys
-    return out
+    case, out = st["case"], st["out"]
+    seqs, w, h, g, hd = case["seqs"], case["window"], case["kv_heads"], case["group"], case["hd"]
+    keys = st["k"][0].shape[1]
+    i, at = torch.arange(w, device=out.device), torch.arange(keys, device=out.device)
+    there = i < st["valid"][:, None]                                                           # [sequence][row]
+    seen = (at <= st["lens"][:, None, None] + i[:, None]) & there[..., None]                   # [sequence][row][key]
+    held = at < (st["lens"] + st["valid"])[:, None]
+    k = _unpacked(*st["k"]).permute(0, 2, 3, 1).reshape(seqs * h, hd, keys)
+    v = torch.where(held[:, :, None, None], _unpacked(*st["v"]), 0.0).transpose(1, 2).reshape(seqs * h, keys, hd)
+    q = st["q"].float().view(seqs, w, h, g, hd).permute(0, 2, 3, 1, 4).reshape(seqs * h, g * w, hd)
+    sc = (q @ k / math.sqrt(hd)).view(seqs, h, g, w, keys).masked_fill(~seen[:, None, None], -math.inf)
+    p = torch.exp(sc - sc.amax(-1, keepdim=True)).view(seqs * h, g * w, keys)
+    o = (p @ v / p.sum(-1, keepdim=True)).view(seqs, h, g, w, hd).permute(0, 3, 1, 2, 4).reshape(out.shape)
+    return out.copy_(torch.where(there[:, :, None, None], o.to(out.dtype), out))
 
 
 def run(state):
@@ -288,13 +278,12 @@ def run(state):
             sess.kv4_store(state["kv"], state["kv4"], state["bt"], state["first"], state["count"], case["hi"])
             sess.kv4_read(state["kv4"], state["bt"], state["first"], state["count"], case["hi"], ok, ov)
             return ok, ov
-        at = 0
-        for s in range(case["seqs"]):
-            f, n = int(state["a"][s]), int(state["b"][s])
-            if n:
-                ok[:, s, :n] = _values(*_quantized(state["k"][:, at + f:at + f + n])).to(torch.bfloat16)
-                ov[:, s, :n] = _values(*_quantized(state["v"][:, at + f:at + f + n])).to(torch.bfloat16)
-            at += f + n
+        at = torch.arange(case["hi"], device=ok.device)
+        there = (at < state["count"][:, None])[:, :, None, None]
+        at = (state["first"][:, None] + at).clamp(max=state["k"].shape[2] - 1)                  # [sequence][n-th position]
+        at = at[:, :, None, None].expand(state["k"].shape[0], *at.shape, *ok.shape[3:])
+        for o, x in ((ok, state["k"]), (ov, state["v"])):
+            o.copy_(torch.where(there, _values(*_quantized(torch.gather(x, 2, at))).to(torch.bfloat16), o))
         return ok, ov
     if own:
         return state["sess"].kv4_attention(0, state["kv4"], state["bt"], state["q"], state["lens"], state["valid"], state["max_context"],
@@ -332,29 +321,27 @@ def exact(case, seed):
         return torch.cat([_defined(w[i:i + 4096]) @ x for i in range(0, case["n"], 4096)]).t().contiguous()
     a, b = _lengths(case)
     if case["op"] == "store":
-        k, v, _ = _kv_inputs(case, seed, case["layers"], (a + b).sum())
+        k, v, _ = _kv_inputs(case, seed, case["layers"], (a + b).max())
         shape = (case["layers"], case["seqs"], case["hi"], case["kv_heads"], case["hd"])
         out = []
         for x in (k, v):
-            o, at = torch.zeros(shape, dtype=torch.float64, device=DEVICE), 0
+            o = torch.zeros(shape, dtype=torch.float64, device=DEVICE)
             for s in range(case["seqs"]):
                 f, n = int(a[s]), int(b[s])
                 for l in range(case["layers"]):
                     if n:
-                        o[l, s, :n] = _defined(x[l, at + f:at + f + n])
-                at += f + n
+                        o[l, s, :n] = _defined(x[l, s, f:f + n])
             out.append(o)
         return tuple(out)
-    k, v, g = _kv_inputs(case, seed, 1, (a + b).sum())
+    k, v, g = _kv_inputs(case, seed, 1, (a + b).max())
     heads = case["kv_heads"] * case["group"]
     q = torch.randn((case["seqs"], case["window"], heads, case["hd"]), generator=g, device=DEVICE).to(torch.bfloat16).double()
-    o, at = torch.zeros_like(q), 0
+    o = torch.zeros_like(q)
     for s in range(case["seqs"]):
         cached, n = int(a[s]), int(b[s])
-        kd, vd = _defined(k[0, at:at + cached + n]), _defined(v[0, at:at + cached + n])
-        at += cached + n
         if not n:
             continue
+        kd, vd = _defined(k[0, s, :cached + n]), _defined(v[0, s, :cached + n])
         hidden = torch.ones(n, cached + n, dtype=torch.bool, device=DEVICE).triu(cached + 1)
         for h in range(heads):
             z = (q[s, :n, h] @ kd[:, h // case["group"]].t()) * case["hd"] ** -0.5
