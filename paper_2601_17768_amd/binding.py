@@ -1,4 +1,4 @@
-"""ctypes binding of the verifier library (include/llm42.h).
+"""ctypes binding of the verifier library (include/llm42.h, include/llm42_mx4.h).
 
 Argument marshalling only: every function here has the name and meaning of the
 C entry point it wraps, takes torch tensors where the C call takes device
@@ -22,12 +22,16 @@ LLM42_KV_BLOCK = 16
 LLM42_MAX_WINDOW = 512
 LLM42_MAX_ROWS = 65536
 LLM42_STATIC_SCRATCH_BYTES = 64 << 20
+LLM42_BF16, LLM42_F32 = 0, 1
 LLM42_SEQ_OK, LLM42_SEQ_BAD_LENGTH, LLM42_SEQ_BAD_BLOCK, LLM42_SEQ_BAD_TOKEN = 0, 1, 2, 4
 
 EXPORTS = ("llm42_model_create", "llm42_model_destroy", "llm42_kv_bytes", "llm42_workspace_bytes",
            "llm42_verify_window", "llm42_verify_window_static", "llm42_commit_rollback", "llm42_last_error", "llm42_schedule_info",
            "llm42_profile_enable", "llm42_profile_collect", "llm42_measure_verify_window_batch_chosen", "llm42_measure_attention_plan", "llm42_decode_step", "llm42_verify_window_sampled",
-           "llm42_decode_step_sampled", "llm42_prefill", "llm42_prefill_workspace_bytes")
+           "llm42_decode_step_sampled", "llm42_prefill", "llm42_prefill_workspace_bytes",
+           "llm42_mx4_bytes", "llm42_mx4_quantize", "llm42_mx4_dequantize", "llm42_mx4_matmul_workspace_bytes", "llm42_mx4_matmul",
+           "llm42_kv4_bytes", "llm42_kv4_store", "llm42_kv4_read", "llm42_kv4_attention_workspace_bytes", "llm42_kv4_attention",
+           "llm42_mx4_model_create", "llm42_mx4_model_destroy", "llm42_decode_step_mx4_workspace_bytes", "llm42_decode_step_mx4")
 KERNEL_CLASSES = ("prepare", "embed", "rmsnorm", "qkv", "attention", "o_proj", "gate_up", "down", "lm_head",
                   "argmax", "commit")
 
@@ -113,6 +117,25 @@ def load_library(path: Optional[str] = None):
     lib.llm42_measure_verify_window_batch_chosen.restype = i32
     lib.llm42_measure_attention_plan.argtypes = [vp, i32, i32, i32, ctypes.POINTER(i64)]
     lib.llm42_measure_attention_plan.restype = i32
+    size, size_p, kvp = ctypes.c_size_t, ctypes.POINTER(ctypes.c_size_t), ctypes.POINTER(KVCache)
+    for name, args in {
+            "llm42_mx4_bytes": [i32, i32, size_p],
+            "llm42_mx4_quantize": [vp, i32, i64, i32, i32, vp, size, vp],
+            "llm42_mx4_dequantize": [vp, size, i32, i32, vp, i32, i64, vp],
+            "llm42_mx4_matmul_workspace_bytes": [i32, i32, i32, size_p],
+            "llm42_mx4_matmul": [vp, size, i32, i32, vp, i64, i32, vp, i32, i64, vp, size, vp],
+            "llm42_kv4_bytes": [vp, i64, size_p],
+            "llm42_kv4_store": [vp, kvp, kvp, vp, vp, i32, i32, vp, vp],
+            "llm42_kv4_read": [vp, kvp, vp, vp, i32, i32, vp, vp, vp, vp],
+            "llm42_kv4_attention_workspace_bytes": [vp, i32, i32, i32, size_p],
+            "llm42_kv4_attention": [vp, i32, kvp, vp, i64, vp, i32, vp, i32, i32, vp, i64, vp, vp, size, vp],
+            "llm42_mx4_model_create": [vp, ctypes.POINTER(vp)],
+            "llm42_decode_step_mx4_workspace_bytes": [vp, i32, i32, size_p],
+            "llm42_decode_step_mx4": [vp, kvp, kvp, vp, vp, i32, i32, vp, vp, vp, size, vp, ctypes.POINTER(Sampling)]}.items():
+        getattr(lib, name).argtypes = args
+        getattr(lib, name).restype = i32
+    lib.llm42_mx4_model_destroy.argtypes = [vp]
+    lib.llm42_mx4_model_destroy.restype = None
     lib.llm42_last_error.argtypes = []
     lib.llm42_last_error.restype = ctypes.c_char_p
     lib.llm42_schedule_info.argtypes = []
@@ -283,6 +306,193 @@ def llm42_prefill(model: int, kv_base: torch.Tensor, num_blocks: int, block_tabl
         _ptr(out_next_tokens, torch.int32), _ptr(seq_status, torch.int32), _ptr(workspace),
         workspace.numel() * workspace.element_size(), _stream_handle(stream),
         ctypes.byref(sampling) if sampling is not None else None))
+
+
+_TYPES = {torch.bfloat16: LLM42_BF16, torch.float32: LLM42_F32}
+
+
+def _on_current_device(*tensors: Optional[torch.Tensor]) -> None:
+    """The library launches on the current device and sees bare pointers only."""
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.device.index != torch.cuda.current_device()):
+            raise ValueError("expected tensors on the current device")
+
+
+def _matrix(t: torch.Tensor, rows: int, cols: int):
+    """(pointer, type, row stride) of a plain matrix whose rows may lie apart."""
+    if t.dim() != 2 or tuple(t.shape) != (rows, cols):
+        raise ValueError(f"expected a [{rows}, {cols}] tensor, got {tuple(t.shape)}")
+    if t.dtype not in _TYPES:
+        raise ValueError(f"expected bfloat16 or float32, got {t.dtype}")
+    if cols > 1 and t.stride(1) != 1:
+        raise ValueError("the values of a row must be neighbours in memory")
+    return t.data_ptr(), _TYPES[t.dtype], t.stride(0) if rows > 1 else cols
+
+
+def _packed(t: torch.Tensor):
+    if t.dtype != torch.uint8:
+        raise ValueError(f"a 4-bit matrix is a uint8 tensor, got {t.dtype}")
+    return _ptr(t), t.numel()
+
+
+def llm42_mx4_bytes(rows: int, cols: int) -> int:
+    out = ctypes.c_size_t()
+    _check(load_library().llm42_mx4_bytes(rows, cols, ctypes.byref(out)))
+    return out.value
+
+
+def llm42_mx4_quantize(src: torch.Tensor, dst: torch.Tensor, stream=None) -> None:
+    """src [rows, cols], bfloat16 or float32; dst: uint8, llm42_mx4_bytes(rows, cols) or more."""
+    if src.dim() != 2:
+        raise ValueError("expected a matrix")
+    _on_current_device(src, dst)
+    rows, cols = src.shape
+    p, kind, stride = _matrix(src, rows, cols)
+    _check(load_library().llm42_mx4_quantize(p, kind, stride, rows, cols, *_packed(dst), _stream_handle(stream)))
+
+
+def llm42_mx4_dequantize(src: torch.Tensor, dst: torch.Tensor, stream=None) -> None:
+    """dst [rows, cols], bfloat16 or float32, receives what src stands for."""
+    if dst.dim() != 2:
+        raise ValueError("expected a matrix")
+    _on_current_device(src, dst)
+    rows, cols = dst.shape
+    p, kind, stride = _matrix(dst, rows, cols)
+    _check(load_library().llm42_mx4_dequantize(*_packed(src), rows, cols, p, kind, stride, _stream_handle(stream)))
+
+
+def llm42_mx4_matmul_workspace_bytes(rows: int, n: int, k: int) -> int:
+    out = ctypes.c_size_t()
+    _check(load_library().llm42_mx4_matmul_workspace_bytes(rows, n, k, ctypes.byref(out)))
+    return out.value
+
+
+def llm42_mx4_matmul(w: torch.Tensor, x: torch.Tensor, out: torch.Tensor, workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """out [rows, n] = x [rows, k] (bfloat16) times the transpose of the n x k matrix w."""
+    if x.dim() != 2 or out.dim() != 2:
+        raise ValueError("x and out must be matrices")
+    _on_current_device(w, x, out, workspace)
+    (rows, k), n = x.shape, out.shape[1]
+    if x.dtype != torch.bfloat16:
+        raise ValueError(f"x must be bfloat16, got {x.dtype}")
+    xp, _, xs = _matrix(x, rows, k)
+    op, kind, os_ = _matrix(out, rows, n)
+    wp, wb = _packed(w)
+    _check(load_library().llm42_mx4_matmul(wp, wb, n, k, xp, xs, rows, op, kind, os_, _ptr(workspace),
+                                           0 if workspace is None else workspace.numel() * workspace.element_size(), _stream_handle(stream)))
+
+
+def llm42_kv4_bytes(model: int, num_blocks: int) -> int:
+    out = ctypes.c_size_t()
+    _check(load_library().llm42_kv4_bytes(model, num_blocks, ctypes.byref(out)))
+    return out.value
+
+
+def _kv4_view(model: int, kv4: torch.Tensor, num_blocks: int, block_table: torch.Tensor, num_seqs: int) -> KVCache:
+    if block_table.dim() != 2 or block_table.shape[0] != num_seqs:
+        raise ValueError("block_table must be [num_seqs, max_blocks_per_seq]")
+    need = llm42_kv4_bytes(model, num_blocks)
+    if kv4.numel() * kv4.element_size() < need:
+        raise ValueError(f"kv4 holds {kv4.numel() * kv4.element_size()} bytes, {num_blocks} blocks need {need}")
+    return KVCache(_ptr(kv4), num_blocks, _ptr(block_table, torch.int32), block_table.shape[1])
+
+
+def _per_seq(t: Optional[torch.Tensor], num_seqs: int):
+    if t is not None and t.numel() != num_seqs:
+        raise ValueError("expected one entry per sequence")
+    return _ptr(t, torch.int32)
+
+
+def llm42_kv4_store(model: int, kv_base: torch.Tensor, num_blocks: int, block_table: torch.Tensor, kv4_base: torch.Tensor,
+                    kv4_num_blocks: int, kv4_block_table: torch.Tensor, first: torch.Tensor, count: torch.Tensor, max_count: int,
+                    seq_status: Optional[torch.Tensor] = None, stream=None) -> None:
+    num_seqs = first.numel()
+    _on_current_device(kv_base, block_table, kv4_base, kv4_block_table, first, count, seq_status)
+    kv = _kv_view(model, kv_base, num_blocks, block_table, num_seqs)
+    kv4 = _kv4_view(model, kv4_base, kv4_num_blocks, kv4_block_table, num_seqs)
+    _check(load_library().llm42_kv4_store(model, ctypes.byref(kv), ctypes.byref(kv4), _per_seq(first, num_seqs), _per_seq(count, num_seqs),
+                                          num_seqs, max_count, _per_seq(seq_status, num_seqs), _stream_handle(stream)))
+
+
+def llm42_kv4_read(model: int, kv4_base: torch.Tensor, kv4_num_blocks: int, kv4_block_table: torch.Tensor, first: torch.Tensor,
+                   count: torch.Tensor, max_count: int, out_k: torch.Tensor, out_v: torch.Tensor,
+                   seq_status: Optional[torch.Tensor] = None, stream=None) -> None:
+    """out_k, out_v: bfloat16 [n_layers, num_seqs, max_count, n_kv_heads, head_dim]."""
+    num_seqs = first.numel()
+    _on_current_device(kv4_base, kv4_block_table, first, count, out_k, out_v, seq_status)
+    kv4 = _kv4_view(model, kv4_base, kv4_num_blocks, kv4_block_table, num_seqs)
+    if out_k.dim() != 5 or out_k.shape != out_v.shape or tuple(out_k.shape[1:3]) != (num_seqs, max_count):
+        raise ValueError("out_k and out_v must be [n_layers, num_seqs, max_count, n_kv_heads, head_dim]")
+    # a token's bytes in the cache are 17/32 of a byte a value: what kv4_bytes of one block says about layers, heads and head_dim
+    layers, _, _, heads, hd = out_k.shape
+    if llm42_kv4_bytes(model, 1) != layers * heads * hd * 17:
+        raise ValueError("out_k and out_v do not have the model's layers, kv heads and head_dim")
+    _check(load_library().llm42_kv4_read(model, ctypes.byref(kv4), _per_seq(first, num_seqs), _per_seq(count, num_seqs), num_seqs, max_count,
+                                         _ptr(out_k, torch.bfloat16), _ptr(out_v, torch.bfloat16), _per_seq(seq_status, num_seqs),
+                                         _stream_handle(stream)))
+
+
+def llm42_kv4_attention_workspace_bytes(model: int, num_seqs: int, window: int, max_context: int) -> int:
+    out = ctypes.c_size_t()
+    _check(load_library().llm42_kv4_attention_workspace_bytes(model, num_seqs, window, max_context, ctypes.byref(out)))
+    return out.value
+
+
+def llm42_kv4_attention(model: int, layer: int, kv4_base: torch.Tensor, kv4_num_blocks: int, kv4_block_table: torch.Tensor,
+                        q: torch.Tensor, seq_lens: torch.Tensor, n_valid: Optional[torch.Tensor], max_context: int, out: torch.Tensor,
+                        workspace: torch.Tensor, seq_status: Optional[torch.Tensor] = None, stream=None) -> None:
+    """q, out: bfloat16 [num_seqs, window, n_q_heads, head_dim]; the rows of a token may lie apart, a token's heads may not."""
+    num_seqs = seq_lens.numel()
+    _on_current_device(kv4_base, kv4_block_table, q, seq_lens, n_valid, out, workspace, seq_status)
+    if q.dim() != 4 or q.shape != out.shape or q.shape[0] != num_seqs:
+        raise ValueError("q and out must be [num_seqs, window, n_q_heads, head_dim]")
+    window, heads, hd = q.shape[1:]
+    strides = []
+    for t in (q, out):
+        if t.dtype != torch.bfloat16:
+            raise ValueError(f"expected bfloat16, got {t.dtype}")
+        row = t.stride(1) if window > 1 else t.stride(0) if num_seqs > 1 else heads * hd
+        if t.stride(3) != 1 or (heads > 1 and t.stride(2) != hd) or (num_seqs > 1 and window > 1 and t.stride(0) != window * row):
+            raise ValueError("q and out: rows (sequence, token) at one distance from each other, their heads side by side")
+        strides.append(row)
+    kv4 = _kv4_view(model, kv4_base, kv4_num_blocks, kv4_block_table, num_seqs)
+    _check(load_library().llm42_kv4_attention(model, layer, ctypes.byref(kv4), q.data_ptr(), strides[0], _per_seq(seq_lens, num_seqs), window,
+                                              _per_seq(n_valid, num_seqs), num_seqs, max_context, out.data_ptr(), strides[1],
+                                              _per_seq(seq_status, num_seqs), _ptr(workspace), workspace.numel() * workspace.element_size(),
+                                              _stream_handle(stream)))
+
+
+def llm42_mx4_model_create(model: int) -> int:
+    handle = ctypes.c_void_p()
+    _check(load_library().llm42_mx4_model_create(model, ctypes.byref(handle)))
+    return handle.value
+
+
+def llm42_mx4_model_destroy(mx4: int) -> None:
+    load_library().llm42_mx4_model_destroy(mx4)
+
+
+def llm42_decode_step_mx4_workspace_bytes(mx4: int, max_seqs: int, max_context: int) -> int:
+    out = ctypes.c_size_t()
+    _check(load_library().llm42_decode_step_mx4_workspace_bytes(mx4, max_seqs, max_context, ctypes.byref(out)))
+    return out.value
+
+
+def llm42_decode_step_mx4(model: int, mx4: int, kv_base: torch.Tensor, num_blocks: int, block_table: torch.Tensor,
+                          kv4_base: Optional[torch.Tensor], kv4_num_blocks: int, kv4_block_table: Optional[torch.Tensor],
+                          seq_lens: torch.Tensor, tokens: torch.Tensor, max_context: int, out_tokens: torch.Tensor,
+                          workspace: torch.Tensor, seq_status: Optional[torch.Tensor] = None, stream=None,
+                          sampling: Optional[Sampling] = None) -> None:
+    """kv4_base None: attention over the bf16 cache.  (`model`: the one that mx4 was made from, for the checks of the cache tensors.)"""
+    num_seqs = seq_lens.numel()
+    _on_current_device(kv_base, block_table, kv4_base, kv4_block_table, seq_lens, tokens, out_tokens, workspace, seq_status)
+    kv = _kv_view(model, kv_base, num_blocks, block_table, num_seqs)
+    kv4 = None if kv4_base is None else _kv4_view(model, kv4_base, kv4_num_blocks, kv4_block_table, num_seqs)
+    _check(load_library().llm42_decode_step_mx4(mx4, ctypes.byref(kv), None if kv4 is None else ctypes.byref(kv4), _per_seq(seq_lens, num_seqs),
+                                                _per_seq(tokens, num_seqs), num_seqs, max_context, _per_seq(out_tokens, num_seqs),
+                                                _per_seq(seq_status, num_seqs), _ptr(workspace),
+                                                workspace.numel() * workspace.element_size(), _stream_handle(stream),
+                                                ctypes.byref(sampling) if sampling is not None else None))
 
 
 def llm42_commit_rollback(candidates: torch.Tensor, out_tokens: torch.Tensor, n_valid: Optional[torch.Tensor],

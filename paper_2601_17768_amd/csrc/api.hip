@@ -9,7 +9,9 @@
 #include <mutex>
 #include <vector>
 
-#include "llm42_dev.h"
+#include <new>
+
+#include "mx4.h"
 
 // Scratch area of llm42_verify_window_static: one copy per GPU that loads the library, held until the process ends.
 // In host code the array's name is only a handle for hipGetSymbolAddress; the device address it yields (one per
@@ -24,6 +26,8 @@ std::mutex g_scratch_mutex;
 
 thread_local char g_err[512] = "";
 
+}  // namespace
+
 llm42_status fail(llm42_status code, const char* fmt, ...) {
   va_list ap;
   va_start(ap, fmt);
@@ -31,6 +35,8 @@ llm42_status fail(llm42_status code, const char* fmt, ...) {
   va_end(ap);
   return code;
 }
+
+namespace {
 
 #define HIP_TRY(expr)                                                                        \
   do {                                                                                       \
@@ -271,6 +277,55 @@ Workspace call_workspace(const llm42_model* m, int num_seqs, int window, int max
   return waves.bytes <= have ? waves : ws;
 }
 
+// A decoding step in 4 bits: the weights, and the cache if attention reads that one.
+struct Fast4 {
+  const llm42_mx4_model* m4;
+  const llm42_kv_cache* kv4;   // or null
+  int splits, split_steps;     // of its attention
+};
+
+// ... its workspace: that of a decoding step, with room for the partials of the 4-bit attention.
+size_t part_rows4(const llm42_model* m, int num_seqs, int max_context, Fast4& f4) {
+  plan_kv4_attention(num_seqs, m->cfg.n_kv_heads, m->group, max_context, m->num_cus, f4.splits, f4.split_steps);
+  return f4.splits > 1 ? (size_t)num_seqs * m->cfg.n_kv_heads * f4.splits * m->group : 0;
+}
+
+void attention4(const Fast4& f4, int layer, int num_seqs, const Workspace& ws, hipStream_t st) {
+  const llm42_model* m = f4.m4->model;
+  const llm42_config& c = m->cfg;
+  Attention4 a;
+  memset(&a, 0, sizeof a);
+  a.base = (const char*)f4.kv4->kv_base + (size_t)layer * f4.kv4->num_blocks * c.n_kv_heads * mx4::kv_record(c.head_dim);
+  a.num_blocks = f4.kv4->num_blocks;
+  a.block_table = f4.kv4->block_table;
+  a.max_blocks = f4.kv4->max_blocks_per_seq;
+  a.seq_len = ws.seq_len;
+  a.q = ws.q;
+  a.out = ws.attn;
+  a.tiles = true;
+  a.num_seqs = num_seqs;
+  a.n_kv_heads = c.n_kv_heads;
+  a.group = m->group;
+  a.head_dim = c.head_dim;
+  a.window = 1;
+  a.splits = f4.splits;
+  a.split_steps = f4.split_steps;
+  a.part_acc = ws.part_acc;
+  a.part_ml = ws.part_ml;
+  launch_kv4_attention(a, st);
+}
+
+// Layer l behind its attention, by the 4-bit weights.
+void run_mlp4(const Fast4& f4, int l, const Workspace& ws, hipStream_t st) {
+  const llm42_model* m = f4.m4->model;
+  const llm42_config& c = m->cfg;
+  const llm42_mx4_model::Layer& w = f4.m4->layers[l];
+  TIMED(LLM42_K_O_PROJ, launch_mx4_residual(w.wo, ws.attn, c.d_model, m->d_attn, ws, st));
+  TIMED(LLM42_K_RMSNORM, launch_rmsnorm(false, m->layers[l].ffn_norm, c.d_model, c.rms_eps, ws, st));
+  TIMED(LLM42_K_GATE_UP, launch_mx4_swiglu(f4.m4, l, ws, st));
+  TIMED(LLM42_K_DOWN, launch_mx4_residual(w.wdown, ws.hidden, c.d_model, m->ffn_k, ws, st));
+}
+
 // Layer `ly` behind its attention.  Returns whether the residual stream still lacks the down-projection (see
 // launch_gemm_residual).
 bool run_mlp(const llm42_model* m, const llm42_model::Layer& ly, const Workspace& ws, hipStream_t st) {
@@ -285,11 +340,11 @@ bool run_mlp(const llm42_model* m, const llm42_model::Layer& ly, const Workspace
 
 // Final norm, LM head and sampler.
 void run_head(const llm42_model* m, bool pending, int window, int num_seqs, int32_t* out_tokens, float* out_logits,
-              const llm42_sampling* sampling, const Workspace& ws, hipStream_t st) {
+              const llm42_sampling* sampling, const Workspace& ws, hipStream_t st, const Fast4* f4 = nullptr) {
   const llm42_config& c = m->cfg;
   TIMED(LLM42_K_RMSNORM, launch_rmsnorm(pending, m->final_norm, c.d_model, c.rms_eps, ws, st));
   int parts;
-  TIMED(LLM42_K_LM_HEAD, parts = launch_gemm_logits(m, window, out_logits, sampling, ws, st));
+  TIMED(LLM42_K_LM_HEAD, parts = f4 ? launch_mx4_logits(f4->m4, sampling, ws, st) : launch_gemm_logits(m, window, out_logits, sampling, ws, st));
   TIMED(LLM42_K_ARGMAX, launch_argmax_merge(parts, num_seqs, window, out_tokens, ws, st));
 }
 
@@ -298,8 +353,9 @@ void run_head(const llm42_model* m, bool pending, int window, int num_seqs, int3
 llm42_status run_pass(const llm42_model* m, const llm42_kv_cache* kv, const int32_t* seq_lens, const int32_t* candidates,
                       int window, const int32_t* n_valid, int num_seqs, int max_context, int32_t* out_tokens,
                       int32_t* seq_status, float* out_logits, const int32_t* dump_seq_ids, int n_dump,
-                      Workspace& ws, hipStream_t st, const llm42_sampling* sampling, bool prefill_pass) {
+                      Workspace& ws, hipStream_t st, const llm42_sampling* sampling, bool prefill_pass, const Fast4* f4 = nullptr) {
   const llm42_config& c = m->cfg;
+  const bool kv4 = f4 && f4->kv4;
   // Partly filled windows: the rows are packed, and what pads the end of the grid is skipped.  (Each workgroup of the prepare
   // launch adds up the counts before it, so not for very many sequences.)
   ws.live = n_valid && num_seqs <= 4096 ? ws.seq_n + num_seqs - 1 : nullptr;
@@ -307,21 +363,37 @@ llm42_status run_pass(const llm42_model* m, const llm42_kv_cache* kv, const int3
   // (windows of several row groups behind little context: leaving out the keys that a group cannot see gives more, 8 x 512 behind
   // nothing 74 -> 54 us a layer; an item saves about half its window, so 1/16 of its keys at the line drawn here)
   ws.full = !n_valid && ws.r_pad % 128 == 0 && (window <= 64 || 8 * window <= max_context);
-  plan_gemms(m, ws);
+  if (!f4) plan_gemms(m, ws);
   TIMED(LLM42_K_PREPARE, launch_prepare(m, kv, seq_lens, candidates, n_valid, num_seqs, window, max_context,
                                         dump_seq_ids, n_dump, out_tokens, seq_status, ws, st, prefill_pass));
-  if (ws.attn_list) TIMED(LLM42_K_PREPARE, launch_attention_plan(m, num_seqs, max_context, ws, st));
+  if (kv4) {
+    // (a mirror with the bf16 cache's own table has been checked with it)
+    if (f4->kv4->block_table != kv->block_table || f4->kv4->max_blocks_per_seq != kv->max_blocks_per_seq || f4->kv4->num_blocks < kv->num_blocks)
+      TIMED(LLM42_K_PREPARE, launch_kv4_step_check(m, f4->kv4, num_seqs, seq_status, ws, st));
+  } else if (ws.attn_list) {
+    TIMED(LLM42_K_PREPARE, launch_attention_plan(m, num_seqs, max_context, ws, st));
+  }
   TIMED(LLM42_K_EMBED, launch_embed(m, candidates, window, ws, st));
   bool pending = false;
   for (int l = 0; l < c.n_layers; ++l) {
     const llm42_model::Layer& ly = m->layers[l];
     TIMED(LLM42_K_RMSNORM, launch_rmsnorm(pending, ly.attn_norm, c.d_model, c.rms_eps, ws, st));
-    TIMED(LLM42_K_QKV, launch_gemm_qkv(m, l, kv, window, ws, st));
-    TIMED(LLM42_K_ATTENTION, launch_attention(m, l, kv, num_seqs, window, max_context, ws, st));
+    if (f4) TIMED(LLM42_K_QKV, launch_mx4_qkv(f4->m4, l, kv, ws, st));
+    else TIMED(LLM42_K_QKV, launch_gemm_qkv(m, l, kv, window, ws, st));
+    if (kv4) {
+      TIMED(LLM42_K_ATTENTION, launch_kv4_store(m, l, kv, f4->kv4, ws.seq_len, nullptr, num_seqs, 1, nullptr, st));
+      TIMED(LLM42_K_ATTENTION, attention4(*f4, l, num_seqs, ws, st));
+    } else {
+      TIMED(LLM42_K_ATTENTION, launch_attention(m, l, kv, num_seqs, window, max_context, ws, st));
+    }
+    if (f4) {
+      run_mlp4(*f4, l, ws, st);
+      continue;
+    }
     if (prefill_pass && l + 1 == c.n_layers) return LLM42_OK;   // the rest is run once, for the rows that need it (see llm42_prefill)
     pending = run_mlp(m, ly, ws, st);
   }
-  run_head(m, pending, window, num_seqs, out_tokens, out_logits, sampling, ws, st);
+  run_head(m, pending, window, num_seqs, out_tokens, out_logits, sampling, ws, st, f4);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return fail(LLM42_EHIP, "verifier pass: launch failed: %s", hipGetErrorString(e));
   return LLM42_OK;
@@ -357,12 +429,13 @@ PrefillExtra carve_prefill(const llm42_model* m, size_t verifier_bytes, int num_
   return x;
 }
 
-// llm42_verify_window_sampled and llm42_decode_step_sampled behind their argument names; batch_chosen: see Workspace.
+// llm42_verify_window_sampled, llm42_decode_step_sampled and llm42_decode_step_mx4 behind their argument names; batch_chosen: see
+// Workspace.
 llm42_status verify_impl(const char* who, const llm42_model* m, const llm42_kv_cache* kv, const int32_t* seq_lens,
                          const int32_t* candidates, int32_t window, const int32_t* n_valid, int32_t num_seqs,
                          int32_t max_context, int32_t* out_tokens, int32_t* seq_status, float* out_logits,
                          const int32_t* dump_seq_ids, int32_t n_dump, void* workspace, size_t workspace_bytes,
-                         void* hip_stream, const llm42_sampling* sampling, bool batch_chosen) {
+                         void* hip_stream, const llm42_sampling* sampling, bool batch_chosen, Fast4* f4 = nullptr) {
   if (sampling && !(sampling->temperature >= 0.f)) return fail(LLM42_EINVAL, "%s: negative temperature", who);
   if (!m || !kv || !seq_lens || !candidates || !out_tokens || !workspace)
     return fail(LLM42_EINVAL, "%s: null argument", who);
@@ -380,11 +453,20 @@ llm42_status verify_impl(const char* who, const llm42_model* m, const llm42_kv_c
     return fail(LLM42_ECAPACITY, "%s: max_context %d exceeds block-table capacity %lld", who, max_context,
                 (long long)kv->max_blocks_per_seq * LLM42_KV_BLOCK);
   if ((uintptr_t)workspace % 256) return fail(LLM42_EWORKSPACE, "%s: workspace not 256-byte aligned", who);
-  Workspace ws = call_workspace(m, num_seqs, window, max_context, (char*)workspace, workspace_bytes, batch_chosen);
+  if (f4 && f4->kv4) {
+    const llm42_kv_cache& k = *f4->kv4;
+    if (!k.kv_base || !k.block_table || k.num_blocks < 1 || k.max_blocks_per_seq < 1 || (uintptr_t)k.kv_base % 256)
+      return fail(LLM42_EINVAL, "%s: bad kv4_cache view", who);
+    if ((int64_t)max_context > (int64_t)k.max_blocks_per_seq * LLM42_KV_BLOCK)
+      return fail(LLM42_ECAPACITY, "%s: max_context %d exceeds the 4-bit cache's block-table capacity %lld", who, max_context,
+                  (long long)k.max_blocks_per_seq * LLM42_KV_BLOCK);
+  }
+  Workspace ws = f4 && f4->kv4 ? carve(m, num_seqs, window, max_context, (char*)workspace, true, part_rows4(m, num_seqs, max_context, *f4))
+                               : call_workspace(m, num_seqs, window, max_context, (char*)workspace, workspace_bytes, batch_chosen);
   if (ws.bytes > workspace_bytes)
     return fail(LLM42_EWORKSPACE, "%s: workspace %zu < %zu bytes", who, workspace_bytes, ws.bytes);
   return run_pass(m, kv, seq_lens, candidates, window, n_valid, num_seqs, max_context, out_tokens, seq_status,
-                  n_dump > 0 ? out_logits : nullptr, dump_seq_ids, n_dump, ws, (hipStream_t)hip_stream, sampling, false);
+                  n_dump > 0 ? out_logits : nullptr, dump_seq_ids, n_dump, ws, (hipStream_t)hip_stream, sampling, false, f4);
 }
 
 }  // namespace
@@ -625,6 +707,83 @@ llm42_status llm42_decode_step_sampled(const llm42_model* m, const llm42_kv_cach
                                        size_t workspace_bytes, void* hip_stream, const llm42_sampling* sampling) {
   return verify_impl("decode_step", m, kv, seq_lens, tokens, 1, nullptr, num_seqs, max_context, out_tokens, seq_status,
                      nullptr, nullptr, 0, workspace, workspace_bytes, hip_stream, sampling, true);
+}
+
+llm42_status llm42_mx4_model_create(const llm42_model* m, llm42_mx4_model** out) {
+  if (!m || !out) return fail(LLM42_EINVAL, "mx4_model_create: null argument");
+  *out = nullptr;
+  int dev = -1;
+  if (hipGetDevice(&dev) != hipSuccess || dev != m->device)
+    return fail(LLM42_EINVAL, "mx4_model_create: the model lives on device %d, current device is %d", m->device, dev);
+  const llm42_config& c = m->cfg;
+  llm42_mx4_model* q = new (std::nothrow) llm42_mx4_model();
+  if (q) q->layers = new (std::nothrow) llm42_mx4_model::Layer[c.n_layers];
+  if (!q || !q->layers) {
+    delete q;
+    return fail(LLM42_EHIP, "mx4_model_create: out of host memory");
+  }
+  q->model = m;
+  const auto size = [](int rows, int cols) { return align_up(mx4::matrix_bytes(rows, cols), 256); };
+  const size_t sz_qkv = size(m->n_qkv, c.d_model), sz_o = size(c.d_model, m->d_attn), sz_gu = size(m->gu_blocks * 16, c.d_model),
+               sz_down = size(c.d_model, m->ffn_k), sz_lm = size(c.vocab, c.d_model);
+  const size_t bytes = (sz_qkv + sz_o + sz_gu + sz_down) * c.n_layers + sz_lm;
+  hipError_t e = hipMalloc((void**)&q->arena, bytes);
+  if (e != hipSuccess) {
+    delete[] q->layers;
+    delete q;
+    return fail(LLM42_EHIP, "mx4_model_create: hipMalloc(%zu): %s", bytes, hipGetErrorString(e));
+  }
+  char* p = q->arena;
+  hipStream_t st = nullptr;
+  const auto make = [&](const uint16_t* src, int rows, int cols, size_t n) {
+    char* r = p;
+    p += n;
+    launch_mx4_quantize_tiles(src, rows, cols, r, st);
+    return r;
+  };
+  for (int l = 0; l < c.n_layers; ++l) {
+    const llm42_model::Layer& ly = m->layers[l];
+    q->layers[l].wqkv = make(ly.wqkv, m->n_qkv, c.d_model, sz_qkv);
+    q->layers[l].wo = make(ly.wo, c.d_model, m->d_attn, sz_o);
+    q->layers[l].wgu = make(ly.wgu, m->gu_blocks * 16, c.d_model, sz_gu);
+    q->layers[l].wdown = make(ly.wdown, c.d_model, m->ffn_k, sz_down);
+  }
+  q->lm_head = make(m->lm_head, c.vocab, c.d_model, sz_lm);
+  e = hipGetLastError();
+  if (e == hipSuccess) e = hipStreamSynchronize(st);
+  if (e != hipSuccess) {
+    llm42_mx4_model_destroy(q);
+    return fail(LLM42_EHIP, "mx4_model_create: %s", hipGetErrorString(e));
+  }
+  *out = q;
+  return LLM42_OK;
+}
+
+void llm42_mx4_model_destroy(llm42_mx4_model* q) {
+  if (!q) return;
+  if (q->arena) (void)hipFree(q->arena);
+  delete[] q->layers;
+  delete q;
+}
+
+llm42_status llm42_decode_step_mx4_workspace_bytes(const llm42_mx4_model* m4, int32_t max_seqs, int32_t max_context, size_t* out_bytes) {
+  if (!m4) return fail(LLM42_EINVAL, "decode_step_mx4_workspace_bytes: null argument");
+  size_t plain = 0, rows = 0;
+  if (llm42_status st = llm42_workspace_bytes(m4->model, max_seqs, 1, max_context, &plain)) return st;
+  Fast4 f4{m4, nullptr, 0, 0};
+  for (int n = 1; n <= max_seqs; ++n) rows = std::max(rows, part_rows4(m4->model, n, max_context, f4));
+  *out_bytes = std::max(plain, carve(m4->model, max_seqs, 1, max_context, nullptr, true, rows).bytes);
+  return LLM42_OK;
+}
+
+llm42_status llm42_decode_step_mx4(const llm42_mx4_model* m4, const llm42_kv_cache* kv, const llm42_kv_cache* kv4, const int32_t* seq_lens,
+                                   const int32_t* tokens, int32_t num_seqs, int32_t max_context, int32_t* out_tokens,
+                                   int32_t* seq_status, void* workspace, size_t workspace_bytes, void* hip_stream,
+                                   const llm42_sampling* sampling) {
+  if (!m4) return fail(LLM42_EINVAL, "decode_step_mx4: null argument");
+  Fast4 f4{m4, kv4, 0, 0};
+  return verify_impl("decode_step_mx4", m4->model, kv, seq_lens, tokens, 1, nullptr, num_seqs, max_context, out_tokens, seq_status,
+                     nullptr, nullptr, 0, workspace, workspace_bytes, hip_stream, sampling, true, &f4);
 }
 
 llm42_status llm42_prefill_workspace_bytes(const llm42_model* m, int32_t max_seqs, int32_t chunk, int32_t max_context,

@@ -454,22 +454,8 @@ void plan_gemms(const llm42_model* m, Workspace& ws) {
 
 void launch_gemm_qkv(const llm42_model* m, int layer, const llm42_kv_cache* kv, int window, const Workspace& ws,
                      hipStream_t st) {
-  const llm42_config& c = m->cfg;
-  const size_t plane = (size_t)kv->num_blocks * c.n_kv_heads * 16 * c.head_dim;
-  QkvEpi e;
-  e.row_rope = (const float4*)ws.row_rope;
-  e.row_pos = ws.row_pos;
-  e.row_seq = ws.row_seq;
-  e.row_blk = ws.row_blk;
-  e.q = ws.q;
-  e.k_plane = (uint16_t*)kv->kv_base + ((size_t)layer * 2 + 0) * plane;
-  e.v_plane = (uint16_t*)kv->kv_base + ((size_t)layer * 2 + 1) * plane;
-  e.n_q_heads = c.n_q_heads;
-  e.n_kv_heads = c.n_kv_heads;
-  e.head_dim = c.head_dim;
-  e.order = row_order(m->group, window);
-  e.r_pad = ws.r_pad;
-  launch_gemm<kSplit[GEMM_QKV]>(m->layers[layer].wqkv, ws.normed, m->n_qkv / 16, c.d_model, m->n_qkv, ws, ws.gemm[GEMM_QKV], e, st);
+  const QkvEpi e = qkv_epilogue(m, layer, kv, window, ws);
+  launch_gemm<kSplit[GEMM_QKV]>(m->layers[layer].wqkv, ws.normed, m->n_qkv / 16, m->cfg.d_model, m->n_qkv, ws, ws.gemm[GEMM_QKV], e, st);
 }
 
 bool launch_gemm_residual(GemmKind kind, const uint16_t* w, const uint16_t* x, float* resid, int n, int k_padded,
@@ -488,19 +474,9 @@ void launch_gemm_swiglu(const llm42_model* m, int layer, const Workspace& ws, hi
 template <bool SAMPLED>
 static int launch_logits(const llm42_model* m, int window, float* out_logits, const llm42_sampling* sampling, const Workspace& ws,
                          hipStream_t st) {
-  LogitsEpi<SAMPLED> e;
-  e.row_pos = ws.row_pos;
-  e.row_seq = ws.row_seq;
-  e.dump_slot = ws.dump_slot;
-  e.out_logits = out_logits;
-  e.amax = ws.amax;
-  e.window = window;
-  e.vocab = m->cfg.vocab;
+  LogitsEpi<SAMPLED> e = logits_epilogue<SAMPLED>(m, window, out_logits, sampling, ws);
   const int n_blocks = m->cfg.vocab / 16, k_tiles = m->cfg.d_model / 32;
   const bf16x8 *wp = (const bf16x8*)m->lm_head, *xp = (const bf16x8*)ws.normed;
-  e.inv_temp = SAMPLED ? 1.0f / sampling->temperature : 0.f;
-  e.seed = SAMPLED ? sampling->seed : 0;
-  e.request_ids = SAMPLED ? sampling->request_ids : nullptr;
   if (ws.m_pad <= 64) {
     e.parts = n_blocks;
     launch_wide(wp, xp, n_blocks, k_tiles, ws, e, st);

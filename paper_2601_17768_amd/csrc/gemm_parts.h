@@ -88,6 +88,25 @@ struct QkvEpi {
   }
 };
 
+inline QkvEpi qkv_epilogue(const llm42_model* m, int layer, const llm42_kv_cache* kv, int window, const Workspace& ws) {
+  const llm42_config& c = m->cfg;
+  const size_t plane = (size_t)kv->num_blocks * c.n_kv_heads * 16 * c.head_dim;
+  QkvEpi e;
+  e.row_rope = (const float4*)ws.row_rope;
+  e.row_pos = ws.row_pos;
+  e.row_seq = ws.row_seq;
+  e.row_blk = ws.row_blk;
+  e.q = ws.q;
+  e.k_plane = (uint16_t*)kv->kv_base + ((size_t)layer * 2 + 0) * plane;
+  e.v_plane = (uint16_t*)kv->kv_base + ((size_t)layer * 2 + 1) * plane;
+  e.n_q_heads = c.n_q_heads;
+  e.n_kv_heads = c.n_kv_heads;
+  e.head_dim = c.head_dim;
+  e.order = row_order(m->group, window);
+  e.r_pad = ws.r_pad;
+  return e;
+}
+
 struct ResidualEpi {
   float* resid;   // fp32 residual stream [m_pad][n], updated in place (one lane owns each element)
   ResidLayout rl;
@@ -220,6 +239,24 @@ struct LogitsEpi {
     if (lane < 16) amax[(size_t)row * parts + nb] = make_float2(b.v, __int_as_float(b.i));
   }
 };
+
+// (`parts` is left to the caller, who knows the kernel)
+template <bool SAMPLED>
+LogitsEpi<SAMPLED> logits_epilogue(const llm42_model* m, int window, float* out_logits, const llm42_sampling* sampling,
+                                   const Workspace& ws) {
+  LogitsEpi<SAMPLED> e;
+  e.row_pos = ws.row_pos;
+  e.row_seq = ws.row_seq;
+  e.dump_slot = ws.dump_slot;
+  e.out_logits = out_logits;
+  e.amax = ws.amax;
+  e.window = window;
+  e.vocab = m->cfg.vocab;
+  e.inv_temp = SAMPLED ? 1.0f / sampling->temperature : 0.f;
+  e.seed = SAMPLED ? sampling->seed : 0;
+  e.request_ids = SAMPLED ? sampling->request_ids : nullptr;
+  return e;
+}
 
 template <class Epi>
 struct is_logits : std::false_type {};

@@ -165,6 +165,9 @@ struct Workspace {
   size_t bytes;
 };
 
+// Keeps the message that llm42_last_error returns on this thread; returns `code` (api.hip).
+llm42_status fail(llm42_status code, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
+
 // ---------------------------------------------------------------------------
 // launchers (each defined in the .hip file that holds its kernel)
 // ---------------------------------------------------------------------------

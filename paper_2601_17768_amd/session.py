@@ -28,12 +28,16 @@ class VerifierSession:
         dev_w = weights if weights["embed"].is_cuda else _to_device(weights, self.device)
         self.model = B.llm42_model_create(self.cfg, dev_w)
         del dev_w
+        self._mx4 = None
         self._ws = None
         self._ws_key = None
 
     def close(self):
         if self.model:
             torch.cuda.synchronize()
+            if self._mx4:
+                B.llm42_mx4_model_destroy(self._mx4)
+                self._mx4 = None
             B.llm42_model_destroy(self.model)
             self.model = None
 
@@ -76,6 +80,67 @@ class VerifierSession:
         B.llm42_verify_window(self.model, kv, kv.shape[2], block_table, seq_lens, candidates, window, n_valid,
                               max_context, out_tokens, ws, seq_status, out_logits, dump_seq_ids, sampling=sampling)
         return out_tokens, seq_status, out_logits
+
+    # ---- the fast path in 4 bits ----
+    @property
+    def mx4(self) -> int:
+        """Handle of the model's 4-bit copy, made when it is first asked for."""
+        if not self._mx4:
+            self._mx4 = B.llm42_mx4_model_create(self.model)
+        return self._mx4
+
+    def kv4_cache(self, num_blocks: int) -> torch.Tensor:
+        """A 4-bit cache of num_blocks blocks."""
+        shape = (self.shape.n_layers, num_blocks, self.shape.n_kv_heads, 17 * self.shape.head_dim)
+        assert np.prod(shape) == B.llm42_kv4_bytes(self.model, num_blocks)
+        return torch.empty(shape, dtype=torch.uint8, device=self.device)
+
+    def kv4_store(self, kv: torch.Tensor, kv4: torch.Tensor, block_table: torch.Tensor, first: torch.Tensor, count: torch.Tensor,
+                  max_count: int, kv4_block_table: Optional[torch.Tensor] = None, seq_status: Optional[torch.Tensor] = None) -> None:
+        """One llm42_kv4_store call (the 4-bit cache has the bf16 cache's block table unless another is given)."""
+        B.llm42_kv4_store(self.model, kv, kv.shape[2], block_table, kv4, kv4.shape[1],
+                          block_table if kv4_block_table is None else kv4_block_table, first, count, max_count, seq_status)
+
+    def kv4_read(self, kv4: torch.Tensor, block_table: torch.Tensor, first: torch.Tensor, count: torch.Tensor, max_count: int,
+                 out_k: Optional[torch.Tensor] = None, out_v: Optional[torch.Tensor] = None, seq_status: Optional[torch.Tensor] = None):
+        """One llm42_kv4_read call.  Returns (out_k, out_v)."""
+        shape = (self.shape.n_layers, first.numel(), max_count, self.shape.n_kv_heads, self.shape.head_dim)
+        if out_k is None:
+            out_k = torch.zeros(shape, dtype=torch.bfloat16, device=self.device)
+        if out_v is None:
+            out_v = torch.zeros(shape, dtype=torch.bfloat16, device=self.device)
+        B.llm42_kv4_read(self.model, kv4, kv4.shape[1], block_table, first, count, max_count, out_k, out_v, seq_status)
+        return out_k, out_v
+
+    def kv4_attention(self, layer: int, kv4: torch.Tensor, block_table: torch.Tensor, q: torch.Tensor, seq_lens: torch.Tensor,
+                      n_valid: Optional[torch.Tensor] = None, max_context: Optional[int] = None, out: Optional[torch.Tensor] = None,
+                      seq_status: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """One llm42_kv4_attention call.  Returns out."""
+        if max_context is None:
+            max_context = block_table.shape[1] * B.LLM42_KV_BLOCK
+        need = B.llm42_kv4_attention_workspace_bytes(self.model, q.shape[0], q.shape[1], max_context)
+        if self._ws is None or self._ws.numel() < need:
+            self._ws = torch.empty(need, dtype=torch.uint8, device=self.device)
+        if out is None:
+            out = torch.zeros_like(q)
+        B.llm42_kv4_attention(self.model, layer, kv4, kv4.shape[1], block_table, q, seq_lens, n_valid, max_context, out, self._ws, seq_status)
+        return out
+
+    def decode_mx4(self, kv: torch.Tensor, block_table: torch.Tensor, seq_lens: torch.Tensor, tokens: torch.Tensor,
+                   kv4: Optional[torch.Tensor] = None, kv4_block_table: Optional[torch.Tensor] = None, max_context: Optional[int] = None,
+                   out_tokens: Optional[torch.Tensor] = None, seq_status: Optional[torch.Tensor] = None, sampling=None) -> torch.Tensor:
+        """One llm42_decode_step_mx4 call: the fast path by 4-bit weights, over the 4-bit cache if one is given.  Returns out_tokens."""
+        if max_context is None:
+            max_context = block_table.shape[1] * B.LLM42_KV_BLOCK
+        need = B.llm42_decode_step_mx4_workspace_bytes(self.mx4, seq_lens.numel(), max_context)
+        if self._ws is None or self._ws.numel() < need:
+            self._ws = torch.empty(need, dtype=torch.uint8, device=self.device)
+        if out_tokens is None:
+            out_tokens = torch.empty(seq_lens.numel(), dtype=torch.int32, device=self.device)
+        table4 = None if kv4 is None else block_table if kv4_block_table is None else kv4_block_table
+        B.llm42_decode_step_mx4(self.model, self.mx4, kv, kv.shape[2], block_table, kv4, 0 if kv4 is None else kv4.shape[1], table4, seq_lens,
+                                tokens, max_context, out_tokens, self._ws, seq_status, sampling=sampling)
+        return out_tokens
 
     def commit(self, candidates: torch.Tensor, out_tokens: torch.Tensor, seq_lens: torch.Tensor,
                n_valid: Optional[torch.Tensor] = None):
