@@ -161,7 +161,8 @@ def _ptr(t: Optional[torch.Tensor], dtype: Optional[torch.dtype] = None) -> Opti
 
 def _stream_handle(stream) -> Optional[int]:
     if stream is None:
-        stream = torch.cuda.current_stream()
+        # (the handle alone: without the Stream object around it 0.4 instead of 2.8 us a call)
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()) or None
     return stream.cuda_stream or None
 
 
@@ -314,19 +315,21 @@ _TYPES = {torch.bfloat16: LLM42_BF16, torch.float32: LLM42_F32}
 def _on_current_device(*tensors: Optional[torch.Tensor]) -> None:
     """The library launches on the current device and sees bare pointers only."""
     for t in tensors:
-        if t is not None and (not t.is_cuda or t.device.index != torch.cuda.current_device()):
+        if t is not None and not (t.is_cuda and t.get_device() == torch._C._cuda_getDevice()):
             raise ValueError("expected tensors on the current device")
 
 
 def _matrix(t: torch.Tensor, rows: int, cols: int):
     """(pointer, type, row stride) of a plain matrix whose rows may lie apart."""
-    if t.dim() != 2 or tuple(t.shape) != (rows, cols):
+    if t.shape != (rows, cols):
         raise ValueError(f"expected a [{rows}, {cols}] tensor, got {tuple(t.shape)}")
-    if t.dtype not in _TYPES:
+    kind = _TYPES.get(t.dtype)
+    if kind is None:
         raise ValueError(f"expected bfloat16 or float32, got {t.dtype}")
-    if cols > 1 and t.stride(1) != 1:
+    apart, near = t.stride()
+    if cols > 1 and near != 1:
         raise ValueError("the values of a row must be neighbours in memory")
-    return t.data_ptr(), _TYPES[t.dtype], t.stride(0) if rows > 1 else cols
+    return t.data_ptr(), kind, apart if rows > 1 else cols
 
 
 def _packed(t: torch.Tensor):

@@ -315,15 +315,17 @@ void attention4(const Fast4& f4, int layer, int num_seqs, const Workspace& ws, h
   launch_kv4_attention(a, st);
 }
 
-// Layer l behind its attention, by the 4-bit weights.
-void run_mlp4(const Fast4& f4, int l, const Workspace& ws, hipStream_t st) {
+// Layer l behind its attention, by the 4-bit weights; as run_mlp.
+bool run_mlp4(const Fast4& f4, int l, const Workspace& ws, hipStream_t st) {
   const llm42_model* m = f4.m4->model;
   const llm42_config& c = m->cfg;
   const llm42_mx4_model::Layer& w = f4.m4->layers[l];
-  TIMED(LLM42_K_O_PROJ, launch_mx4_residual(w.wo, ws.attn, c.d_model, m->d_attn, ws, st));
-  TIMED(LLM42_K_RMSNORM, launch_rmsnorm(false, m->layers[l].ffn_norm, c.d_model, c.rms_eps, ws, st));
+  bool pending;
+  TIMED(LLM42_K_O_PROJ, pending = launch_mx4_residual(w.wo, ws.attn, c.d_model, m->d_attn, ws, st));
+  TIMED(LLM42_K_RMSNORM, launch_rmsnorm(pending, m->layers[l].ffn_norm, c.d_model, c.rms_eps, ws, st));
   TIMED(LLM42_K_GATE_UP, launch_mx4_swiglu(f4.m4, l, ws, st));
-  TIMED(LLM42_K_DOWN, launch_mx4_residual(w.wdown, ws.hidden, c.d_model, m->ffn_k, ws, st));
+  TIMED(LLM42_K_DOWN, pending = launch_mx4_residual(w.wdown, ws.hidden, c.d_model, m->ffn_k, ws, st));
+  return pending;
 }
 
 // Layer `ly` behind its attention.  Returns whether the residual stream still lacks the down-projection (see
@@ -387,7 +389,7 @@ llm42_status run_pass(const llm42_model* m, const llm42_kv_cache* kv, const int3
       TIMED(LLM42_K_ATTENTION, launch_attention(m, l, kv, num_seqs, window, max_context, ws, st));
     }
     if (f4) {
-      run_mlp4(*f4, l, ws, st);
+      pending = run_mlp4(*f4, l, ws, st);
       continue;
     }
     if (prefill_pass && l + 1 == c.n_layers) return LLM42_OK;   // the rest is run once, for the rows that need it (see llm42_prefill)

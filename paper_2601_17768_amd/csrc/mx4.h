@@ -96,11 +96,13 @@ void launch_mx4_dequantize(const void* src, int rows, int cols, void* dst, int t
 // x to the tile layout, columns padded with zeros to a multiple of 32
 void launch_mx4_pack_x(const uint16_t* x, int64_t stride, int rows, int k, uint16_t* dst, hipStream_t st);
 
-// x: row-major (x_stride > 0) or tile layout (0); k a multiple of 32.
+// x: row-major (x_stride > 0; k a multiple of 32) or tile layout (0).  parts: mx4_matmul_part_bytes bytes, or null: the sum is not split.
+size_t mx4_matmul_part_bytes(int n, int k, int rows, int num_cus);
 void launch_mx4_matmul(const void* w, int n, int k, const uint16_t* x, int64_t x_stride, int rows, void* out, int out_type,
-                       int64_t out_stride, int num_cus, hipStream_t st);
+                       int64_t out_stride, int num_cus, float* parts, hipStream_t st);
 void launch_mx4_qkv(const llm42_mx4_model* m4, int layer, const llm42_kv_cache* kv, const Workspace& ws, hipStream_t st);
-void launch_mx4_residual(const void* w, const uint16_t* x, int n, int k, const Workspace& ws, hipStream_t st);
+// true: the residual stream is not complete yet; the halves are in split_part, for the RMSNorm that follows
+bool launch_mx4_residual(const void* w, const uint16_t* x, int n, int k, const Workspace& ws, hipStream_t st);
 void launch_mx4_swiglu(const llm42_mx4_model* m4, int layer, const Workspace& ws, hipStream_t st);
 int launch_mx4_logits(const llm42_mx4_model* m4, const llm42_sampling* sampling, const Workspace& ws, hipStream_t st);
 

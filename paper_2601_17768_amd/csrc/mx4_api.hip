@@ -43,6 +43,8 @@ llm42_status check_matrix(const char* who, const void* packed, size_t bytes, int
   return LLM42_OK;
 }
 
+size_t packed_x_bytes(int rows, int k) { return align_up(2 * align_up(rows, 16) * align_up(k, 32), 256); }
+
 llm42_status check_cache(const char* who, const char* name, const llm42_kv_cache* kv) {
   if (!kv || !kv->kv_base || !kv->block_table || kv->num_blocks < 1 || kv->max_blocks_per_seq < 1 || (uintptr_t)kv->kv_base % 16)
     return fail(LLM42_EINVAL, "%s: bad %s view", who, name);
@@ -118,7 +120,7 @@ llm42_status llm42_mx4_dequantize(const void* src, size_t src_bytes, int32_t row
 llm42_status llm42_mx4_matmul_workspace_bytes(int32_t rows, int32_t n, int32_t k, size_t* out_bytes) {
   if (!out_bytes) return fail(LLM42_EINVAL, "mx4_matmul_workspace_bytes: null argument");
   if (rows < 1 || rows > LLM42_MAX_ROWS || n < 1 || k < 1) return fail(LLM42_EINVAL, "mx4_matmul_workspace_bytes: sizes out of range");
-  *out_bytes = 2 * align_up(rows, 16) * align_up(k, 32);
+  *out_bytes = packed_x_bytes(rows, k) + mx4_matmul_part_bytes(n, k, rows, num_cus());
   return LLM42_OK;
 }
 
@@ -132,17 +134,16 @@ llm42_status llm42_mx4_matmul(const void* w, size_t w_bytes, int32_t n, int32_t 
   if (x_stride < k) return fail(LLM42_EINVAL, "%s: x_stride %lld is less than k", who, (long long)x_stride);
   if ((uintptr_t)x % 2) return fail(LLM42_EINVAL, "%s: x not aligned to its type", who);
   hipStream_t st = (hipStream_t)hip_stream;
-  const uint16_t* xp = (const uint16_t*)x;
-  if (k % 32 || (uintptr_t)x % 16 || (rows > 1 && x_stride % 8)) {
-    size_t need = 0;
-    (void)llm42_mx4_matmul_workspace_bytes(rows, n, k, &need);
+  const size_t packed = packed_x_bytes(rows, k), need = packed + mx4_matmul_part_bytes(n, k, rows, num_cus());
+  const bool pack = k % 32 || (uintptr_t)x % 16 || (rows > 1 && (x_stride % 8 || x_stride > (1 << 26)));
+  const bool room = workspace && (uintptr_t)workspace % 256 == 0 && workspace_bytes >= need;
+  if (pack && !room) {
     if (!workspace || (uintptr_t)workspace % 256) return fail(LLM42_EWORKSPACE, "%s: this x needs a workspace, 256-byte aligned", who);
-    if (workspace_bytes < need) return fail(LLM42_EWORKSPACE, "%s: workspace %zu < %zu bytes", who, workspace_bytes, need);
-    launch_mx4_pack_x(xp, x_stride, rows, k, (uint16_t*)workspace, st);
-    xp = (const uint16_t*)workspace;
-    x_stride = 0;
+    return fail(LLM42_EWORKSPACE, "%s: workspace %zu < %zu bytes", who, workspace_bytes, need);
   }
-  launch_mx4_matmul(w, n, k, xp, x_stride, rows, out, out_type, out_stride, num_cus(), st);
+  if (pack) launch_mx4_pack_x((const uint16_t*)x, x_stride, rows, k, (uint16_t*)workspace, st);
+  launch_mx4_matmul(w, n, k, (const uint16_t*)(pack ? workspace : x), pack ? 0 : x_stride, rows, out, out_type, out_stride, num_cus(),
+                    room && need > packed ? (float*)((char*)workspace + packed) : nullptr, st);
   return launched(who);
 }
 

@@ -34,15 +34,15 @@ class Mx4Matrix:
 
     def matmul(self, x: torch.Tensor, dtype: torch.dtype = torch.bfloat16, out: Optional[torch.Tensor] = None,
                workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
-        """One llm42_mx4_matmul call: x [m, cols] (bfloat16) times the transpose, [m, rows] in dtype (or in out's).  An x whose rows are
-        not 16-byte aligned, or cols not a multiple of 32, needs a workspace; it is allocated if none is given."""
+        """One llm42_mx4_matmul call: x [m, cols] (bfloat16) times the transpose, [m, rows] in dtype (or in out's).  The workspace is allocated
+        if none is given (up to 8 rows only if the call cannot do without)."""
         if x.dim() != 2 or x.shape[1] != self.cols:
             raise ValueError(f"x must be [rows, {self.cols}]")
         if out is None:
             out = torch.empty((x.shape[0], self.rows), dtype=dtype, device=self.data.device)
         if tuple(out.shape) != (x.shape[0], self.rows):
             raise ValueError(f"out must be [{x.shape[0]}, {self.rows}]")
-        if workspace is None and (self.cols % 32 or x.data_ptr() % 16 or (x.shape[0] > 1 and x.stride(0) % 8)):
+        if workspace is None and (x.shape[0] > 8 or self.cols % 32 or x.data_ptr() % 16 or x.stride(0) % 8):
             workspace = torch.empty(B.llm42_mx4_matmul_workspace_bytes(x.shape[0], self.rows, self.cols), dtype=torch.uint8, device=x.device)
         B.llm42_mx4_matmul(self.data, x, out, workspace)
         return out
