@@ -31,6 +31,7 @@ FLAGS = [
 # placed in the accumulation registers would be copied out and back each time.
 FILE_FLAGS = {
     "attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+    "kv4_attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
 }
 
 

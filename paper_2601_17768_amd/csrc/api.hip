@@ -290,7 +290,7 @@ size_t part_rows4(const llm42_model* m, int num_seqs, int max_context, Fast4& f4
   return f4.splits > 1 ? (size_t)num_seqs * m->cfg.n_kv_heads * f4.splits * m->group : 0;
 }
 
-void attention4(const Fast4& f4, int layer, int num_seqs, const Workspace& ws, hipStream_t st) {
+void attention4(const Fast4& f4, int layer, int num_seqs, int max_context, const Workspace& ws, hipStream_t st) {
   const llm42_model* m = f4.m4->model;
   const llm42_config& c = m->cfg;
   Attention4 a;
@@ -308,6 +308,7 @@ void attention4(const Fast4& f4, int layer, int num_seqs, const Workspace& ws, h
   a.group = m->group;
   a.head_dim = c.head_dim;
   a.window = 1;
+  a.max_context = max_context;
   a.splits = f4.splits;
   a.split_steps = f4.split_steps;
   a.part_acc = ws.part_acc;
@@ -384,7 +385,7 @@ llm42_status run_pass(const llm42_model* m, const llm42_kv_cache* kv, const int3
     else TIMED(LLM42_K_QKV, launch_gemm_qkv(m, l, kv, window, ws, st));
     if (kv4) {
       TIMED(LLM42_K_ATTENTION, launch_kv4_store(m, l, kv, f4->kv4, ws.seq_len, nullptr, num_seqs, 1, nullptr, st));
-      TIMED(LLM42_K_ATTENTION, attention4(*f4, l, num_seqs, ws, st));
+      TIMED(LLM42_K_ATTENTION, attention4(*f4, l, num_seqs, max_context, ws, st));
     } else {
       TIMED(LLM42_K_ATTENTION, launch_attention(m, l, kv, num_seqs, window, max_context, ws, st));
     }

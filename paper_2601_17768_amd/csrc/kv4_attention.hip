@@ -1,34 +1,13 @@
 // Causal attention of the last positions of every sequence over the 4-bit cache.
+#include <type_traits>
+
 #include "mx4.h"
 
 using namespace mx4;
 
 namespace {
 
-// One workgroup per sequence, for a call that has no prepare pass of its own.
-__global__ __launch_bounds__(64) void kv4_attention_check_kernel(const int32_t* __restrict__ seq_lens, const int32_t* __restrict__ n_valid,
-                                                                 int window, int max_context, const int32_t* __restrict__ table, int width,
-                                                                 int64_t num_blocks, int32_t* __restrict__ seq_status,
-                                                                 int32_t* __restrict__ ws_len, int32_t* __restrict__ ws_n) {
-  const int s = blockIdx.x, lane = threadIdx.x;
-  const int64_t len = seq_lens[s], n = n_valid ? n_valid[s] : window;
-  int status = len < 0 || n < 0 || n > window || len + n > max_context ? LLM42_SEQ_BAD_LENGTH : LLM42_SEQ_OK;
-  if (status == LLM42_SEQ_OK) {
-    const int blocks = n ? (int)((len + n + LLM42_KV_BLOCK - 1) / LLM42_KV_BLOCK) : 0;   // (<= width: checked on the host)
-    bool bad = false;
-    for (int b = lane; b < blocks; b += 64) {
-      const int id = table[(size_t)s * width + b];
-      bad |= id < 0 || id >= num_blocks;
-    }
-    if (__any(bad)) status = LLM42_SEQ_BAD_BLOCK;
-  }
-  if (lane == 0) {
-    if (seq_status) seq_status[s] = status;
-    ws_len[s] = status == LLM42_SEQ_OK && n > 0 ? (int)len : -1;
-    ws_n[s] = (int)n;
-  }
-}
-
+// A decoding step whose 4-bit cache has a block table of its own: one wave per sequence.
 __global__ __launch_bounds__(64) void kv4_step_check_kernel(const int32_t* __restrict__ table, int width, int64_t num_blocks,
                                                             int32_t* __restrict__ seq_status, int32_t* __restrict__ ws_len,
                                                             int32_t* __restrict__ row_pos, uint16_t* __restrict__ attn, int d_attn) {
@@ -54,17 +33,17 @@ constexpr int kStep = 64;   // keys
 template <int HD>
 struct Step {
   static constexpr int KT = HD / 32;
-  uint32_t k[4][KT], v[4][KT], ks[4], vs[4][KT];
+  uint32_t k[4][KT], ks[4], v[4][KT], vs[4][KT];
 };
 
-template <int HD>
+template <int HD, bool NT>
 __device__ __forceinline__ void load_words(uint32_t (&d)[HD / 32], const char* p) {
   if constexpr (HD == 128) {
-    const u32x4 w = *(const u32x4*)p;
+    const u32x4 w = NT ? __builtin_nontemporal_load((const u32x4*)p) : *(const u32x4*)p;
 #pragma unroll
     for (int i = 0; i < 4; ++i) d[i] = w[i];
   } else {
-    const u32x2 w = *(const u32x2*)p;
+    const u32x2 w = NT ? __builtin_nontemporal_load((const u32x2*)p) : *(const u32x2*)p;
     d[0] = w.x;
     d[1] = w.y;
   }
@@ -72,8 +51,10 @@ __device__ __forceinline__ void load_words(uint32_t (&d)[HD / 32], const char* p
 
 // Maximum / sum over the four lanes that hold a query row's keys (lanes l, l ^ 16, l ^ 32, l ^ 48).
 __device__ __forceinline__ float row_max(float v) {
-  v = fmaxf(v, __shfl_xor(v, 16));
-  return fmaxf(v, __shfl_xor(v, 32));
+  const u32x2 a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(a.x), __uint_as_float(a.y));
+  const u32x2 b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(b.x), __uint_as_float(b.y));
 }
 __device__ __forceinline__ float row_sum(float v) {
   v += __shfl_xor(v, 16);
@@ -81,13 +62,17 @@ __device__ __forceinline__ float row_sum(float v) {
 }
 
 // A workgroup takes RB blocks of 16 query rows of a (sequence, kv head) over one of the parts of its context; its four waves take the
-// part's steps of 64 keys in turn, each with a running maximum and sum of its own, and are joined through LDS.
+// part's steps of 64 keys in turn, each with a maximum and sum of its own, and are joined through LDS.
 //   scores: D[key][row] = K Q, K converted with its scales (exact in bf16);
-//   weights: p = exp2((s - max) / sqrt(head_dim) log2 e) in fp32; D's layout is that of the P V operand, no exchange between lanes;
-//   output: D[feature][row] = V P, V's codes converted with scale 1, V's scales - one per key and 32 features, and an operand holds 8 keys of
-//   one feature - multiplied into p, before it is rounded to bf16.
-template <int HD, int RB, bool TILES>
-__global__ __launch_bounds__(64 * kWaves) void kv4_attention_kernel(Attention4 a, float scale_log2) {
+//   weights: p = exp2((s - ref) / sqrt(head_dim) log2 e) in fp32; ref moves to a step's maximum when that exceeds it by more than 8, so
+//   that most steps rescale nothing and p stays below 2^8; rounded to bf16 (2^-8 of a weight: what the matrix instruction takes), their sum
+//   is taken before that.  D's layout is that of the P V operand: no exchange between lanes;
+//   output: D[feature][row] = V P.  An operand holds 8 keys of one feature, and a scale belongs to 32 features of one key: two neighbouring
+//   features of a key are converted together, with its scale, and the halves of 8 keys gathered into the operands of the one and
+//   the other feature.  Where a row does not see all keys of the step, the scales go into its weights instead (the same products): V that a row must not
+//   see may stand for NaN, and 0 NaN is NaN.
+template <int HD, int RB, bool TILES, bool NT>
+__global__ __launch_bounds__(64 * kWaves, RB == 1 ? 3 : 2) void kv4_attention_kernel(Attention4 a, float scale_log2) {
   constexpr int KT = HD / 32, FB = HD / 16;
   __shared__ float sh_ml[kWaves][RB][2][16];
   __shared__ f32x4 sh_acc[kWaves][64 * FB];
@@ -99,9 +84,24 @@ __global__ __launch_bounds__(64 * kWaves) void kv4_attention_kernel(Attention4 a
   const int rg = id % row_groups;
   id /= row_groups;
   const int kvh = id % a.n_kv_heads, s = id / a.n_kv_heads;
-  const int len = a.seq_len[s];
-  if (len < 0) return;
-  const int n = a.seq_n ? a.seq_n[s] : a.window;
+  int len = a.seq_len[s], n = a.window;
+  if constexpr (TILES) {
+    if (len < 0) return;
+  } else {
+    // a call by itself: every workgroup of a sequence checks it (a launch of its own took 2 - 5 us)
+    if (a.seq_n) n = a.seq_n[s];
+    int status = len < 0 || n < 0 || n > a.window || (int64_t)len + n > a.max_context ? LLM42_SEQ_BAD_LENGTH : LLM42_SEQ_OK;
+    bool bad = false;
+    if (status == LLM42_SEQ_OK && n > 0)
+      for (int b = threadIdx.x; b <= (len + n - 1) / LLM42_KV_BLOCK; b += 64 * kWaves) {
+        const int block = a.block_table[(size_t)s * a.max_blocks + b];
+        bad |= block < 0 || block >= a.num_blocks;
+      }
+    if (__syncthreads_or(bad)) status = LLM42_SEQ_BAD_BLOCK;
+    if (a.seq_status && kvh == 0 && rg == 0 && split == 0 && threadIdx.x == 0) a.seq_status[s] = status;
+    if (a.merge_n && rg == 0 && split == 0 && threadIdx.x == 0) a.merge_n[(size_t)s * a.n_kv_heads + kvh] = status == LLM42_SEQ_OK ? n : 0;
+    if (status != LLM42_SEQ_OK) return;
+  }
   const int r0 = rg * 16 * RB, rows = n * a.group;               // rows past the last one repeat it
   if (r0 >= rows) return;
   const int keys = len + (min(r0 + 16 * RB, rows) - 1) / a.group + 1;
@@ -122,7 +122,7 @@ __global__ __launch_bounds__(64 * kWaves) void kv4_attention_kernel(Attention4 a
         q[b][j] = *(const bf16x8*)(a.q + ((size_t)s * a.window + i) * a.q_stride + (size_t)(kvh * a.group + h) * HD + j * 32 + g * 8);
     }
   }
-  f32x4 acc[RB][FB];
+  f32x4 acc[RB][FB];                                              // [2 j]: features 32 j + 8 g + 0, 2, 4, 6; [2 j + 1]: 1, 3, 5, 7
   float m[RB], l[RB];
 #pragma unroll
   for (int b = 0; b < RB; ++b) {
@@ -133,116 +133,155 @@ __global__ __launch_bounds__(64 * kWaves) void kv4_attention_kernel(Attention4 a
   }
   const int32_t* ids = a.block_table + (size_t)s * a.max_blocks;
   const int last_block = (keys - 1) / LLM42_KV_BLOCK;
-  auto load = [&](Step<HD>& d, int step) __attribute__((always_inline)) {
+  const int64_t to_block = (int64_t)a.n_kv_heads * kv_record(HD);
+  const char* base = a.base + (int64_t)kvh * kv_record(HD);
+  // block ids of a step are asked for a step ahead of the loads that need them
+  auto blocks_of = [&](int (&id)[4], int step) __attribute__((always_inline)) {
+#pragma unroll
+    for (int t = 0; t < 4; ++t) id[t] = ids[min(step * 4 + t, last_block)];
+  };
+  auto load_k = [&](Step<HD>& d, const int (&id)[4]) __attribute__((always_inline)) {
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
-      const int blk = ids[min(step * 4 + t, last_block)];
-      const char* rec = a.base + ((size_t)blk * a.n_kv_heads + kvh) * kv_record(HD);
-      load_words<HD>(d.k[t], rec + lane * KT * 4);
-      load_words<HD>(d.v[t], rec + 8 * HD + lane * KT * 4);
+      const char* rec = base + id[t] * to_block;
+      load_words<HD, NT>(d.k[t], rec + lane * KT * 4);
       d.ks[t] = KT == 4 ? *(const uint32_t*)(rec + 16 * HD + l16 * 4) : *(const uint16_t*)(rec + 16 * HD + l16 * 2);
-      load_words<HD>(d.vs[t], rec + 16 * HD + HD / 2 + g * KT * 4);
     }
   };
-  auto compute = [&](const Step<HD>& d, int step) __attribute__((always_inline)) {
-    const bool edge = (step + 1) * kStep > len + 1;               // keys that some row does not see
-    float p[RB][4][4];
+  auto load_v = [&](Step<HD>& d, const int (&id)[4]) __attribute__((always_inline)) {
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
-      f32x4 sc[RB];
+      const char* rec = base + id[t] * to_block;
+      load_words<HD, NT>(d.v[t], rec + 8 * HD + lane * KT * 4);
+      load_words<HD, NT>(d.vs[t], rec + 16 * HD + HD / 2 + g * KT * 4);
+    }
+  };
+  float p[RB][4][4];
+  auto weights = [&](const Step<HD>& d, int step, auto is_edge) __attribute__((always_inline)) {
+    constexpr bool edge = decltype(is_edge)::value;
+    f32x4 sc[4][RB];
 #pragma unroll
-      for (int b = 0; b < RB; ++b) sc[b] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    for (int t = 0; t < 4; ++t)
 #pragma unroll
-      for (int j = 0; j < KT; ++j) {
+      for (int b = 0; b < RB; ++b) sc[t][b] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < KT; ++j)
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
         const bf16x8 k = operand(d.k[t][j], scale_of(d.ks[t], j));
 #pragma unroll
-        for (int b = 0; b < RB; ++b) sc[b] = mfma16(k, q[b][j], sc[b]);
+        for (int b = 0; b < RB; ++b) sc[t][b] = mfma16(k, q[b][j], sc[t][b]);
+        __builtin_amdgcn_sched_barrier(0);                        // (left alone, the compiler converts far ahead and runs out of registers)
       }
-#pragma unroll
-      for (int b = 0; b < RB; ++b)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) p[b][t][i] = sc[b][i];
-    }
 #pragma unroll
     for (int b = 0; b < RB; ++b) {
-      if (edge) {
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (step * kStep + t * 16 + g * 4 + i >= limit[b]) p[b][t][i] = -INFINITY;
-      }
       float mx = -INFINITY;
 #pragma unroll
       for (int t = 0; t < 4; ++t)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) mx = fmaxf(mx, p[b][t][i]);
-      const float m_new = fmaxf(m[b], row_max(mx) * scale_log2);
-      const float ref = m_new == -INFINITY ? 0.f : m_new;         // (nothing seen yet: every weight is 0)
-      const float alpha = exp2f(m[b] - ref);
-      m[b] = m_new;
+        for (int i = 0; i < 4; ++i) {
+          p[b][t][i] = edge && step * kStep + t * 16 + g * 4 + i >= limit[b] ? -INFINITY : sc[t][b][i];
+          mx = fmaxf(mx, p[b][t][i]);
+        }
+      mx = row_max(mx) * scale_log2;
+      const bool moves = mx > m[b] + 8.f;
+      if (__any(moves)) {
+        const float next = moves ? mx : m[b], alpha = __builtin_amdgcn_exp2f(m[b] - (next == -INFINITY ? 0.f : next));
+        m[b] = next;
+        l[b] *= alpha;
+#pragma unroll
+        for (int f = 0; f < FB; ++f) acc[b][f] *= alpha;
+      }
+      const float ref = m[b] == -INFINITY ? 0.f : m[b];           // (nothing seen yet: every weight is 0)
       float sum = 0.f;
 #pragma unroll
       for (int t = 0; t < 4; ++t)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          p[b][t][i] = exp2f(fmaf(p[b][t][i], scale_log2, -ref));
+          p[b][t][i] = __builtin_amdgcn_exp2f(fmaf(p[b][t][i], scale_log2, -ref));
           sum += p[b][t][i];
         }
-      l[b] = l[b] * alpha + sum;
-#pragma unroll
-      for (int f = 0; f < FB; ++f) acc[b][f] *= alpha;
+      l[b] += sum;
     }
+  };
+  auto pack = [&](const float (&w)[8]) __attribute__((always_inline)) {
+    u32x4 u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) u[i] = pack2_bf16(w[2 * i], w[2 * i + 1]);
+    return __builtin_bit_cast(bf16x8, u);
+  };
+  // pairs [i]: features 2 p and 2 p + 1 of 8 keys -> the operands of the one and of the other
+  auto gather = [&](const uint32_t (&r)[8], bool odd) __attribute__((always_inline)) {
+    u32x4 u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) u[i] = __builtin_amdgcn_perm(r[2 * i + 1], r[2 * i], odd ? 0x07060302u : 0x05040100u);
+    return __builtin_bit_cast(bf16x8, u);
+  };
+  auto values = [&](const Step<HD>& d, int step, auto is_edge) __attribute__((always_inline)) {
+    constexpr bool edge = decltype(is_edge)::value;
 #pragma unroll
     for (int t = 0; t < 4; t += 2) {
+      bf16x8 pw[RB];
+#pragma unroll
+      for (int b = 0; b < RB; ++b) {
+        float w[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = p[b][t + (i >> 2)][i & 3];
+        pw[b] = pack(w);
+      }
 #pragma unroll
       for (int j = 0; j < KT; ++j) {
-        bf16x8 pw[RB];
+        uint32_t r[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          r[i] = pair_bf16(d.v[t + (i >> 2)][j], edge ? 1.0f : scale_of(d.vs[t + (i >> 2)][j], i & 3), i & 3);
+        if (edge) {
+#pragma unroll
+          for (int b = 0; b < RB; ++b) {
+            float w[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const float e = __uint_as_float((d.vs[t + (i >> 2)][j] >> (8 * (i & 3)) & 255u) << 23);
+              w[i] = step * kStep + (t + (i >> 2)) * 16 + g * 4 + (i & 3) >= limit[b] ? 0.f : p[b][t + (i >> 2)][i & 3] * e;
+            }
+            pw[b] = pack(w);
+          }
+        }
+        const bf16x8 even = gather(r, false), odd = gather(r, true);
 #pragma unroll
         for (int b = 0; b < RB; ++b) {
-          float w[8];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            w[i] = p[b][t][i] * scale_of(d.vs[t][j], i);
-            w[4 + i] = p[b][t + 1][i] * scale_of(d.vs[t + 1][j], i);
-          }
-          if (edge) {                                             // (whatever scale stands behind the last key)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              if (step * kStep + t * 16 + g * 4 + i >= limit[b]) w[i] = 0.f;
-              if (step * kStep + t * 16 + 16 + g * 4 + i >= limit[b]) w[4 + i] = 0.f;
-            }
-          }
-          u32x4 u;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) u[i] = pack2_bf16(w[2 * i], w[2 * i + 1]);
-          pw[b] = __builtin_bit_cast(bf16x8, u);
+          acc[b][2 * j] = mfma16(even, pw[b], acc[b][2 * j]);
+          acc[b][2 * j + 1] = mfma16(odd, pw[b], acc[b][2 * j + 1]);
         }
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          const int f = 2 * j + half;
-          u32x4 u;
-#pragma unroll
-          for (int x = 0; x < 2; ++x) {
-            const uint32_t w = d.v[t + x][j];
-            u[2 * x] = __builtin_bit_cast(uint32_t, half ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 2)
-                                                         : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 0));
-            u[2 * x + 1] = __builtin_bit_cast(uint32_t, half ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 3)
-                                                             : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 1));
-          }
-          const bf16x8 v = __builtin_bit_cast(bf16x8, u);
-#pragma unroll
-          for (int b = 0; b < RB; ++b) acc[b][f] = mfma16(v, pw[b], acc[b][f]);
-        }
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
   };
-  Step<HD> cur, next;
-  if (begin + wave < end) load(cur, begin + wave);
-  for (int step = begin + wave; step < end; step += kWaves) {
-    load(next, min(step + kWaves, end - 1));
-    compute(cur, step);
-    cur = next;
+  // Steps that every row sees whole, then the last ones.
+  const int inner = min(end, (len + 1) / kStep);
+  int step = begin + wave;
+  if (step < end) {
+    // K of the next step is asked for behind the scores, V behind the output
+    Step<HD> d;
+    int now[4], next[4];
+    blocks_of(now, step);
+    load_k(d, now);
+    load_v(d, now);
+    blocks_of(now, min(step + kWaves, end - 1));
+    const auto one = [&](auto is_edge) __attribute__((always_inline)) {
+      blocks_of(next, min(step + 2 * kWaves, end - 1));
+      weights(d, step, is_edge);
+      load_k(d, now);
+      __builtin_amdgcn_sched_barrier(0);
+      values(d, step, is_edge);
+      load_v(d, now);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int t = 0; t < 4; ++t) now[t] = next[t];
+      step += kWaves;
+    };
+    while (step < inner) one(std::false_type{});
+    while (step < end) one(std::true_type{});
   }
   // join the waves
 #pragma unroll
@@ -265,7 +304,7 @@ __global__ __launch_bounds__(64 * kWaves) void kv4_attention_kernel(Attention4 a
     const float ref = top == -INFINITY ? 0.f : top;
 #pragma unroll
     for (int v = 0; v < kWaves; ++v) {
-      w[v] = exp2f(sh_ml[v][b][0][l16] - ref);
+      w[v] = __builtin_amdgcn_exp2f(sh_ml[v][b][0][l16] - ref);
       sum += w[v] * sh_ml[v][b][1][l16];
     }
     const int r = r0 + b * 16 + l16;
@@ -276,19 +315,25 @@ __global__ __launch_bounds__(64 * kWaves) void kv4_attention_kernel(Attention4 a
       a.part_ml[2 * slot] = top;
       a.part_ml[2 * slot + 1] = sum;
     }
-    for (int f = wave; f < FB; f += kWaves) {
-      f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int j = wave; j < KT; j += kWaves) {                     // features 32 j + 8 g .. + 7
+      f32x4 even = {0.f, 0.f, 0.f, 0.f}, odd = even;
 #pragma unroll
-      for (int v = 0; v < kWaves; ++v) o += sh_acc[v][f * 64 + lane] * w[v];
+      for (int v = 0; v < kWaves; ++v) {
+        even += sh_acc[v][2 * j * 64 + lane] * w[v];
+        odd += sh_acc[v][(2 * j + 1) * 64 + lane] * w[v];
+      }
       if (a.splits > 1) {
-        *(f32x4*)(a.part_acc + slot * HD + f * 16 + g * 4) = o;
+        float* o = a.part_acc + slot * HD + j * 32 + g * 8;
+        *(f32x4*)o = (f32x4){even[0], odd[0], even[1], odd[1]};
+        *(f32x4*)(o + 4) = (f32x4){even[2], odd[2], even[3], odd[3]};
         continue;
       }
-      o /= sum;
-      const u32x2 packed = {pack2_bf16(o[0], o[1]), pack2_bf16(o[2], o[3])};
-      const int col = (kvh * a.group + h) * HD + f * 16 + g * 4;
-      if constexpr (TILES) *(u32x2*)(a.out + pk_off(s, col, a.n_kv_heads * a.group * HD)) = packed;
-      else *(u32x2*)(a.out + ((size_t)s * a.window + i) * a.out_stride + col) = packed;
+      u32x4 packed;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) packed[e] = pack2_bf16(even[e] / sum, odd[e] / sum);
+      const int col = (kvh * a.group + h) * HD + j * 32 + g * 8;
+      if constexpr (TILES) *(u32x4*)(a.out + pk_off(s, col, a.n_kv_heads * a.group * HD)) = packed;
+      else *(u32x4*)(a.out + ((size_t)s * a.window + i) * a.out_stride + col) = packed;
     }
   }
 }
@@ -302,8 +347,8 @@ __global__ __launch_bounds__(256) void kv4_merge_kernel(Attention4 a) {
   const int lane = threadIdx.x & 63, r = (int)(at % rows_all), kvh = (int)(at / rows_all % a.n_kv_heads), s = (int)(at / rows_all / a.n_kv_heads);
   const int len = a.seq_len[s];
   const int i = r / a.group, h = r - i * a.group;
-  if (len < 0 || (a.seq_n && i >= a.seq_n[s])) return;
-  const int n = a.seq_n ? a.seq_n[s] : a.window;
+  const int n = TILES ? (len < 0 ? 0 : 1) : a.merge_n[(size_t)s * a.n_kv_heads + kvh];
+  if (i >= n) return;
   // the parts that the row's workgroup went through (its block of rows sees as much as its last row does)
   const int rb = rows_all > 16 ? 32 : 16, last = min((r / rb + 1) * rb, n * a.group) - 1;
   const int keys = len + last / a.group + 1, steps = (keys + kStep - 1) / kStep, parts = (steps + a.split_steps - 1) / a.split_steps;
@@ -315,7 +360,7 @@ __global__ __launch_bounds__(256) void kv4_merge_kernel(Attention4 a) {
   float o[E] = {}, sum = 0.f;
   for (int p = 0; p < parts; ++p) {
     const size_t slot = slot0 + (size_t)p * rows_all;
-    const float w = exp2f(a.part_ml[2 * slot] - ref);
+    const float w = __builtin_amdgcn_exp2f(a.part_ml[2 * slot] - ref);
     sum += w * a.part_ml[2 * slot + 1];
 #pragma unroll
     for (int e = 0; e < E; ++e) o[e] += w * a.part_acc[slot * HD + lane * E + e];
@@ -331,8 +376,12 @@ void launch(const Attention4& a, hipStream_t st) {
   const float scale_log2 = 1.4426950408889634f / sqrtf((float)HD);
   const int rows = a.group * a.window, rb = rows > 16 ? 2 : 1, groups = (rows + 16 * rb - 1) / (16 * rb);
   const unsigned grid = (unsigned)((int64_t)a.num_seqs * a.n_kv_heads * groups * a.splits);
-  if (rb == 1) kv4_attention_kernel<HD, 1, TILES><<<grid, 64 * kWaves, 0, st>>>(a, scale_log2);
-  else if constexpr (!TILES) kv4_attention_kernel<HD, 2, TILES><<<grid, 64 * kWaves, 0, st>>>(a, scale_log2);
+  // K and V past the caches where there is no more than one block of rows to read them and they may be more than the memory-side cache holds
+  // (128 sequences of 1024 - 8192 keys 149 -> 134 us, of 8192 220 -> 193; what the caches do hold is slower so, 1 x 8192 16 -> 17.6)
+  const bool nt = rb == 1 && (int64_t)a.num_seqs * a.max_context * a.n_kv_heads * kv_record(HD) / LLM42_KV_BLOCK > (256 << 20);
+  if (nt) kv4_attention_kernel<HD, 1, TILES, true><<<grid, 64 * kWaves, 0, st>>>(a, scale_log2);
+  else if (rb == 1) kv4_attention_kernel<HD, 1, TILES, false><<<grid, 64 * kWaves, 0, st>>>(a, scale_log2);
+  else if constexpr (!TILES) kv4_attention_kernel<HD, 2, TILES, false><<<grid, 64 * kWaves, 0, st>>>(a, scale_log2);
   if (a.splits > 1) {
     const int64_t all = (int64_t)a.num_seqs * a.n_kv_heads * rows;
     kv4_merge_kernel<HD, TILES><<<(unsigned)((all + 3) / 4), 256, 0, st>>>(a);
@@ -341,28 +390,25 @@ void launch(const Attention4& a, hipStream_t st) {
 
 }  // namespace
 
-void launch_kv4_attention_check(const int32_t* seq_lens, const int32_t* n_valid, int window, int max_context, int num_seqs,
-                                const llm42_kv_cache* kv4, int32_t* seq_status, int32_t* ws_len, int32_t* ws_n, hipStream_t st) {
-  kv4_attention_check_kernel<<<num_seqs, 64, 0, st>>>(seq_lens, n_valid, window, max_context, kv4->block_table, kv4->max_blocks_per_seq,
-                                                      kv4->num_blocks, seq_status, ws_len, ws_n);
-}
-
 void launch_kv4_step_check(const llm42_model* m, const llm42_kv_cache* kv4, int num_seqs, int32_t* seq_status, const Workspace& ws,
                            hipStream_t st) {
   kv4_step_check_kernel<<<num_seqs, 64, 0, st>>>(kv4->block_table, kv4->max_blocks_per_seq, kv4->num_blocks, seq_status, ws.seq_len,
                                                  ws.row_pos, ws.attn, m->d_attn);
 }
 
-// Parts of a context: as many as it takes to put four workgroups on every CU, none of fewer than four steps.
+// Parts of a context: two workgroups for every CU, parts of 8 steps (2 a wave) or more - if that is worth the launch that joins them: a wave's step
+// takes about 1 us, the launch 4 - 5, and a device half full of workgroups hides some of the former (us in parts / whole, sequences x
+// keys, 8 kv heads: 1 x 2000 12.8 / 15.9, 1 x 8192 16.9 / 41, 16 x 8192 34 / 50, 4 of window 64 x 4000 41.8 / 43.2; but 8 x 1000
+// 12.8 / 12.0, 24 of 16 - 2040 20.0 / 18.1, 64 x 2048 34.7 / 29.6).
 void plan_kv4_attention(int num_seqs, int n_kv_heads, int rows, int max_context, int num_cus, int& splits, int& split_steps) {
   const int rb = rows > 16 ? 2 : 1;
   const int64_t wgs = (int64_t)num_seqs * n_kv_heads * ((rows + 16 * rb - 1) / (16 * rb));
   const int steps = (max_context + kStep - 1) / kStep;
-  int64_t want = (4LL * num_cus + wgs - 1) / wgs;
-  if (want > (steps + kWaves - 1) / kWaves) want = (steps + kWaves - 1) / kWaves;
-  if (want < 1) want = 1;
-  split_steps = (int)((steps + want - 1) / want);
-  split_steps = (split_steps + kWaves - 1) / kWaves * kWaves;
+  const int64_t want = (2LL * num_cus + wgs - 1) / wgs;
+  int part = (int)((steps + want - 1) / want);
+  part = (part < 8 ? 8 : part + kWaves - 1) / kWaves * kWaves;
+  const bool split = (steps + kWaves - 1) / kWaves - part / kWaves >= (2 * wgs < num_cus ? 6 : 8);
+  split_steps = split ? part : steps;
   splits = (steps + split_steps - 1) / split_steps;
 }
 

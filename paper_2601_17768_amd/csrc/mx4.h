@@ -6,8 +6,8 @@
 // with one 16-byte load a lane.  Scales: 8 bytes per row, one per k-tile.
 //
 // The cache holds a record of 17 * head_dim bytes per (layer, block of 16 positions, kv head).  K codes: as above, word j of lane
-// (g, token) features 32 j + 8 g .. + 7.  V codes: lane (g, f) has 2 bytes per block of 16 features, tokens 4 g .. 4 g + 3 of
-// feature 16 b + f: the operand of P V.  K scales: per token a byte per 32 features.  V scales: [g][32 features][4 tokens].
+// (g, token) features 32 j + 8 g .. + 7.  V codes: byte i of word j of lane (g, p) holds features 32 j + 2 p and + 1 of token 4 g + i.
+// K scales: per token a byte per 32 features.  V scales: [g][32 features][4 tokens].
 #pragma once
 #include "../../include/llm42_mx4.h"
 #include "llm42_dev.h"
@@ -30,34 +30,53 @@ __host__ __device__ constexpr int kv_record(int head_dim) { return 17 * head_dim
 __device__ inline uint32_t scale_byte(uint32_t top) {
   return top >= 0x7F800000u ? 255u : (uint32_t)max((int)(top >> 23) - 2, 0);
 }
-// The code of x in a block of that byte: nearest level, ties to the even index.
-__device__ inline uint32_t code_of(float x, uint32_t byte) {
-  const float m = ldexpf(fabsf(x), 127 - (int)byte);           // exact wherever it matters
-  const uint32_t c = (m > 0.25f) + (m >= 0.75f) + (m > 1.25f) + (m >= 1.75f) + (m > 2.5f) + (m >= 3.5f) + (m > 5.0f);
-  return byte == 255u ? 0u : c | (__float_as_uint(x) >> 31) << 3;
-}
-// What a code stands for in a block of scale 1, and 2^E.
-__device__ inline float level(uint32_t code) {
-  const uint32_t m = code & 7;
-  const uint32_t bits = m >= 2 ? (m + 252) << 22 : m ? 0x3F000000u : 0u;
-  return __uint_as_float(bits | (code & 8) << 28);
-}
-__device__ inline float value_of(uint32_t code, uint32_t byte) {
-  return byte == 255u ? __uint_as_float(0x7FC00000u) : ldexpf(level(code), (int)byte - 127);
-}
 
-// 8 codes to an MFMA operand, times `scale` (its exponent bits are what counts).
+// 2^E of byte i of a word of scale bytes, as the conversions take it: of a float's bits they use the eight of the exponent alone, so
+// what stands beside the byte does not matter (all 256 exponents and 256 pairs of codes compared).
+__device__ __forceinline__ float scale_of(uint32_t bytes, int i) { return __uint_as_float(i < 3 ? bytes << (23 - 8 * i) : bytes >> 1); }
+
+// The hardware's conversions.  To 4 bits: nearest level, ties to the even index, saturating - the format's own rule, compared for every
+// bf16 and 16 M floats, subnormal ones too, in blocks of up to 2^13 times their size.  From 4 bits: exact; NaN under byte 255.
+// (Pair e of a word of 8: the builtins want a constant, which e is once unrolled.)
+__device__ __forceinline__ uint32_t pair_bf16(uint32_t codes, float scale, int e) {
+  return __builtin_bit_cast(uint32_t, e == 0   ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0)
+                                      : e == 1 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1)
+                                      : e == 2 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2)
+                                               : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3));
+}
+__device__ __forceinline__ f32x2 pair_f32(uint32_t codes, float scale, int e) {
+  return e == 0   ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 0)
+         : e == 1 ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 1)
+         : e == 2 ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 2)
+                  : __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, 3);
+}
+// 8 codes as bf16: an MFMA operand.
 __device__ __forceinline__ bf16x8 operand(uint32_t codes, float scale) {
-  typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_;
-  u32x4_ r;
-  r.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0));
-  r.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1));
-  r.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2));
-  r.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3));
+  u32x4 r;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) r[e] = pair_bf16(codes, scale, e);
   return __builtin_bit_cast(bf16x8, r);
 }
-// 2^E of byte i of a word of scale bytes, as the conversion takes it.
-__device__ __forceinline__ float scale_of(uint32_t bytes, int i) { return __uint_as_float((bytes >> (8 * i) & 255u) << 23); }
+// Codes of two bf16 in the bytes `e` of a word, the rest of which stays.
+__device__ __forceinline__ uint32_t put_pair(uint32_t word, uint32_t two, float scale, int e) {
+  const bf16x2 v = __builtin_bit_cast(bf16x2, two);
+  return e == 0   ? __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(word, v, scale, 0)
+         : e == 1 ? __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(word, v, scale, 1)
+         : e == 2 ? __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(word, v, scale, 2)
+                  : __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(word, v, scale, 3);
+}
+__device__ __forceinline__ uint32_t put_pair(uint32_t word, float a, float b, float scale, int e) {
+  return e == 0   ? __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, a, b, scale, 0)
+         : e == 1 ? __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, a, b, scale, 1)
+         : e == 2 ? __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, a, b, scale, 2)
+                  : __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, a, b, scale, 3);
+}
+// The larger magnitudes of two pairs of bf16, half by half, and of a pair, as a float's bits.
+typedef __attribute__((ext_vector_type(2))) uint16_t u16x2;
+__device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) {
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a & 0x7FFF7FFFu), __builtin_bit_cast(u16x2, b & 0x7FFF7FFFu)));
+}
+__device__ __forceinline__ uint32_t larger_half(uint32_t a) { return max(a << 16 & 0x7FFF0000u, a & 0x7FFF0000u); }
 
 }  // namespace mx4
 
@@ -77,13 +96,15 @@ struct Attention4 {
   int64_t num_blocks;
   const int32_t* block_table;
   int max_blocks;
-  const int32_t* seq_len;      // cached length before the window; -1: takes no part
+  const int32_t* seq_len;      // cached length before the window (tiles: -1 takes no part)
   const int32_t* seq_n;        // rows of the window that are there, or null: all
+  int32_t* seq_status;         // or null
+  int32_t* merge_n;            // [seq][kv head]: rows of a sequence that is in order, for the launch that joins its parts
   const uint16_t* q;           // rows of q_stride, or (tiles) the layout that the QKV projection leaves
   uint16_t* out;               // rows of out_stride, or (tiles) operand of the O-projection
   int64_t q_stride, out_stride;
   bool tiles;
-  int num_seqs, n_kv_heads, group, head_dim, window;
+  int num_seqs, n_kv_heads, group, head_dim, window, max_context;
   int splits, split_steps;     // parts of a sequence, steps of 64 keys in each
   float* part_acc;             // [seq][kv head][split][row][head_dim]
   float* part_ml;              // [seq][kv head][split][row][2]
@@ -114,7 +135,5 @@ void launch_kv4_read(const llm42_model* m, const llm42_kv_cache* kv4, const int3
 // A decoding step's sequences against the 4-bit cache's own block table; those that fail are switched off as by launch_prepare.
 void launch_kv4_step_check(const llm42_model* m, const llm42_kv_cache* kv4, int num_seqs, int32_t* seq_status,
                            const Workspace& ws, hipStream_t st);
-void launch_kv4_attention_check(const int32_t* seq_lens, const int32_t* n_valid, int window, int max_context, int num_seqs,
-                                const llm42_kv_cache* kv4, int32_t* seq_status, int32_t* ws_len, int32_t* ws_n, hipStream_t st);
 void plan_kv4_attention(int num_seqs, int n_kv_heads, int rows, int max_context, int num_cus, int& splits, int& split_steps);
 void launch_kv4_attention(const Attention4& a, hipStream_t st);

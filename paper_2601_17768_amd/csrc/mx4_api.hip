@@ -55,14 +55,14 @@ llm42_status check_ranges(const char* who, const llm42_model* m, const int32_t* 
                           int32_t max_count) {
   if (!m || !first || !count) return fail(LLM42_EINVAL, "%s: null argument", who);
   if (num_seqs < 1 || max_count < 1) return fail(LLM42_EINVAL, "%s: num_seqs and max_count must be positive", who);
-  if (m->cfg.n_layers > 65535 || (int64_t)num_seqs * (((int64_t)max_count + 14) / 16 + 1) > 0x7FFFFFFF)
+  if (m->cfg.n_layers > 65535 || (int64_t)num_seqs * (((int64_t)max_count + 14) / 16 + 1) > 0x7FFFFFFF / ((m->cfg.n_kv_heads + 3) / 4))
     return fail(LLM42_EINVAL, "%s: num_seqs * max_count too large", who);
   return LLM42_OK;
 }
 
-// Workspace of llm42_kv4_attention: checked lengths and rows, partials.
+// Workspace of llm42_kv4_attention: partials, and the rows that those of a sequence hold.
 struct Attention4Workspace {
-  int32_t *len, *n;
+  int32_t* n;
   float *acc, *ml;
   size_t bytes;
 };
@@ -74,8 +74,7 @@ Attention4Workspace carve(const llm42_model* m, int num_seqs, int window, int sp
     off = align_up(off + bytes, 256);
     return p;
   };
-  w.len = (int32_t*)take(4ull * num_seqs);
-  w.n = (int32_t*)take(4ull * num_seqs);
+  w.n = (int32_t*)take(4ull * num_seqs * m->cfg.n_kv_heads);
   const size_t slots = splits > 1 ? (size_t)num_seqs * m->cfg.n_kv_heads * splits * m->group * window : 0;
   w.acc = (float*)take(4 * slots * m->cfg.head_dim);
   w.ml = (float*)take(8 * slots);
@@ -209,8 +208,10 @@ llm42_status llm42_kv4_attention(const llm42_model* m, int32_t layer, const llm4
   a.num_blocks = kv4->num_blocks;
   a.block_table = kv4->block_table;
   a.max_blocks = kv4->max_blocks_per_seq;
-  a.seq_len = ws.len;
-  a.seq_n = ws.n;
+  a.seq_len = seq_lens;
+  a.seq_n = n_valid;
+  a.seq_status = seq_status;
+  a.merge_n = a.splits > 1 ? ws.n : nullptr;
   a.q = (const uint16_t*)q;
   a.out = (uint16_t*)out;
   a.q_stride = q_stride;
@@ -221,11 +222,10 @@ llm42_status llm42_kv4_attention(const llm42_model* m, int32_t layer, const llm4
   a.group = m->group;
   a.head_dim = c.head_dim;
   a.window = window;
+  a.max_context = max_context;
   a.part_acc = ws.acc;
   a.part_ml = ws.ml;
-  hipStream_t st = (hipStream_t)hip_stream;
-  launch_kv4_attention_check(seq_lens, n_valid, window, max_context, num_seqs, kv4, seq_status, ws.len, ws.n, st);
-  launch_kv4_attention(a, st);
+  launch_kv4_attention(a, (hipStream_t)hip_stream);
   return launched(who);
 }
 

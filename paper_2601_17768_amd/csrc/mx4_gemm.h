@@ -12,14 +12,6 @@ namespace mx4 {
 
 using namespace gemm;
 
-// Values 2 e, 2 e + 1 of a word's eight (e a constant once unrolled).
-__device__ __forceinline__ uint32_t convert_pair(uint32_t codes, float scale, int e) {
-  return __builtin_bit_cast(uint32_t, e == 0   ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0)
-                                      : e == 1 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1)
-                                      : e == 2 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2)
-                                               : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3));
-}
-
 // Where the activations lie: the tile layout, or plain rows of `stride` elements.
 struct X {
   const uint16_t* p;
@@ -248,7 +240,7 @@ __global__ __launch_bounds__(64 * (NW + F), (NW + F + 3) / 4) void mx4_tile_kern
 #pragma unroll
           for (int e = idx % TB * 4 * FB / TB; e < (idx % TB + 1) * 4 * FB / TB; ++e) {
             const int i = e >> 2;
-            conv[i][e & 3] = convert_pair(codes[U][i][(j + 1) & 3], scale_of(scales[U][i], (j + 1) & 3), e & 3);
+            conv[i][e & 3] = pair_bf16(codes[U][i][(j + 1) & 3], scale_of(scales[U][i], (j + 1) & 3), e & 3);
             if ((e & 3) == 3) a[(j + 1) & 1][i] = __builtin_bit_cast(bf16x8, conv[i]);
           }
         }

@@ -5,62 +5,76 @@ using namespace mx4;
 
 namespace {
 
-constexpr int kLane = 8;   // columns of a k-tile that a lane has
-
-// Where the values of a record come from: 8 consecutive columns of a row as fp32, zeros outside the matrix.
+// Where the values of a record come from: 8 consecutive columns of a row, zeros outside the matrix, as words of two bf16 (or 8 floats), and
+// the bits of the largest magnitude.  wide: rows are 16-byte aligned and the record lies within the columns; rows past the last
+// one are then read from it.
 struct PlainBf16 {
   const uint16_t* src;
   int64_t stride;
   int rows, cols;
-  bool wide;               // rows are 16-byte aligned
-  __device__ void load(int r, int c, float (&v)[8]) const {
-    const uint16_t* p = src + (int64_t)r * stride + c;
-    if (wide && r < rows && c + 8 <= cols) {
-      const u32x4 w = *(const u32x4*)p;
+  bool aligned;
+  struct V {
+    u32x4 w;
+    __device__ uint32_t top() const { return larger_half(larger(larger(w[0], w[1]), larger(w[2], w[3]))); }
+    __device__ uint32_t codes(float scale) const {
+      uint32_t word = 0;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        v[2 * i] = __uint_as_float(w[i] << 16);
-        v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = r < rows && c + i < cols ? bf16_bits_to_f32(p[i]) : 0.f;
+      for (int e = 0; e < 4; ++e) word = put_pair(word, w[e], scale, e);
+      return word;
     }
+  };
+  __device__ V wide(int r, int c) const { return {*(const u32x4*)(src + (int64_t)min(r, rows - 1) * stride + c)}; }
+  __device__ V any(int r, int c) const {
+    V v{{0, 0, 0, 0}};
+    const uint16_t* p = src + (int64_t)r * stride + c;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (r < rows && c + i < cols) v.w[i >> 1] |= (uint32_t)p[i] << (16 * (i & 1));
+    return v;
   }
 };
 struct PlainF32 {
   const float* src;
   int64_t stride;
   int rows, cols;
-  bool wide;
-  __device__ void load(int r, int c, float (&v)[8]) const {
-    const float* p = src + (int64_t)r * stride + c;
-    if (wide && r < rows && c + 8 <= cols) {
-      const f32x4 a = *(const f32x4*)p, b = *(const f32x4*)(p + 4);
+  bool aligned;
+  struct V {
+    f32x4 a, b;
+    __device__ uint32_t top() const {
+      uint32_t t = 0;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] = a[i], v[4 + i] = b[i];
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = r < rows && c + i < cols ? p[i] : 0.f;
+      for (int i = 0; i < 4; ++i) t = max(t, max(__float_as_uint(a[i]) & 0x7FFFFFFFu, __float_as_uint(b[i]) & 0x7FFFFFFFu));
+      return t;
     }
+    __device__ uint32_t codes(float scale) const {
+      uint32_t word = put_pair(0, a[0], a[1], scale, 0);
+      word = put_pair(word, a[2], a[3], scale, 1);
+      word = put_pair(word, b[0], b[1], scale, 2);
+      return put_pair(word, b[2], b[3], scale, 3);
+    }
+  };
+  __device__ V wide(int r, int c) const {
+    const float* p = src + (int64_t)min(r, rows - 1) * stride + c;
+    return {*(const f32x4*)p, *(const f32x4*)(p + 4)};
   }
-};
-struct Tiles {             // the tile layout of the bf16 GEMMs
-  const uint16_t* src;
-  int cols;
-  __device__ void load(int r, int c, float (&v)[8]) const {
-    if (c >= cols) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = 0.f;
-      return;
-    }
-    const u32x4 w = *(const u32x4*)(src + pk_off(r, c, cols));
+  __device__ V any(int r, int c) const {
+    V v{{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+    const float* p = src + (int64_t)r * stride + c;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      v[2 * i] = __uint_as_float(w[i] << 16);
-      v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+      if (r < rows && c + i < cols) v.a[i] = p[i];
+      if (r < rows && c + 4 + i < cols) v.b[i] = p[4 + i];
     }
+    return v;
   }
+};
+struct Tiles {             // the tile layout of the bf16 GEMMs (whole blocks of rows and columns)
+  const uint16_t* src;
+  int rows, cols;
+  static constexpr bool aligned = true;
+  typedef PlainBf16::V V;
+  __device__ V wide(int r, int c) const { return {*(const u32x4*)(src + pk_off(r, c, cols))}; }
+  __device__ V any(int r, int c) const { return c < cols ? wide(r, c) : V{{0, 0, 0, 0}}; }
 };
 
 // A wave makes a record.  A block of 32 columns lies in the four lanes of a row, 8 columns each.
@@ -71,22 +85,27 @@ __global__ __launch_bounds__(256) void mx4_quantize_kernel(Src src, char* __rest
   const int lane = threadIdx.x & 63, g = lane >> 4;
   const int r = (int)(rec / units) * 16 + (lane & 15), c0 = (int)(rec % units) * kUnit;
   char* out = dst + rec * kRecord;
+  typename Src::V v[8];
+  if (src.aligned && c0 + kUnit <= src.cols) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = src.wide(r, c0 + j * 32 + g * 8);
+    if (r >= src.rows) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = {};
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = src.any(r, c0 + j * 32 + g * 8);
+  }
   u32x4 codes[2];
   uint32_t scales[2] = {0, 0};
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    float v[8];
-    src.load(r, c0 + j * 32 + g * kLane, v);
-    uint32_t top = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+    uint32_t top = v[j].top();
     top = max(top, (uint32_t)__shfl_xor((int)top, 16));
     top = max(top, (uint32_t)__shfl_xor((int)top, 32));
-    const uint32_t byte = scale_byte(top);
-    uint32_t word = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) word |= code_of(v[i], byte) << (4 * i);
-    codes[j >> 2][j & 3] = word;
+    const uint32_t byte = scale_byte(top), word = v[j].codes(scale_of(byte, 0));
+    codes[j >> 2][j & 3] = byte == 255u ? 0u : word;
     scales[j >> 2] |= byte << (8 * (j & 3));
   }
   *(u32x4*)(out + lane * 16) = codes[0];
@@ -107,13 +126,18 @@ __global__ __launch_bounds__(256) void mx4_dequantize_kernel(const char* __restr
   const u32x2 scales = *(const u32x2*)(in + kScales + (lane & 15) * 8);
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    const int c = c0 + j * 32 + g * kLane;
-    const uint32_t byte = scales[j >> 2] >> (8 * (j & 3)) & 255u, word = codes[j >> 2][j & 3];
-    float v[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = value_of(word >> (4 * i) & 15u, byte);
+    const int c = c0 + j * 32 + g * 8;
+    const uint32_t word = codes[j >> 2][j & 3];
+    const float scale = scale_of(scales[j >> 2], j & 3);
     if constexpr (F32) {
       float* p = (float*)dst + (int64_t)r * stride + c;
+      float v[8];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const f32x2 two = pair_f32(word, scale, e);
+        v[2 * e] = two.x;
+        v[2 * e + 1] = two.y;
+      }
       if (wide && c + 8 <= cols) {
         *(f32x4*)p = (f32x4){v[0], v[1], v[2], v[3]};
         *(f32x4*)(p + 4) = (f32x4){v[4], v[5], v[6], v[7]};
@@ -123,16 +147,13 @@ __global__ __launch_bounds__(256) void mx4_dequantize_kernel(const char* __restr
           if (c + i < cols) p[i] = v[i];
       }
     } else {
-      uint16_t* p = (uint16_t*)dst + (int64_t)r * stride + c;   // (the values are bf16s: the upper halves)
-      if (wide && c + 8 <= cols) {
-        u32x4 w;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = __float_as_uint(v[2 * i]) >> 16 | (__float_as_uint(v[2 * i + 1]) & 0xFFFF0000u);
-        *(u32x4*)p = w;
-      } else {
+      uint16_t* p = (uint16_t*)dst + (int64_t)r * stride + c;
+      const u32x4 w = __builtin_bit_cast(u32x4, operand(word, scale));
+      if (wide && c + 8 <= cols) *(u32x4*)p = w;
+      else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-          if (c + i < cols) p[i] = (uint16_t)(__float_as_uint(v[i]) >> 16);
+          if (c + i < cols) p[i] = (uint16_t)(w[i >> 1] >> (16 * (i & 1)));
       }
     }
   }
@@ -167,7 +188,7 @@ void launch_mx4_quantize(const void* src, int type, int64_t stride, int rows, in
 }
 
 void launch_mx4_quantize_tiles(const uint16_t* src, int rows, int cols, void* dst, hipStream_t st) {
-  quantize(Tiles{src, cols}, rows, cols, dst, st);
+  quantize(Tiles{src, rows, cols}, rows, cols, dst, st);
 }
 
 void launch_mx4_dequantize(const void* src, int rows, int cols, void* dst, int type, int64_t stride, hipStream_t st) {

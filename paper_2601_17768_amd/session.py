@@ -29,6 +29,7 @@ class VerifierSession:
         self.model = B.llm42_model_create(self.cfg, dev_w)
         del dev_w
         self._mx4 = None
+        self._attention4_need = {}
         self._ws = None
         self._ws_key = None
 
@@ -118,7 +119,10 @@ class VerifierSession:
         """One llm42_kv4_attention call.  Returns out."""
         if max_context is None:
             max_context = block_table.shape[1] * B.LLM42_KV_BLOCK
-        need = B.llm42_kv4_attention_workspace_bytes(self.model, q.shape[0], q.shape[1], max_context)
+        key = (q.shape[0], q.shape[1], max_context)
+        need = self._attention4_need.get(key)
+        if need is None:
+            need = self._attention4_need[key] = B.llm42_kv4_attention_workspace_bytes(self.model, *key)
         if self._ws is None or self._ws.numel() < need:
             self._ws = torch.empty(need, dtype=torch.uint8, device=self.device)
         if out is None:
