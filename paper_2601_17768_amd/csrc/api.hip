@@ -282,6 +282,7 @@ struct Fast4 {
   const llm42_mx4_model* m4;
   const llm42_kv_cache* kv4;   // or null
   int splits, split_steps;     // of its attention
+  float* parts;                // scratch of the residual projections
 };
 
 // ... its workspace: that of a decoding step, with room for the partials of the 4-bit attention.
@@ -290,12 +291,12 @@ size_t part_rows4(const llm42_model* m, int num_seqs, int max_context, Fast4& f4
   return f4.splits > 1 ? (size_t)num_seqs * m->cfg.n_kv_heads * f4.splits * m->group : 0;
 }
 
-void attention4(const Fast4& f4, int layer, int num_seqs, int max_context, const Workspace& ws, hipStream_t st) {
+void attention4(const Fast4& f4, int layer, const llm42_kv_cache* kv, int num_seqs, int max_context, const Workspace& ws, hipStream_t st) {
   const llm42_model* m = f4.m4->model;
   const llm42_config& c = m->cfg;
   Attention4 a;
   memset(&a, 0, sizeof a);
-  a.base = (const char*)f4.kv4->kv_base + (size_t)layer * f4.kv4->num_blocks * c.n_kv_heads * mx4::kv_record(c.head_dim);
+  a.base = (char*)f4.kv4->kv_base + (size_t)layer * f4.kv4->num_blocks * c.n_kv_heads * mx4::kv_record(c.head_dim);
   a.num_blocks = f4.kv4->num_blocks;
   a.block_table = f4.kv4->block_table;
   a.max_blocks = f4.kv4->max_blocks_per_seq;
@@ -313,6 +314,10 @@ void attention4(const Fast4& f4, int layer, int num_seqs, int max_context, const
   a.split_steps = f4.split_steps;
   a.part_acc = ws.part_acc;
   a.part_ml = ws.part_ml;
+  const size_t plane = (size_t)kv->num_blocks * c.n_kv_heads * 16 * c.head_dim;
+  a.k_plane = (const uint16_t*)kv->kv_base + (size_t)layer * 2 * plane;
+  a.v_plane = a.k_plane + plane;
+  a.row_blk = ws.row_blk;
   launch_kv4_attention(a, st);
 }
 
@@ -322,10 +327,10 @@ bool run_mlp4(const Fast4& f4, int l, const Workspace& ws, hipStream_t st) {
   const llm42_config& c = m->cfg;
   const llm42_mx4_model::Layer& w = f4.m4->layers[l];
   bool pending;
-  TIMED(LLM42_K_O_PROJ, pending = launch_mx4_residual(w.wo, ws.attn, c.d_model, m->d_attn, ws, st));
+  TIMED(LLM42_K_O_PROJ, pending = launch_mx4_residual(w.wo, ws.attn, c.d_model, m->d_attn, f4.parts, ws, st));
   TIMED(LLM42_K_RMSNORM, launch_rmsnorm(pending, m->layers[l].ffn_norm, c.d_model, c.rms_eps, ws, st));
   TIMED(LLM42_K_GATE_UP, launch_mx4_swiglu(f4.m4, l, ws, st));
-  TIMED(LLM42_K_DOWN, pending = launch_mx4_residual(w.wdown, ws.hidden, c.d_model, m->ffn_k, ws, st));
+  TIMED(LLM42_K_DOWN, pending = launch_mx4_residual(w.wdown, ws.hidden, c.d_model, m->ffn_k, f4.parts, ws, st));
   return pending;
 }
 
@@ -383,12 +388,8 @@ llm42_status run_pass(const llm42_model* m, const llm42_kv_cache* kv, const int3
     TIMED(LLM42_K_RMSNORM, launch_rmsnorm(pending, ly.attn_norm, c.d_model, c.rms_eps, ws, st));
     if (f4) TIMED(LLM42_K_QKV, launch_mx4_qkv(f4->m4, l, kv, ws, st));
     else TIMED(LLM42_K_QKV, launch_gemm_qkv(m, l, kv, window, ws, st));
-    if (kv4) {
-      TIMED(LLM42_K_ATTENTION, launch_kv4_store(m, l, kv, f4->kv4, ws.seq_len, nullptr, num_seqs, 1, nullptr, st));
-      TIMED(LLM42_K_ATTENTION, attention4(*f4, l, num_seqs, max_context, ws, st));
-    } else {
-      TIMED(LLM42_K_ATTENTION, launch_attention(m, l, kv, num_seqs, window, max_context, ws, st));
-    }
+    if (kv4) TIMED(LLM42_K_ATTENTION, attention4(*f4, l, kv, num_seqs, max_context, ws, st));
+    else TIMED(LLM42_K_ATTENTION, launch_attention(m, l, kv, num_seqs, window, max_context, ws, st));
     if (f4) {
       pending = run_mlp4(*f4, l, ws, st);
       continue;
@@ -465,9 +466,12 @@ llm42_status verify_impl(const char* who, const llm42_model* m, const llm42_kv_c
                   (long long)k.max_blocks_per_seq * LLM42_KV_BLOCK);
   }
   Workspace ws = f4 && f4->kv4 ? carve(m, num_seqs, window, max_context, (char*)workspace, true, part_rows4(m, num_seqs, max_context, *f4))
-                               : call_workspace(m, num_seqs, window, max_context, (char*)workspace, workspace_bytes, batch_chosen);
-  if (ws.bytes > workspace_bytes)
-    return fail(LLM42_EWORKSPACE, "%s: workspace %zu < %zu bytes", who, workspace_bytes, ws.bytes);
+                               : call_workspace(m, num_seqs, window, max_context, (char*)workspace,
+                                                f4 ? workspace_bytes - std::min(workspace_bytes, mx4_residual_bytes(num_seqs, padded_rows(num_seqs), m->cfg.d_model))
+                                                   : workspace_bytes, batch_chosen);
+  const size_t parts4 = f4 ? mx4_residual_bytes(ws.m_rows, ws.m_pad, m->cfg.d_model) : 0, need = ws.bytes + parts4;
+  if (need > workspace_bytes) return fail(LLM42_EWORKSPACE, "%s: workspace %zu < %zu bytes", who, workspace_bytes, need);
+  if (f4) f4->parts = (float*)((char*)workspace + ws.bytes);
   return run_pass(m, kv, seq_lens, candidates, window, n_valid, num_seqs, max_context, out_tokens, seq_status,
                   n_dump > 0 ? out_logits : nullptr, dump_seq_ids, n_dump, ws, (hipStream_t)hip_stream, sampling, false, f4);
 }
@@ -773,9 +777,13 @@ llm42_status llm42_decode_step_mx4_workspace_bytes(const llm42_mx4_model* m4, in
   if (!m4) return fail(LLM42_EINVAL, "decode_step_mx4_workspace_bytes: null argument");
   size_t plain = 0, rows = 0;
   if (llm42_status st = llm42_workspace_bytes(m4->model, max_seqs, 1, max_context, &plain)) return st;
-  Fast4 f4{m4, nullptr, 0, 0};
-  for (int n = 1; n <= max_seqs; ++n) rows = std::max(rows, part_rows4(m4->model, n, max_context, f4));
-  *out_bytes = std::max(plain, carve(m4->model, max_seqs, 1, max_context, nullptr, true, rows).bytes);
+  Fast4 f4{m4, nullptr, 0, 0, nullptr};
+  size_t parts = 0;                                              // (it grows with the rows, but from one number of parts to the next)
+  for (int n = 1; n <= max_seqs; ++n) {
+    rows = std::max(rows, part_rows4(m4->model, n, max_context, f4));
+    parts = std::max(parts, mx4_residual_bytes(n, padded_rows(n), m4->model->cfg.d_model));
+  }
+  *out_bytes = std::max(plain, carve(m4->model, max_seqs, 1, max_context, nullptr, true, rows).bytes) + parts;
   return LLM42_OK;
 }
 
@@ -784,7 +792,7 @@ llm42_status llm42_decode_step_mx4(const llm42_mx4_model* m4, const llm42_kv_cac
                                    int32_t* seq_status, void* workspace, size_t workspace_bytes, void* hip_stream,
                                    const llm42_sampling* sampling) {
   if (!m4) return fail(LLM42_EINVAL, "decode_step_mx4: null argument");
-  Fast4 f4{m4, kv4, 0, 0};
+  Fast4 f4{m4, kv4, 0, 0, nullptr};
   return verify_impl("decode_step_mx4", m4->model, kv, seq_lens, tokens, 1, nullptr, num_seqs, max_context, out_tokens, seq_status,
                      nullptr, nullptr, 0, workspace, workspace_bytes, hip_stream, sampling, true, &f4);
 }

@@ -1,5 +1,5 @@
 // The 4-bit cache: K and V from the bf16 cache into it, and what it stands for.
-#include "mx4.h"
+#include "kv4_store.h"
 
 using namespace mx4;
 
@@ -24,24 +24,16 @@ __device__ inline int range_status(int64_t first, int64_t count, int max_count, 
   return __any(bad) ? LLM42_SEQ_BAD_BLOCK : LLM42_SEQ_OK;
 }
 
-// The larger of two magnitudes, half by half, over the 16 lanes of a group.
-__device__ inline uint32_t max_of_16(uint32_t v) {
-#pragma unroll
-  for (int d = 1; d < 16; d <<= 1) v = larger(v, (uint32_t)__shfl_xor((int)v, d));
-  return v;
-}
-
 // One wave per (block of 16 positions, kv head), four heads of a block to a workgroup; blockIdx.y: layer.
 template <int HD>
 __global__ __launch_bounds__(256) void kv4_store_kernel(const uint16_t* __restrict__ kv, Table src, char* __restrict__ kv4, Table dst,
-                                                        int n_kv_heads, int layer0, const int32_t* __restrict__ first_,
+                                                        int n_kv_heads, const int32_t* __restrict__ first_,
                                                         const int32_t* __restrict__ count_, int max_count, int slots,
                                                         int32_t* __restrict__ seq_status) {
-  constexpr int KT = HD / 32;
   const int hg = (n_kv_heads + 3) / 4, at_slot = blockIdx.x / hg;
-  const int s = at_slot / slots, slot = at_slot % slots, layer = layer0 + blockIdx.y;
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, g = lane >> 4, l16 = lane & 15, h = (int)(blockIdx.x % hg) * 4 + wave;
-  const int64_t first = first_[s], count = count_ ? count_[s] : first >= 0;   // (no counts: of sequences that take part one each)
+  const int s = at_slot / slots, slot = at_slot % slots, layer = blockIdx.y;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, h = (int)(blockIdx.x % hg) * 4 + wave;
+  const int64_t first = first_[s], count = count_[s];
   const int status = range_status(first, count, max_count, src, dst, s, lane);
   if (seq_status && blockIdx.y == 0 && slot == 0 && h == 0 && lane == 0) seq_status[s] = status;
   const int block = (int)(first / LLM42_KV_BLOCK) + slot;
@@ -50,73 +42,8 @@ __global__ __launch_bounds__(256) void kv4_store_kernel(const uint16_t* __restri
   const size_t sb = src.ids[(size_t)s * src.width + block], db = dst.ids[(size_t)s * dst.width + block];
   const size_t plane = (size_t)src.num_blocks * n_kv_heads * 16 * HD;
   const uint16_t* kt = kv + (size_t)layer * 2 * plane + (sb * n_kv_heads + h) * 16 * HD;
-  const uint16_t* vt = kt + plane;
   char* rec = kv4 + (((size_t)layer * dst.num_blocks + db) * n_kv_heads + h) * kv_record(HD);
-  u32x4 kw[KT], vw[KT];                            // V: features 32 j + 2 p and + 1, four tokens of each
-#pragma unroll
-  for (int j = 0; j < KT; ++j) kw[j] = vw[j] = (u32x4){0, 0, 0, 0};
-  if (l16 >= lo && l16 < hi) {                     // (a single token is 3 KiB of lines so, 8 as a whole tile)
-#pragma unroll
-    for (int j = 0; j < KT; ++j) kw[j] = *(const u32x4*)(kt + j * 512 + lane * 8);
-  }
-  if (4 * g + 3 >= lo && 4 * g < hi) {
-#pragma unroll
-    for (int j = 0; j < KT; ++j) vw[j] = *(const u32x4*)(vt + v_tile_off(32 * j + 2 * l16, 4 * g));
-  }
-  // K: lane (g, token) has features 32 j + 8 g .. + 7
-  uint32_t kc[KT], ks = 0;
-#pragma unroll
-  for (int j = 0; j < KT; ++j) {
-    uint32_t top = larger_half(larger(larger(kw[j][0], kw[j][1]), larger(kw[j][2], kw[j][3])));
-    top = max(top, (uint32_t)__shfl_xor((int)top, 16));
-    top = max(top, (uint32_t)__shfl_xor((int)top, 32));
-    const uint32_t byte = scale_byte(top);
-    uint32_t word = 0;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) word = put_pair(word, kw[j][e], scale_of(byte, 0), e);
-    kc[j] = byte == 255u ? 0u : word;
-    ks |= byte << (8 * j);
-  }
-  if (l16 >= lo && l16 < hi) {
-    uint32_t* p = (uint32_t*)(rec + lane * KT * 4);
-#pragma unroll
-    for (int j = 0; j < KT; ++j) p[j] = kc[j];
-    if (g == 0) {
-      if constexpr (HD == 128) *(uint32_t*)(rec + 16 * HD + l16 * 4) = ks;
-      else *(uint16_t*)(rec + 16 * HD + l16 * 2) = (uint16_t)ks;
-    }
-  }
-  // V: byte i of word j is token 4 g + i
-  uint32_t vs[KT], vc[KT];
-#pragma unroll
-  for (int j = 0; j < KT; ++j) {
-    const uint32_t pair[2] = {max_of_16(larger(vw[j][0], vw[j][2])), max_of_16(larger(vw[j][1], vw[j][3]))};   // tokens 0, 1 and 2, 3
-    vs[j] = vc[j] = 0;
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      const uint32_t byte = scale_byte(t & 1 ? pair[t >> 1] & 0xFFFF0000u : pair[t >> 1] << 16);
-      const uint32_t two = t & 1 ? vw[j][t >> 1] >> 16 | (vw[j][2 + (t >> 1)] & 0xFFFF0000u) : (vw[j][t >> 1] & 0xFFFFu) | vw[j][2 + (t >> 1)] << 16;
-      vs[j] |= byte << (8 * t);
-      vc[j] = put_pair(vc[j], two, scale_of(byte, 0), t);
-      if (byte == 255u) vc[j] &= ~(255u << (8 * t));
-    }
-  }
-  // tokens of this lane that are in range: a byte of each word of codes and of scales
-  uint32_t take = 0;
-#pragma unroll
-  for (int t = 0; t < 4; ++t)
-    if (4 * g + t >= lo && 4 * g + t < hi) take |= 0xFFu << (8 * t);
-  if (take) {
-    uint32_t* p = (uint32_t*)(rec + 8 * HD + lane * KT * 4);
-    uint32_t* q = (uint32_t*)(rec + 16 * HD + HD / 2 + g * KT * 4);
-    const bool part = take != 0xFFFFFFFFu;         // (other positions share the word: this wave alone writes it)
-#pragma unroll
-    for (int j = 0; j < KT; ++j) p[j] = part ? (p[j] & ~take) | (vc[j] & take) : vc[j];
-    if (l16 == 0) {
-#pragma unroll
-      for (int j = 0; j < KT; ++j) q[j] = part ? (q[j] & ~take) | (vs[j] & take) : vs[j];
-    }
-  }
+  store_positions<HD>(kt, kt + plane, rec, lo, hi, lane);
 }
 
 // The other way.  A wave's values lie in LDS between the cache's order and rows, so that every store is of 256 (head_dim 64: 128) bytes of a
@@ -175,13 +102,13 @@ Table table_of(const llm42_kv_cache* c) { return {c->block_table, c->max_blocks_
 
 }  // namespace
 
-void launch_kv4_store(const llm42_model* m, int layer, const llm42_kv_cache* kv, const llm42_kv_cache* kv4, const int32_t* first,
+void launch_kv4_store(const llm42_model* m, const llm42_kv_cache* kv, const llm42_kv_cache* kv4, const int32_t* first,
                       const int32_t* count, int num_seqs, int max_count, int32_t* seq_status, hipStream_t st) {
   const int slots = (max_count + 14) / 16 + 1;                 // blocks that a run of max_count positions can touch
-  const dim3 grid((unsigned)(num_seqs * slots * ((m->cfg.n_kv_heads + 3) / 4)), layer < 0 ? m->cfg.n_layers : 1);
+  const dim3 grid((unsigned)(num_seqs * slots * ((m->cfg.n_kv_heads + 3) / 4)), m->cfg.n_layers);
   const auto go = [&](auto kernel) {
     kernel<<<grid, 256, 0, st>>>((const uint16_t*)kv->kv_base, table_of(kv), (char*)kv4->kv_base, table_of(kv4), m->cfg.n_kv_heads,
-                                 layer < 0 ? 0 : layer, first, count, max_count, slots, seq_status);
+                                 first, count, max_count, slots, seq_status);
   };
   if (m->cfg.head_dim == 128) go(kv4_store_kernel<128>);
   else go(kv4_store_kernel<64>);

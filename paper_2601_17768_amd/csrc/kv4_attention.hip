@@ -1,7 +1,7 @@
 // Causal attention of the last positions of every sequence over the 4-bit cache.
 #include <type_traits>
 
-#include "mx4.h"
+#include "kv4_store.h"
 
 using namespace mx4;
 
@@ -257,6 +257,16 @@ __global__ __launch_bounds__(64 * kWaves, RB == 1 ? 3 : 2) void kv4_attention_ke
       }
     }
   };
+  // The newest position of a decoding step is in the bf16 cache: the wave whose last step holds it stores it before it reads anything
+  // (nobody else reads that block; a launch of its own took 5 - 7 us).
+  if constexpr (TILES) {
+    if (end == steps && (end - 1 - begin) % kWaves == wave) {
+      const size_t tile = ((size_t)a.row_blk[s] * a.n_kv_heads + kvh) * 16 * HD;
+      const int t = len % LLM42_KV_BLOCK;
+      store_positions<HD>(a.k_plane + tile, a.v_plane + tile, a.base + kvh * (int64_t)kv_record(HD) + ids[len / LLM42_KV_BLOCK] * to_block, t, t + 1, lane);
+      __threadfence_block();
+    }
+  }
   // Steps that every row sees whole, then the last ones.
   const int inner = min(end, (len + 1) / kStep);
   int step = begin + wave;

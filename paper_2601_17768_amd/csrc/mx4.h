@@ -92,7 +92,7 @@ struct llm42_mx4_model {
 
 // Attention over a 4-bit cache: who sees what, and how the work is split.
 struct Attention4 {
-  const char* base;            // the layer's records
+  char* base;                  // the layer's records
   int64_t num_blocks;
   const int32_t* block_table;
   int max_blocks;
@@ -108,6 +108,9 @@ struct Attention4 {
   int splits, split_steps;     // parts of a sequence, steps of 64 keys in each
   float* part_acc;             // [seq][kv head][split][row][head_dim]
   float* part_ml;              // [seq][kv head][split][row][2]
+  // tiles: the layer's K and V in the bf16 cache and a row's block there, from which the newest position is stored first
+  const uint16_t *k_plane, *v_plane;
+  const int32_t* row_blk;
 };
 
 void launch_mx4_quantize(const void* src, int type, int64_t stride, int rows, int cols, void* dst, hipStream_t st);
@@ -122,13 +125,17 @@ size_t mx4_matmul_part_bytes(int n, int k, int rows, int num_cus);
 void launch_mx4_matmul(const void* w, int n, int k, const uint16_t* x, int64_t x_stride, int rows, void* out, int out_type,
                        int64_t out_stride, int num_cus, float* parts, hipStream_t st);
 void launch_mx4_qkv(const llm42_mx4_model* m4, int layer, const llm42_kv_cache* kv, const Workspace& ws, hipStream_t st);
+// Most parts that a residual projection's sum is taken in, and the scratch that takes beside the workspace of the pass.
+inline int mx4_residual_parts(int m_rows) { return m_rows <= 256 ? 8 : m_rows <= 1024 ? 4 : 1; }
+inline size_t mx4_residual_bytes(int m_rows, int m_pad, int d_model) {
+  return mx4_residual_parts(m_rows) > 1 ? 4ull * mx4_residual_parts(m_rows) * m_pad * d_model : 0;
+}
 // true: the residual stream is not complete yet; the halves are in split_part, for the RMSNorm that follows
-bool launch_mx4_residual(const void* w, const uint16_t* x, int n, int k, const Workspace& ws, hipStream_t st);
+bool launch_mx4_residual(const void* w, const uint16_t* x, int n, int k, float* parts, const Workspace& ws, hipStream_t st);
 void launch_mx4_swiglu(const llm42_mx4_model* m4, int layer, const Workspace& ws, hipStream_t st);
 int launch_mx4_logits(const llm42_mx4_model* m4, const llm42_sampling* sampling, const Workspace& ws, hipStream_t st);
 
-// count null: 1 each, of sequences whose `first` is not negative.  layer < 0: all.
-void launch_kv4_store(const llm42_model* m, int layer, const llm42_kv_cache* kv, const llm42_kv_cache* kv4, const int32_t* first,
+void launch_kv4_store(const llm42_model* m, const llm42_kv_cache* kv, const llm42_kv_cache* kv4, const int32_t* first,
                       const int32_t* count, int num_seqs, int max_count, int32_t* seq_status, hipStream_t st);
 void launch_kv4_read(const llm42_model* m, const llm42_kv_cache* kv4, const int32_t* first, const int32_t* count, int num_seqs,
                      int max_count, uint16_t* out_k, uint16_t* out_v, int32_t* seq_status, hipStream_t st);

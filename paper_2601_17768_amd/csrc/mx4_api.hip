@@ -158,7 +158,7 @@ llm42_status llm42_kv4_store(const llm42_model* m, const llm42_kv_cache* kv, con
   if (llm42_status st = check_ranges(who, m, first, count, num_seqs, max_count)) return st;
   if (llm42_status st = check_cache(who, "kv_cache", kv)) return st;
   if (llm42_status st = check_cache(who, "kv4_cache", kv4)) return st;
-  launch_kv4_store(m, -1, kv, kv4, first, count, num_seqs, max_count, seq_status, (hipStream_t)hip_stream);
+  launch_kv4_store(m, kv, kv4, first, count, num_seqs, max_count, seq_status, (hipStream_t)hip_stream);
   return launched(who);
 }
 
@@ -204,7 +204,7 @@ llm42_status llm42_kv4_attention(const llm42_model* m, int32_t layer, const llm4
   plan_kv4_attention(num_seqs, c.n_kv_heads, m->group * window, max_context, m->num_cus, a.splits, a.split_steps);
   const Attention4Workspace ws = carve(m, num_seqs, window, a.splits, (char*)workspace);
   if (ws.bytes > workspace_bytes) return fail(LLM42_EWORKSPACE, "%s: workspace %zu < %zu bytes", who, workspace_bytes, ws.bytes);
-  a.base = (const char*)kv4->kv_base + (size_t)layer * kv4->num_blocks * c.n_kv_heads * mx4::kv_record(c.head_dim);
+  a.base = (char*)kv4->kv_base + (size_t)layer * kv4->num_blocks * c.n_kv_heads * mx4::kv_record(c.head_dim);
   a.num_blocks = kv4->num_blocks;
   a.block_table = kv4->block_table;
   a.max_blocks = kv4->max_blocks_per_seq;
@@ -225,6 +225,8 @@ llm42_status llm42_kv4_attention(const llm42_model* m, int32_t layer, const llm4
   a.max_context = max_context;
   a.part_acc = ws.acc;
   a.part_ml = ws.ml;
+  a.k_plane = a.v_plane = nullptr;
+  a.row_blk = nullptr;
   launch_kv4_attention(a, (hipStream_t)hip_stream);
   return launched(who);
 }

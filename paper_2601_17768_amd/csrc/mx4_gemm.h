@@ -385,7 +385,7 @@ inline Plan plan(int n_blocks, int k_tiles, int rows, int num_cus, int most_part
       const double tiles = (double)((n_blocks + q.bn() - 1) / q.bn()) * ((blocks + q.tb - 1) / q.tb) * parts;
       const double rounds = (double)(((long long)tiles + num_cus - 1) / num_cus), full = tiles / (rounds * num_cus);
       double ns = 2100 + rounds * (q.round_ns + q.k_ns * (1 + 0.01 * q.full * full) * pg * 4);
-      if (parts > 1) ns = (ns + (joined ? 0 : 2600) + parts * (double)rows * n_blocks * 64 / 2840) * 1.1;
+      if (parts > 1) ns = (ns + (joined && parts == 2 ? 0 : 2600) + parts * (double)rows * n_blocks * 64 / 2840) * 1.1;
       if (best.tile < 0 || ns < least) {
         best = {t, 0, parts, pg};
         least = ns;

@@ -29,7 +29,7 @@ class VerifierSession:
         self.model = B.llm42_model_create(self.cfg, dev_w)
         del dev_w
         self._mx4 = None
-        self._attention4_need = {}
+        self._attention4_need, self._decode4_need = {}, {}
         self._ws = None
         self._ws_key = None
 
@@ -136,7 +136,10 @@ class VerifierSession:
         """One llm42_decode_step_mx4 call: the fast path by 4-bit weights, over the 4-bit cache if one is given.  Returns out_tokens."""
         if max_context is None:
             max_context = block_table.shape[1] * B.LLM42_KV_BLOCK
-        need = B.llm42_decode_step_mx4_workspace_bytes(self.mx4, seq_lens.numel(), max_context)
+        key = (seq_lens.numel(), max_context)
+        need = self._decode4_need.get(key)
+        if need is None:
+            need = self._decode4_need[key] = B.llm42_decode_step_mx4_workspace_bytes(self.mx4, *key)
         if self._ws is None or self._ws.numel() < need:
             self._ws = torch.empty(need, dtype=torch.uint8, device=self.device)
         if out_tokens is None:
