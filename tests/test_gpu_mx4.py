@@ -106,6 +106,36 @@ def test_product(rows, n, k, out_dtype):
     assert bool((err <= tol).all()), f"largest error {float(err.max()):.3e}, tolerance there {float(tol.flatten()[err.argmax()]):.3e}"
 
 
+# every tile and number of parts that the choice takes on 256 CUs, with plain rows (columns a multiple of 32) and packed ones
+TILES = [(130, 33000, 260), (130, 33000, 288), (70, 33000, 260), (70, 33000, 288), (70, 16400, 260), (70, 16400, 288), (265, 1000, 8200),
+         (265, 1000, 8192), (525, 6000, 260), (525, 6000, 288), (130, 2000, 8200), (130, 2000, 8192), (9, 33000, 260), (20, 33000, 288),
+         (35, 4112, 8200), (35, 4112, 8192), (35, 16400, 260), (45, 16400, 288), (130, 1000, 8200), (130, 1000, 8192), (35, 8200, 545),
+         (35, 8200, 544), (130, 500, 8200), (130, 500, 8192), (9, 16400, 260), (20, 16400, 288), (70, 1000, 8200), (70, 1000, 8192),
+         (20, 8200, 8192), (9, 4112, 4100), (9, 4112, 4096), (9, 40, 8200), (20, 40, 8192), (9, 40, 4100), (20, 40, 4096), (1, 40, 8200),
+         (5, 5000, 1090), (8, 5000, 1088), (9, 8200, 1090), (16, 8200, 1088), (3, 9000, 2050), (8, 33000, 1024 + 64)]
+
+
+@pytest.mark.parametrize("rows,n,k", TILES)
+def test_product_by_every_tile(rows, n, k):
+    g = torch.Generator(device=DEV).manual_seed(rows + n + k)
+    x = torch.randn(rows, k, generator=g, device=DEV).to(torch.bfloat16)
+    m = Mx4Matrix.quantize(torch.randn(n, k, generator=g, device=DEV))
+    w = m.values(torch.float32)                               # (bit for bit: the tests above)
+    out = torch.full((rows + 1, n + 3), 7.0, device=DEV)
+    m.matmul(x, out=out[:rows, :n])
+    want, tol = product_tolerance(x, w, torch.float32)
+    assert bool(((out[:rows, :n].double() - want).abs() <= tol).all())
+    assert bool((out[rows] == 7.0).all()) and bool((out[:, n:] == 7.0).all())
+
+
+def test_product_without_a_workspace_sums_in_one_piece():
+    x, w = values(24, 4096, torch.bfloat16, 1, False).to(DEV), values(100, 4096, torch.bfloat16, 2, False).to(DEV)
+    m, out = Mx4Matrix.quantize(w), torch.empty(24, 100, device=DEV)
+    B.llm42_mx4_matmul(m.data, x, out)
+    want, tol = product_tolerance(x, m.values(torch.float32), torch.float32)
+    assert bool(((out.double() - want).abs() <= tol).all())
+
+
 def test_product_by_one_hot_rows_returns_the_matrix():
     """Conversion and layout: every column of the matrix, bit for bit, whatever its scale."""
     w = values(45, 288, torch.bfloat16, 3)
