@@ -18,7 +18,8 @@
  * The conventions of llm42.h hold here too: "dev" pointers are device addresses on the current
  * device, calls enqueue on `hip_stream`, allocate nothing (but llm42_mx4_model_create),
  * never synchronise, never read device memory on the host, and may be captured into a
- * graph; nothing in a workspace has to start at zero.  Calls of these functions are
+ * graph; nothing in a workspace has to start at zero.  A workspace belongs to one call at a time: calls (and replays of
+ * captured ones) that share one follow each other on a stream.  Calls of these functions are
  * deterministic, but not independent of the batch as the verifier's are.
  */
 #ifndef LLM42_MX4_H_
@@ -36,7 +37,7 @@ extern "C" {
 
 /* ---- matrices ------------------------------------------------------------------------------------------ */
 
-/* Bytes of a rows x cols matrix in MXFP4, rows and cols >= 1.  The layout inside is the library's own (tiles of 16 rows x
+/* Bytes of a rows x cols matrix in MXFP4, rows 1 .. 2^30 and cols 1 .. 2^26.  The layout inside is the library's own (tiles of 16 rows x
  * 256 columns, padded with zeros: about 4.25 bits a value where cols is a multiple of 256). */
 llm42_status llm42_mx4_bytes(int32_t rows, int32_t cols, size_t* out_bytes);
 
@@ -88,7 +89,7 @@ llm42_status llm42_mx4_matmul(
 
 /* ---- the 4-bit cache ------------------------------------------------------------------------------------ */
 
-/* A 4-bit cache is described by the same llm42_kv_cache as the bf16 one: kv_base (256-byte aligned) holds
+/* A 4-bit cache is described by the same llm42_kv_cache as the bf16 one: kv_base (16-byte aligned) holds
  * llm42_kv4_bytes(model, num_blocks) bytes, [layer][block][kv head] records of 17 * head_dim bytes, block_table says where the
  * blocks of 16 positions of a sequence lie.  It may be the bf16 cache's table (a mirror of it) or one of its own.
  * Nothing in a fresh cache has to be initialised: no call reads a position that was not stored before. */
@@ -96,7 +97,7 @@ llm42_status llm42_kv4_bytes(const llm42_model* model, int64_t num_blocks, size_
 
 /* K and V of positions first[s] .. first[s] + count[s] - 1 of every sequence, all layers, from the bf16 cache into the 4-bit
  * one.  Behind a verifier pass and its commit: first = the length before, count = the committed tokens; behind a prefill: 0 and
- * the length.  No other position is written; two sequences of one call must not store into the same 4-bit block.
+ * the length.  No other position is written; no two of a call's blocks of positions may lie in the same 4-bit block.
  * first[s] < 0 or beyond a table's capacity, count[s] outside 0 .. max_count: LLM42_SEQ_BAD_LENGTH; a needed entry of either
  * table out of range: LLM42_SEQ_BAD_BLOCK; nothing of such a sequence is stored. */
 llm42_status llm42_kv4_store(
@@ -127,10 +128,11 @@ llm42_status llm42_kv4_read(
 
 /* Attention of one layer over the 4-bit cache.  Row (s, i), i < n_valid[s], is the query at position seq_lens[s] + i and sees
  * positions 0 .. seq_lens[s] + i, all of which must have been stored; its head h uses kv head h / (n_q_heads / n_kv_heads):
- * out = softmax(q . k / sqrt(head_dim)) v.  Weights are rounded to bf16 before they multiply V; sums are fp32.
+ * out = softmax(q . k / sqrt(head_dim)) v.  Weights are rounded to bf16 before they multiply V; sums are fp32, of weights up to 2^8,
+ * so that magnitudes of V up to about 2^119 / max_context stay in range.
  * q and out: bf16 rows of n_q_heads * head_dim, row (s, i) at (s * window + i) * stride elements; both 16-byte aligned, strides
  * multiples of 8 and at least that long.  Rows that take no part (i >= n_valid[s]; a sequence whose status is not
- * LLM42_SEQ_OK; n_valid[s] may be 0) are left as they were.  max_context: as in llm42_verify_window.
+ * LLM42_SEQ_OK; n_valid[s] may be 0) are left as they were.  max_context: as in llm42_verify_window, up to 2^30.
  * workspace: llm42_kv4_attention_workspace_bytes, 256-byte aligned. */
 llm42_status llm42_kv4_attention_workspace_bytes(const llm42_model* model, int32_t num_seqs, int32_t window, int32_t max_context,
                                                  size_t* out_bytes);
@@ -162,9 +164,9 @@ llm42_status llm42_mx4_model_create(const llm42_model* model, llm42_mx4_model** 
 void         llm42_mx4_model_destroy(llm42_mx4_model* mx4);
 
 /* llm42_decode_step_sampled by the 4-bit copy: the same arguments, effects, errors and status.  K and V of the input tokens are
- * written to the bf16 cache as there.  kv4_cache NULL: attention over the bf16 cache.  Else they are stored into the 4-bit cache as
+ * written to the bf16 cache as there.  workspace: llm42_decode_step_mx4_workspace_bytes, 256-byte aligned.  kv4_cache NULL: attention over the bf16 cache.  Else they are stored into the 4-bit cache as
  * well, and attention reads that: positions 0 .. seq_lens[s] - 1 must have been stored, and its block table needs entries for
- * position seq_lens[s] too.  The verifier overwrites the window's entries of the bf16 cache; those of the 4-bit cache are
+ * position seq_lens[s] too (a block that no other sequence of the call has there; max_context up to 2^30).  The verifier overwrites the window's entries of the bf16 cache; those of the 4-bit cache are
  * overwritten by llm42_kv4_store behind the commit. */
 llm42_status llm42_decode_step_mx4_workspace_bytes(const llm42_mx4_model* mx4, int32_t max_seqs, int32_t max_context,
                                                    size_t* out_bytes);

@@ -444,7 +444,7 @@ def llm42_kv4_attention_workspace_bytes(model: int, num_seqs: int, window: int, 
 def llm42_kv4_attention(model: int, layer: int, kv4_base: torch.Tensor, kv4_num_blocks: int, kv4_block_table: torch.Tensor,
                         q: torch.Tensor, seq_lens: torch.Tensor, n_valid: Optional[torch.Tensor], max_context: int, out: torch.Tensor,
                         workspace: torch.Tensor, seq_status: Optional[torch.Tensor] = None, stream=None) -> None:
-    """q, out: bfloat16 [num_seqs, window, n_q_heads, head_dim]; the rows of a token may lie apart, a token's heads may not."""
+    """q, out: bfloat16 [num_seqs, window, n_q_heads, head_dim] with the model's heads; the rows of a token may lie apart, a token's heads may not."""
     num_seqs = seq_lens.numel()
     _on_current_device(kv4_base, kv4_block_table, q, seq_lens, n_valid, out, workspace, seq_status)
     if q.dim() != 4 or q.shape != out.shape or q.shape[0] != num_seqs:

@@ -459,8 +459,9 @@ llm42_status verify_impl(const char* who, const llm42_model* m, const llm42_kv_c
   if ((uintptr_t)workspace % 256) return fail(LLM42_EWORKSPACE, "%s: workspace not 256-byte aligned", who);
   if (f4 && f4->kv4) {
     const llm42_kv_cache& k = *f4->kv4;
-    if (!k.kv_base || !k.block_table || k.num_blocks < 1 || k.max_blocks_per_seq < 1 || (uintptr_t)k.kv_base % 256)
+    if (!k.kv_base || !k.block_table || k.num_blocks < 1 || k.max_blocks_per_seq < 1 || (uintptr_t)k.kv_base % 16)
       return fail(LLM42_EINVAL, "%s: bad kv4_cache view", who);
+    if (max_context > kMostContext4) return fail(LLM42_EINVAL, "%s: max_context must be 1..%d", who, kMostContext4);
     if ((int64_t)max_context > (int64_t)k.max_blocks_per_seq * LLM42_KV_BLOCK)
       return fail(LLM42_ECAPACITY, "%s: max_context %d exceeds the 4-bit cache's block-table capacity %lld", who, max_context,
                   (long long)k.max_blocks_per_seq * LLM42_KV_BLOCK);
@@ -774,7 +775,8 @@ void llm42_mx4_model_destroy(llm42_mx4_model* q) {
 }
 
 llm42_status llm42_decode_step_mx4_workspace_bytes(const llm42_mx4_model* m4, int32_t max_seqs, int32_t max_context, size_t* out_bytes) {
-  if (!m4) return fail(LLM42_EINVAL, "decode_step_mx4_workspace_bytes: null argument");
+  if (!m4 || !out_bytes) return fail(LLM42_EINVAL, "decode_step_mx4_workspace_bytes: null argument");
+  if (max_context > kMostContext4) return fail(LLM42_EINVAL, "decode_step_mx4_workspace_bytes: max_context must be 1..%d", kMostContext4);
   size_t plain = 0, rows = 0;
   if (llm42_status st = llm42_workspace_bytes(m4->model, max_seqs, 1, max_context, &plain)) return st;
   Fast4 f4{m4, nullptr, 0, 0, nullptr};

@@ -1,4 +1,6 @@
 // The 4-bit cache: K and V from the bf16 cache into it, and what it stands for.
+#include <algorithm>
+
 #include "kv4_store.h"
 
 using namespace mx4;
@@ -98,13 +100,16 @@ __global__ __launch_bounds__(256) void kv4_read_kernel(const char* __restrict__ 
   store(out_v);
 }
 
+// Blocks that a run of max_count positions can touch, of those that a table names.
+int slots_of(int max_count, int width) { return (int)std::min<int64_t>(((int64_t)max_count + 14) / 16 + 1, width); }
+
 Table table_of(const llm42_kv_cache* c) { return {c->block_table, c->max_blocks_per_seq, c->num_blocks}; }
 
 }  // namespace
 
 void launch_kv4_store(const llm42_model* m, const llm42_kv_cache* kv, const llm42_kv_cache* kv4, const int32_t* first,
                       const int32_t* count, int num_seqs, int max_count, int32_t* seq_status, hipStream_t st) {
-  const int slots = (max_count + 14) / 16 + 1;                 // blocks that a run of max_count positions can touch
+  const int slots = slots_of(max_count, std::min(kv->max_blocks_per_seq, kv4->max_blocks_per_seq));
   const dim3 grid((unsigned)(num_seqs * slots * ((m->cfg.n_kv_heads + 3) / 4)), m->cfg.n_layers);
   const auto go = [&](auto kernel) {
     kernel<<<grid, 256, 0, st>>>((const uint16_t*)kv->kv_base, table_of(kv), (char*)kv4->kv_base, table_of(kv4), m->cfg.n_kv_heads,
@@ -116,7 +121,7 @@ void launch_kv4_store(const llm42_model* m, const llm42_kv_cache* kv, const llm4
 
 void launch_kv4_read(const llm42_model* m, const llm42_kv_cache* kv4, const int32_t* first, const int32_t* count, int num_seqs,
                      int max_count, uint16_t* out_k, uint16_t* out_v, int32_t* seq_status, hipStream_t st) {
-  const int slots = (max_count + 14) / 16 + 1;
+  const int slots = slots_of(max_count, kv4->max_blocks_per_seq);
   const dim3 grid((unsigned)(num_seqs * slots * ((m->cfg.n_kv_heads + 3) / 4)), m->cfg.n_layers);
   const auto go = [&](auto kernel) {
     kernel<<<grid, 256, 0, st>>>((const char*)kv4->kv_base, table_of(kv4), m->cfg.n_kv_heads, first, count, num_seqs, max_count, slots,

@@ -90,6 +90,8 @@ struct llm42_mx4_model {
   char* lm_head;
 };
 
+constexpr int32_t kMostContext4 = 1 << 30;   // (positions and steps of keys past it stay within 32 bits)
+
 // Attention over a 4-bit cache: who sees what, and how the work is split.
 struct Attention4 {
   char* base;                  // the layer's records

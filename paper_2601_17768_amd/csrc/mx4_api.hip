@@ -20,6 +20,9 @@ int num_cus() {
   return cus;
 }
 
+// Largest matrix and context: index arithmetic in 32 bits stays in range below them.
+constexpr int32_t kMostRows = 1 << 30, kMostCols = 1 << 26;
+
 bool known_type(int32_t t) { return t == LLM42_BF16 || t == LLM42_F32; }
 size_t size_of(int32_t t) { return t == LLM42_F32 ? 4 : 2; }
 
@@ -32,7 +35,8 @@ llm42_status launched(const char* who) {
 llm42_status check_matrix(const char* who, const void* packed, size_t bytes, int32_t rows, int32_t cols, const void* plain, int32_t type,
                           int64_t stride) {
   if (!packed || !plain) return fail(LLM42_EINVAL, "%s: null argument", who);
-  if (rows < 1 || cols < 1) return fail(LLM42_EINVAL, "%s: rows and cols must be positive", who);
+  if (rows < 1 || cols < 1 || rows > kMostRows || cols > kMostCols)
+    return fail(LLM42_EINVAL, "%s: a matrix has 1..%d rows and 1..%d columns", who, kMostRows, kMostCols);
   if (!known_type(type)) return fail(LLM42_EINVAL, "%s: unknown element type %d", who, type);
   if (stride < cols) return fail(LLM42_EINVAL, "%s: stride %lld is less than cols", who, (long long)stride);
   if ((uintptr_t)plain % size_of(type)) return fail(LLM42_EINVAL, "%s: plain array not aligned to its type", who);
@@ -87,7 +91,7 @@ llm42_status check_attention(const char* who, const llm42_model* m, int32_t num_
   if (window < 1 || window > LLM42_MAX_WINDOW) return fail(LLM42_EINVAL, "%s: window must be 1..%d", who, LLM42_MAX_WINDOW);
   if (num_seqs < 1 || (int64_t)num_seqs * window > LLM42_MAX_ROWS)
     return fail(LLM42_EINVAL, "%s: num_seqs * window must be 1..%d", who, LLM42_MAX_ROWS);
-  if (max_context < 1) return fail(LLM42_EINVAL, "%s: max_context < 1", who);
+  if (max_context < 1 || max_context > kMostContext4) return fail(LLM42_EINVAL, "%s: max_context must be 1..%d", who, kMostContext4);
   return LLM42_OK;
 }
 
@@ -97,7 +101,8 @@ extern "C" {
 
 llm42_status llm42_mx4_bytes(int32_t rows, int32_t cols, size_t* out_bytes) {
   if (!out_bytes) return fail(LLM42_EINVAL, "mx4_bytes: null argument");
-  if (rows < 1 || cols < 1) return fail(LLM42_EINVAL, "mx4_bytes: rows and cols must be positive");
+  if (rows < 1 || cols < 1 || rows > kMostRows || cols > kMostCols)
+    return fail(LLM42_EINVAL, "mx4_bytes: a matrix has 1..%d rows and 1..%d columns", kMostRows, kMostCols);
   *out_bytes = mx4::matrix_bytes(rows, cols);
   return LLM42_OK;
 }
@@ -118,7 +123,8 @@ llm42_status llm42_mx4_dequantize(const void* src, size_t src_bytes, int32_t row
 
 llm42_status llm42_mx4_matmul_workspace_bytes(int32_t rows, int32_t n, int32_t k, size_t* out_bytes) {
   if (!out_bytes) return fail(LLM42_EINVAL, "mx4_matmul_workspace_bytes: null argument");
-  if (rows < 1 || rows > LLM42_MAX_ROWS || n < 1 || k < 1) return fail(LLM42_EINVAL, "mx4_matmul_workspace_bytes: sizes out of range");
+  if (rows < 1 || rows > LLM42_MAX_ROWS || n < 1 || k < 1 || n > kMostRows || k > kMostCols)
+    return fail(LLM42_EINVAL, "mx4_matmul_workspace_bytes: sizes out of range");
   *out_bytes = packed_x_bytes(rows, k) + mx4_matmul_part_bytes(n, k, rows, num_cus());
   return LLM42_OK;
 }

@@ -24,6 +24,9 @@ from . import binding as B
 from .session import VerifierSession
 
 
+FAST_PATHS = ("bf16", "mx4", "mx4_cache")
+
+
 @dataclass
 class DvrStats:
     iterations: int = 0
@@ -42,11 +45,12 @@ def generate(sess: VerifierSession, kv: torch.Tensor, block_table: torch.Tensor,
     seq_lens (int32 [B], device) is advanced in place; first_tokens (int32 [B]) are the consistent
     tokens T_0 whose K/V are not yet cached.  `sampling` (binding.Sampling or None = greedy) is
     used by the fast path and by the verifier alike.  `fast`: "bf16" (llm42_decode_step), "mx4" (4-bit weights)
-    or "mx4_cache" (4-bit weights and a 4-bit cache, which mirrors kv's blocks and is made here).  Returns (tokens [B, max_new] on the host, DvrStats).
+    or "mx4_cache" (4-bit weights and a 4-bit cache, which mirrors kv's blocks and is made here).
+    Returns (tokens [B, max_new] on the host, DvrStats).
     The cache must have room for seq_lens + max_new + 2 * window positions per sequence."""
     if window < 2:
         raise ValueError("the loop needs at least one candidate per window")
-    if fast not in ("bf16", "mx4", "mx4_cache"):
+    if fast not in FAST_PATHS:
         raise ValueError(f"unknown fast path {fast!r}")
     dev = sess.device
     n_seq = seq_lens.numel()

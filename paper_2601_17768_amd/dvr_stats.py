@@ -2,9 +2,11 @@
 paper's rollback / recompute table, section 5.1) on seeded synthetic prompts and random-init weights.
 
     python -m paper_2601_17768_amd.dvr_stats [--layers 32] [--groups 1,8,24] [--windows 16,32,64] [--new 128]
+        [--fast bf16|mx4|mx4_cache]
 
 For every (group size, window) the loop of paper_2601_17768_amd/dvr.py generates `--new` tokens per
-sequence: fast-path candidates from llm42_decode_step (whose reduction order follows the group size),
+sequence: fast-path candidates from llm42_decode_step (whose reduction order follows the group size; with
+`--fast mx4` or `mx4_cache` from llm42_decode_step_mx4, on 4-bit weights and the bf16 or a 4-bit cache),
 verification by llm42_verify_window, commit by llm42_commit_rollback.  Reported per configuration:
 windows verified, windows with a rollback, candidates recomputed (count and share of all fast-path
 tokens), and whether the committed stream of sequence 0 equals the one it gets when it runs alone -
@@ -35,6 +37,7 @@ def main():
     ap.add_argument("--windows", default="16,32,64")
     ap.add_argument("--new", type=int, default=128, help="tokens to commit per sequence")
     ap.add_argument("--prompt", default="32,256", help="prompt lengths: uniform in [lo, hi]")
+    ap.add_argument("--fast", choices=dvr.FAST_PATHS, default="bf16", help="the fast path's weights and cache")
     args = ap.parse_args()
     groups = [int(x) for x in args.groups.split(",")]
     windows = [int(x) for x in args.windows.split(",")]
@@ -63,7 +66,7 @@ def main():
             kv, bt, lens, first = state(prompts[:g])
             torch.cuda.synchronize()
             t0 = time.perf_counter()
-            toks, st = dvr.generate(sess, kv, bt, lens, first, args.new, window)
+            toks, st = dvr.generate(sess, kv, bt, lens, first, args.new, window, fast=args.fast)
             torch.cuda.synchronize()
             dt = time.perf_counter() - t0
             if g == 1:
@@ -82,7 +85,7 @@ def main():
             del kv
     sess.close()
     ok = all(r["stream_equals_alone"] in (True, None) for r in rows)
-    print(json.dumps({"n_layers": args.layers, "new_tokens": args.new, "rows": rows, "all_streams_equal": ok}), flush=True)
+    print(json.dumps({"n_layers": args.layers, "new_tokens": args.new, "fast": args.fast, "rows": rows, "all_streams_equal": ok}), flush=True)
     if not ok:
         sys.exit("a committed stream depended on the group")
 

@@ -32,6 +32,7 @@ class VerifierSession:
         self._attention4_need, self._decode4_need = {}, {}
         self._ws = None
         self._ws_key = None
+        self._ws_captured, self._ws_kept = False, []
 
     def close(self):
         if self.model:
@@ -55,9 +56,15 @@ class VerifierSession:
         return kv
 
     def workspace(self, num_seqs: int, window: int, max_context: int) -> torch.Tensor:
-        need = B.llm42_workspace_bytes(self.model, num_seqs, window, max_context)
+        return self._room(B.llm42_workspace_bytes(self.model, num_seqs, window, max_context))
+
+    def _room(self, need: int) -> torch.Tensor:
+        """The session's workspace, of `need` bytes or more.  One that a captured call uses is kept when it is outgrown: the graph still writes it."""
         if self._ws is None or self._ws.numel() < need:
-            self._ws = torch.empty(need, dtype=torch.uint8, device=self.device)
+            if self._ws_captured:
+                self._ws_kept.append(self._ws)
+            self._ws, self._ws_captured = torch.empty(need, dtype=torch.uint8, device=self.device), False
+        self._ws_captured |= torch.cuda.is_current_stream_capturing()
         return self._ws
 
     def verify(self, kv: torch.Tensor, block_table: torch.Tensor, seq_lens: torch.Tensor,
@@ -85,8 +92,10 @@ class VerifierSession:
     # ---- the fast path in 4 bits ----
     @property
     def mx4(self) -> int:
-        """Handle of the model's 4-bit copy, made when it is first asked for."""
+        """Handle of the model's 4-bit copy, made when it is first asked for (which no graph can hold: ask before a capture)."""
         if not self._mx4:
+            if torch.cuda.is_current_stream_capturing():
+                raise RuntimeError("the 4-bit copy of the model must be made before a capture")
             self._mx4 = B.llm42_mx4_model_create(self.model)
         return self._mx4
 
@@ -117,17 +126,18 @@ class VerifierSession:
                       n_valid: Optional[torch.Tensor] = None, max_context: Optional[int] = None, out: Optional[torch.Tensor] = None,
                       seq_status: Optional[torch.Tensor] = None) -> torch.Tensor:
         """One llm42_kv4_attention call.  Returns out."""
+        if q.dim() != 4 or tuple(q.shape[2:]) != (self.shape.n_q_heads, self.shape.head_dim):
+            raise ValueError(f"q must be [num_seqs, window, {self.shape.n_q_heads}, {self.shape.head_dim}]")
         if max_context is None:
             max_context = block_table.shape[1] * B.LLM42_KV_BLOCK
         key = (q.shape[0], q.shape[1], max_context)
         need = self._attention4_need.get(key)
         if need is None:
             need = self._attention4_need[key] = B.llm42_kv4_attention_workspace_bytes(self.model, *key)
-        if self._ws is None or self._ws.numel() < need:
-            self._ws = torch.empty(need, dtype=torch.uint8, device=self.device)
         if out is None:
             out = torch.zeros_like(q)
-        B.llm42_kv4_attention(self.model, layer, kv4, kv4.shape[1], block_table, q, seq_lens, n_valid, max_context, out, self._ws, seq_status)
+        B.llm42_kv4_attention(self.model, layer, kv4, kv4.shape[1], block_table, q, seq_lens, n_valid, max_context, out, self._room(need),
+                              seq_status)
         return out
 
     def decode_mx4(self, kv: torch.Tensor, block_table: torch.Tensor, seq_lens: torch.Tensor, tokens: torch.Tensor,
@@ -140,13 +150,11 @@ class VerifierSession:
         need = self._decode4_need.get(key)
         if need is None:
             need = self._decode4_need[key] = B.llm42_decode_step_mx4_workspace_bytes(self.mx4, *key)
-        if self._ws is None or self._ws.numel() < need:
-            self._ws = torch.empty(need, dtype=torch.uint8, device=self.device)
         if out_tokens is None:
             out_tokens = torch.empty(seq_lens.numel(), dtype=torch.int32, device=self.device)
         table4 = None if kv4 is None else block_table if kv4_block_table is None else kv4_block_table
         B.llm42_decode_step_mx4(self.model, self.mx4, kv, kv.shape[2], block_table, kv4, 0 if kv4 is None else kv4.shape[1], table4, seq_lens,
-                                tokens, max_context, out_tokens, self._ws, seq_status, sampling=sampling)
+                                tokens, max_context, out_tokens, self._room(need), seq_status, sampling=sampling)
         return out_tokens
 
     def commit(self, candidates: torch.Tensor, out_tokens: torch.Tensor, seq_lens: torch.Tensor,
@@ -173,14 +181,12 @@ class VerifierSession:
         if cached is None:
             cached = torch.zeros(n_seq, dtype=torch.int32, device=self.device)
         max_context = min(block_table.shape[1] * B.LLM42_KV_BLOCK, self.cfg.max_position)
-        need = B.llm42_prefill_workspace_bytes(self.model, n_seq, window, max_context)
-        if self._ws is None or self._ws.numel() < need:
-            self._ws = torch.empty(need, dtype=torch.uint8, device=self.device)
+        ws = self._room(B.llm42_prefill_workspace_bytes(self.model, n_seq, window, max_context))
         first = torch.empty(n_seq, dtype=torch.int32, device=self.device)
         status = torch.empty(n_seq, dtype=torch.int32, device=self.device)
         B.llm42_prefill(self.model, kv, kv.shape[2], block_table, cached, torch.as_tensor(flat, device=self.device),
                         torch.as_tensor(offsets, device=self.device), int(lens.max()), window, max_context, first,
-                        self._ws, status, sampling=sampling)
+                        ws, status, sampling=sampling)
         if int(status.max()) != 0:
             raise RuntimeError(f"prefill: sequence status {status.tolist()}")
         return first

@@ -1,4 +1,8 @@
 """The 4-bit cache on the GPU: storing and reading it bit for bit, attention over it against float64, the fast path that runs on it."""
+import ctypes
+import json
+import math
+
 import numpy as np
 import pytest
 import torch
@@ -6,7 +10,7 @@ import torch
 import mx4_reference as ref
 from helpers import orc, wl, oracle_cfg, randomize_gains
 from paper_2601_17768_amd import binding as B
-from paper_2601_17768_amd import dvr, kv_layout
+from paper_2601_17768_amd import dvr, dvr_stats, kv_layout
 from paper_2601_17768_amd.session import VerifierSession
 
 pytestmark = pytest.mark.gpu
@@ -199,8 +203,170 @@ def test_attention_of_rows_apart_and_of_flagged_sequences():
     for bad in (q.transpose(1, 2), q.float(), q[:, :, :, :32], q[:2]):
         with pytest.raises(ValueError):
             sess.kv4_attention(0, kv4, c.bt, bad, lens, out=torch.zeros_like(bad))
-    with pytest.raises(B.Llm42Error):                            # rows of fewer heads than the model has
-        sess.kv4_attention(0, kv4, c.bt, q[:, :, :2].contiguous(), lens)
+    for few in (q[:, :, :2], q[:, :, :2].contiguous()):          # rows of fewer heads than the model has
+        with pytest.raises(ValueError):
+            sess.kv4_attention(0, kv4, c.bt, few, lens)
+    ws = torch.empty(1 << 20, dtype=torch.uint8, device=DEV)
+    with pytest.raises(B.Llm42Error):
+        B.llm42_kv4_attention(sess.model, 0, kv4, kv4.shape[1], c.bt, q[:, :, :2].contiguous(), lens, None, 80, torch.zeros_like(q[:, :, :2]), ws)
+    sess.close()
+
+
+def test_attention_store_and_read_refuse_at_the_c_entry():
+    """Addresses are real, so that a call which were not refused would be harmless."""
+    lib, sess = B.load_library(), session(2, 2, 64)
+    c = Cache(sess, [50, 50])
+    kv4, q, lens = c.mirror(sess), torch.zeros(2, 3, 4, 64, dtype=torch.bfloat16, device=DEV), i32([10, 10])
+    need = B.llm42_kv4_attention_workspace_bytes(sess.model, 2, 3, 64)
+    ws = torch.empty(need + 512, dtype=torch.uint8, device=DEV)
+    view = lambda **k: B.KVCache(*{**dict(base=kv4.data_ptr(), blocks=kv4.shape[1], table=c.bt.data_ptr(), width=4), **k}.values())
+    kv = lambda **k: view(**{**dict(base=c.kv.data_ptr()), **k})
+    p = lambda t, off=0: t.data_ptr() + off
+    base = dict(model=sess.model, layer=0, kv4=view(), q=p(q), qs=256, lens=p(lens), window=3, valid=None, num=2, ctx=64, out=p(q), os=256,
+                status=None, ws=p(ws), bytes=need, stream=None)
+    for bad, code in [(dict(model=None), B.LLM42_EINVAL), (dict(layer=2), B.LLM42_EINVAL), (dict(q=None), B.LLM42_EINVAL),
+                      (dict(out=None), B.LLM42_EINVAL), (dict(lens=None), B.LLM42_EINVAL), (dict(ws=None), B.LLM42_EINVAL),
+                      (dict(q=p(q, 8)), B.LLM42_EINVAL), (dict(out=p(q, 2)), B.LLM42_EINVAL), (dict(qs=255), B.LLM42_EINVAL),
+                      (dict(qs=260), B.LLM42_EINVAL), (dict(os=248), B.LLM42_EINVAL), (dict(window=0), B.LLM42_EINVAL),
+                      (dict(window=B.LLM42_MAX_WINDOW + 1), B.LLM42_EINVAL), (dict(num=0), B.LLM42_EINVAL),
+                      (dict(num=B.LLM42_MAX_ROWS // 3 + 1), B.LLM42_EINVAL), (dict(ctx=0), B.LLM42_EINVAL), (dict(ctx=65), B.LLM42_ECAPACITY),
+                      (dict(ctx=2 ** 30 + 1), B.LLM42_EINVAL), (dict(ws=p(ws, 16)), B.LLM42_EWORKSPACE), (dict(bytes=need - 1), B.LLM42_EWORKSPACE),
+                      (dict(kv4=view(base=None)), B.LLM42_EINVAL), (dict(kv4=view(base=kv4.data_ptr() + 8)), B.LLM42_EINVAL),
+                      (dict(kv4=view(table=None)), B.LLM42_EINVAL), (dict(kv4=view(blocks=0)), B.LLM42_EINVAL), (dict(kv4=view(width=0)), B.LLM42_EINVAL)]:
+        a = {**base, **bad}
+        a["kv4"] = ctypes.byref(a["kv4"])
+        assert lib.llm42_kv4_attention(*a.values()) == code, bad
+    base = dict(model=sess.model, kv=kv(), kv4=view(), first=p(lens), count=p(lens), num=2, most=64, status=None, stream=None)
+    for bad in (dict(model=None), dict(first=None), dict(count=None), dict(num=0), dict(most=0), dict(num=2 ** 31 - 1, most=2 ** 31 - 1),
+                dict(kv=kv(base=None)), dict(kv=kv(table=None)), dict(kv4=view(base=None)), dict(kv4=view(blocks=0))):
+        a = {**base, **bad}
+        assert lib.llm42_kv4_store(a["model"], ctypes.byref(a["kv"]), ctypes.byref(a["kv4"]), *list(a.values())[3:]) == B.LLM42_EINVAL, bad
+        if "kv" not in bad:
+            out = torch.zeros(2 * 2 * 64 * 2 * 64, dtype=torch.bfloat16, device=DEV)
+            assert lib.llm42_kv4_read(a["model"], ctypes.byref(a["kv4"]), a["first"], a["count"], a["num"], a["most"], p(out), p(out), None,
+                                      None) == B.LLM42_EINVAL, bad
+    out = torch.zeros(2 * 2 * 64 * 2 * 64, dtype=torch.bfloat16, device=DEV)
+    for k, v in ((None, p(out)), (p(out), None), (p(out, 8), p(out))):
+        assert lib.llm42_kv4_read(sess.model, ctypes.byref(view()), p(lens), p(lens), 2, 64, k, v, None, None) == B.LLM42_EINVAL
+    m4, size = sess.mx4, ctypes.c_size_t()
+    assert lib.llm42_decode_step_mx4_workspace_bytes(m4, 2, 64, None) == B.LLM42_EINVAL
+    assert lib.llm42_decode_step_mx4_workspace_bytes(m4, 0, 64, ctypes.byref(size)) == B.LLM42_EINVAL
+    assert lib.llm42_mx4_model_create(sess.model, None) == B.LLM42_EINVAL
+    assert lib.llm42_decode_step_mx4_workspace_bytes(m4, 2, 64, ctypes.byref(size)) == B.LLM42_OK
+    need = size.value
+    ws, tok = torch.empty(need + 512, dtype=torch.uint8, device=DEV), i32([1, 1])
+    base = dict(m4=m4, kv=kv(), kv4=view(), lens=p(lens), tok=p(tok), num=2, ctx=64, out=p(tok), status=None, ws=p(ws), bytes=need, stream=None,
+                sampling=None)
+    for bad, code in [(dict(m4=None), B.LLM42_EINVAL), (dict(lens=None), B.LLM42_EINVAL), (dict(tok=None), B.LLM42_EINVAL), (dict(out=None), B.LLM42_EINVAL),
+                      (dict(num=0), B.LLM42_EINVAL), (dict(ctx=65), B.LLM42_ECAPACITY), (dict(kv4=view(width=3)), B.LLM42_ECAPACITY),
+                      (dict(kv4=view(base=None)), B.LLM42_EINVAL), (dict(kv4=view(table=None)), B.LLM42_EINVAL), (dict(kv=kv(base=None)), B.LLM42_EINVAL),
+                      (dict(ws=p(ws, 128)), B.LLM42_EWORKSPACE), (dict(bytes=4096), B.LLM42_EWORKSPACE),
+                      (dict(sampling=ctypes.byref(B.Sampling(-1.0, 0, None))), B.LLM42_EINVAL)]:
+        a = {**base, **bad}
+        a["kv"], a["kv4"] = ctypes.byref(a["kv"]), ctypes.byref(a["kv4"])
+        assert lib.llm42_decode_step_mx4(*a.values()) == code, bad
+    torch.cuda.synchronize()
+    sess.close()
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+def test_attention_rows_do_not_see_a_later_nan(hd):
+    """A NaN in K or V of one position of the window: the rows before it keep their bits, those from it on have the NaN - of V only in the
+    32 features that share its scale.  (Behind 3000 positions in parts, and at every place in a step of keys.)"""
+    sess = session(2, 4, hd)
+    lens, window = [0, 50, 60, 63, 64, 3000], 13
+    c, kv4, q = check_attention(sess, lens, None, window)
+    qd, at = q.to(DEV), 5
+    clean = sess.kv4_attention(1, kv4, c.bt, qd, i32(lens))
+    for which, value in (("k", math.nan), ("v", math.nan), ("v", math.inf), ("k", -math.inf)):
+        for i, a in enumerate(lens):
+            k, v = c.k[i].clone(), c.v[i].clone()
+            (k if which == "k" else v)[1, a + at, 1, 33] = value
+            kv_layout.write_tokens(c.kv, c.bt[i], k, v)
+        got = sess.kv4_attention(1, c.mirror(sess), c.bt, qd, i32(lens))
+        assert torch.equal(got[:, :at], clean[:, :at]) and torch.equal(got[:, at:, :4], clean[:, at:, :4])
+        nan = torch.isnan(got[:, at:, 4:])
+        if which == "k":
+            assert bool(nan.all())
+        else:
+            assert bool(nan[..., 32:64].all()) and not bool(nan[..., :32].any()) and not bool(nan[..., 64:].any())
+            assert torch.equal(got[:, at:, 4:, :32], clean[:, at:, 4:, :32]) and torch.equal(got[:, at:, 4:, 64:], clean[:, at:, 4:, 64:])
+    sess.close()
+
+
+def test_attention_of_empty_windows_in_parts():
+    sess = session(2, 4, 128)
+    check_attention(sess, [5000, 0, 4000, 77], [0, 0, 1, 3], 5)
+    check_attention(sess, [5000, 0], [0, 0], 1)
+    sess.close()
+
+
+def test_a_cache_of_more_than_4_gib():
+    """Blocks at both ends of it, and their offsets beyond 32 bits."""
+    sess = session(8, 4, 128, layers=1)
+    c = Cache(sess, [40, 100])
+    blocks = 260000
+    kv, kv4 = torch.empty((1, 2, blocks) + tuple(c.kv.shape[3:]), dtype=torch.bfloat16, device=DEV), sess.kv4_cache(blocks)
+    assert kv4.numel() > 2 ** 32 and kv.shape[3:] == c.kv.shape[3:] and c.kv.shape[2] < 200
+    far = c.bt.clone()
+    far[c.bt >= 5] += blocks - c.kv.shape[2]
+    kv[:, :, :5] = c.kv[:, :, :5]
+    kv[:, :, 5 + blocks - c.kv.shape[2]:] = c.kv[:, :, 5:]
+    near, n = c.mirror(sess), i32([40, 100])
+    sess.kv4_store(kv, kv4, far, i32([0, 0]), n, 100)
+    for a, b in zip(sess.kv4_read(kv4, far, i32([0, 0]), n, 100), sess.kv4_read(near, c.bt, i32([0, 0]), n, 100)):
+        assert torch.equal(a, b)
+    q = torch.randn(2, 1, 32, 128, device=DEV).to(torch.bfloat16)
+    assert torch.equal(sess.kv4_attention(0, kv4, far, q, n - 1), sess.kv4_attention(0, near, c.bt, q, n - 1))
+    sess.close()
+
+
+def test_calls_stay_within_their_workspace():
+    sess = session(2, 4, 64)
+    c = Cache(sess, [3000, 20])
+    kv4, q, lens = c.mirror(sess), torch.randn(2, 7, 8, 64, device=DEV).to(torch.bfloat16), i32([2993, 13])
+    need = B.llm42_kv4_attention_workspace_bytes(sess.model, 2, 7, 3008)
+    assert need > 2 * 7 * 8 * 64 * 4                             # (in parts)
+    ws, out = torch.full((need + 4096,), 77, dtype=torch.uint8, device=DEV), torch.zeros_like(q)
+    B.llm42_kv4_attention(sess.model, 0, kv4, kv4.shape[1], c.bt, q, lens, None, 3008, out, ws[:need])
+    assert bool((ws[need:] == 77).all()) and torch.equal(out, sess.kv4_attention(0, kv4, c.bt, q, lens, max_context=3008))
+    for num in (1, 2):
+        need = B.llm42_decode_step_mx4_workspace_bytes(sess.mx4, num, 3008)
+        ws, nxt = torch.full((need + 4096,), 77, dtype=torch.uint8, device=DEV), i32([0] * num)
+        for cache in (None, kv4):
+            B.llm42_decode_step_mx4(sess.model, sess.mx4, c.kv, c.kv.shape[2], c.bt[:num].contiguous(), cache, kv4.shape[1], c.bt[:num].contiguous(),
+                                    lens[:num].contiguous(), i32([3] * num), 3008, nxt, ws[:need])
+            assert bool((ws[need:] == 77).all())
+    sess.close()
+
+
+def test_two_graphs_of_one_session_and_a_workspace_that_is_outgrown():
+    sess = session(2, 4, 128)
+    c = Cache(sess, [900, 40])
+    kv4, q = c.mirror(sess), torch.randn(2, 4, 8, 128, device=DEV).to(torch.bfloat16)
+    lens = i32([800, 30])
+    want = [sess.kv4_attention(0, kv4, c.bt, q[:, :w].contiguous(), lens) for w in (1, 4)]
+    sess._ws = None                                              # (the first capture makes it)
+    graphs, outs, inputs = [], [], []
+    for w in (1, 4):
+        graphs.append(torch.cuda.CUDAGraph())
+        inputs.append(q[:, :w].contiguous())
+        outs.append(torch.zeros_like(inputs[-1]))
+        with torch.cuda.graph(graphs[-1]):
+            sess.kv4_attention(0, kv4, c.bt, inputs[-1], lens, out=outs[-1])
+    sess.kv4_attention(0, kv4, c.bt, q.repeat(1, 60, 1, 1), i32([600, 20]), i32([240, 10]))
+    others = [torch.full((1 << 22,), float(i), device=DEV) for i in range(8)]
+    for i in (0, 1, 1, 0, 1, 0):
+        outs[i].fill_(2.0)
+        graphs[i].replay()
+        torch.cuda.synchronize()
+        assert torch.equal(outs[i], want[i])
+    assert all(bool((t == float(i)).all()) for i, t in enumerate(others))
+    with pytest.raises(RuntimeError):                            # the model's 4-bit copy cannot be made inside a capture
+        with torch.cuda.graph(torch.cuda.CUDAGraph()):
+            sess.decode_mx4(c.kv, c.bt, lens, i32([1, 1]))
+    del graphs
+    torch.cuda.synchronize()
     sess.close()
 
 
@@ -406,3 +572,12 @@ def test_the_loop_releases_the_verifiers_stream_whatever_the_fast_path_proposes(
     assert torch.equal(got, want)
     assert stats.fast_tokens == stats.iterations * 5 * 7
     sess.close()
+
+
+@pytest.mark.parametrize("fast", ["mx4", "mx4_cache"])
+def test_the_statistics_command_runs_on_either_fast_path(fast, monkeypatch, capsys):
+    monkeypatch.setattr(wl, "LLAMA_8B", wl.TINY)
+    monkeypatch.setattr("sys.argv", ["dvr_stats", "--layers", "1", "--groups", "1,3", "--windows", "4", "--new", "6", "--prompt", "5,20", "--fast", fast])
+    dvr_stats.main()                                             # (ends the process where a stream depended on its group)
+    line = json.loads(capsys.readouterr().out.splitlines()[-1])
+    assert line["fast"] == fast and line["all_streams_equal"] and len(line["rows"]) == 2

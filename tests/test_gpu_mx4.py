@@ -202,6 +202,45 @@ def test_replays_and_streams_give_the_same_bits(rows):
         assert bool(((out - want * scale).abs() <= abs(scale) * 512 * 2.0 ** -23 * product_magnitude).all())
 
 
+def test_a_matrix_of_more_than_4_gib():
+    """Its last rows and their offsets beyond 32 bits, in values, product and codes."""
+    n, k = (1 << 21) + 40, 4096
+    src = torch.empty(n, k, dtype=torch.bfloat16, device=DEV)
+    src[:48], src[-48:] = values(48, k, torch.bfloat16, 1, False).to(DEV), values(48, k, torch.bfloat16, 2, False).to(DEV)
+    m = Mx4Matrix.quantize(src)
+    assert m.data.numel() > 2 ** 32
+    small = [Mx4Matrix.quantize(src[:48].contiguous()), Mx4Matrix.quantize(src[-40:].contiguous())]
+    assert torch.equal(m.data[:small[0].data.numel()], small[0].data) and torch.equal(m.data[-small[1].data.numel():], small[1].data)
+    m.values(out=src)
+    same(src[-40:].cpu(), small[1].values().cpu())
+    for rows in (3, 24, 70):
+        x = values(rows, k, torch.bfloat16, 3, False).to(DEV)
+        got = m.matmul(x, torch.float32)
+        for a, part in ((got[:, :48], small[0]), (got[:, -40:], small[1])):
+            want, tol = product_tolerance(x, part.values(torch.float32), torch.float32)
+            assert bool(((a.double() - want).abs() <= tol).all())
+
+
+def test_product_of_rows_far_apart():
+    """More than 2^26 elements: packed first, which needs the workspace."""
+    far = (1 << 26) + 8
+    x = torch.zeros(far + 64, dtype=torch.bfloat16, device=DEV).as_strided((2, 64), (far, 1))
+    x.copy_(values(2, 64, torch.bfloat16, 1, False))
+    m = Mx4Matrix.quantize(values(20, 64, torch.bfloat16, 2, False).to(DEV))
+    assert torch.equal(m.matmul(x, torch.float32), m.matmul(x.contiguous(), torch.float32))
+    with pytest.raises(B.Llm42Error) as e:
+        B.llm42_mx4_matmul(m.data, x, torch.zeros(2, 20, device=DEV))
+    assert e.value.status == B.LLM42_EWORKSPACE
+
+
+@pytest.mark.parametrize("rows,n,k", [(24, 100, 4096), (24, 100, 4100), (9, 40, 8200), (3, 50, 75)])
+def test_product_stays_within_its_workspace(rows, n, k):
+    x, w = values(rows, k, torch.bfloat16, 1, False).to(DEV), values(n, k, torch.bfloat16, 2, False).to(DEV)
+    m, need = Mx4Matrix.quantize(w), B.llm42_mx4_matmul_workspace_bytes(rows, n, k)
+    ws = torch.full((need + 4096,), 77, dtype=torch.uint8, device=DEV)
+    assert torch.equal(m.matmul(x, torch.float32, workspace=ws[:need]), m.matmul(x, torch.float32)) and bool((ws[need:] == 77).all())
+
+
 def test_the_binding_refuses():
     w = torch.zeros(32, 64, dtype=torch.bfloat16, device=DEV)
     m = Mx4Matrix.quantize(w)

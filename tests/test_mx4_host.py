@@ -23,10 +23,11 @@ def test_sizes_and_null_arguments_are_checked_without_a_gpu():
     lib, out = B.load_library(), SZ()
     assert lib.llm42_mx4_bytes(688, 256, ctypes.byref(out)) == B.LLM42_OK and out.value == 43 * 2176
     assert lib.llm42_mx4_bytes(1, 257, ctypes.byref(out)) == B.LLM42_OK and out.value == 2 * 2176
-    for rows, cols in ((0, 4), (4, 0), (-1, 4)):
+    for rows, cols in ((0, 4), (4, 0), (-1, 4), (2 ** 30 + 1, 4), (4, 2 ** 26 + 1), (2 ** 31 - 1, 2 ** 31 - 1)):
         assert lib.llm42_mx4_bytes(rows, cols, ctypes.byref(out)) == B.LLM42_EINVAL
     assert lib.llm42_mx4_matmul_workspace_bytes(17, 5, 33, ctypes.byref(out)) == B.LLM42_OK and out.value == 32 * 64 * 2
     assert lib.llm42_mx4_matmul_workspace_bytes(B.LLM42_MAX_ROWS + 1, 5, 33, ctypes.byref(out)) == B.LLM42_EINVAL
+    assert lib.llm42_mx4_matmul_workspace_bytes(17, 5, 2 ** 26 + 1, ctypes.byref(out)) == B.LLM42_EINVAL
     assert lib.llm42_kv4_bytes(None, 4, ctypes.byref(out)) == B.LLM42_EINVAL
     assert lib.llm42_kv4_attention_workspace_bytes(None, 1, 1, 64, ctypes.byref(out)) == B.LLM42_EINVAL
     assert lib.llm42_decode_step_mx4_workspace_bytes(None, 1, 64, ctypes.byref(out)) == B.LLM42_EINVAL
@@ -41,6 +42,7 @@ QUANTIZE = dict(src=4096, type=B.LLM42_BF16, stride=64, rows=16, cols=64, dst=40
     (dict(src=None), B.LLM42_EINVAL), (dict(dst=None), B.LLM42_EINVAL), (dict(rows=0), B.LLM42_EINVAL), (dict(cols=-3), B.LLM42_EINVAL),
     (dict(type=7), B.LLM42_EINVAL), (dict(stride=63), B.LLM42_EINVAL), (dict(src=4097), B.LLM42_EINVAL),
     (dict(src=4098, type=B.LLM42_F32), B.LLM42_EINVAL), (dict(dst=4104), B.LLM42_EINVAL), (dict(dst_bytes=2175), B.LLM42_EWORKSPACE),
+    (dict(rows=2 ** 30 + 1), B.LLM42_EINVAL), (dict(cols=2 ** 26 + 1, stride=2 ** 27), B.LLM42_EINVAL),
     (dict(rows=2 ** 31 - 1, cols=2 ** 31 - 1, stride=2 ** 31, dst_bytes=2 ** 63), B.LLM42_EINVAL)])
 def test_quantize_and_dequantize_refuse(bad, code):
     lib, a = B.load_library(), {**QUANTIZE, **bad}
@@ -53,7 +55,7 @@ MATMUL = dict(w=4096, w_bytes=1 << 20, n=16, k=64, x=4096, xs=64, rows=3, out=40
     (dict(w=None), B.LLM42_EINVAL), (dict(x=None), B.LLM42_EINVAL), (dict(out=None), B.LLM42_EINVAL), (dict(n=0), B.LLM42_EINVAL),
     (dict(k=0), B.LLM42_EINVAL), (dict(rows=0), B.LLM42_EINVAL), (dict(rows=B.LLM42_MAX_ROWS + 1), B.LLM42_EINVAL),
     (dict(xs=63), B.LLM42_EINVAL), (dict(os=15), B.LLM42_EINVAL), (dict(type=2), B.LLM42_EINVAL), (dict(x=4097), B.LLM42_EINVAL),
-    (dict(w_bytes=2175), B.LLM42_EWORKSPACE),
+    (dict(w_bytes=2175), B.LLM42_EWORKSPACE), (dict(k=2 ** 26 + 1, xs=2 ** 27, w_bytes=2 ** 62), B.LLM42_EINVAL),
     # rows that are not 16-byte aligned, or k not a multiple of 32, need the workspace
     (dict(x=4098), B.LLM42_EWORKSPACE), (dict(xs=65), B.LLM42_EWORKSPACE), (dict(k=63), B.LLM42_EWORKSPACE),
     (dict(k=63, ws=4096, ws_bytes=2 * 16 * 64 - 1), B.LLM42_EWORKSPACE), (dict(k=63, ws=4160, ws_bytes=1 << 20), B.LLM42_EWORKSPACE)])
