@@ -68,8 +68,8 @@ llm42_status llm42_mx4_dequantize(
 /* out[i][j] = sum over c of x[i][c] * w[j][c], w an n x k matrix in MXFP4, x bf16: the products are exact (a 4-bit value is
  * a bf16), summed in fp32 in an order that depends on the sizes; out is rounded once.  x[i] at x + i * x_stride elements and
  * out[i] at out + i * out_stride; what lies between the rows of out is left as it was.  out must not overlap x or w.
- * workspace: llm42_mx4_matmul_workspace_bytes(rows, n, k) bytes, 256-byte aligned.  x whose rows are not 16-byte aligned, are more than
- * 2^26 elements apart or whose k is not a multiple of 32 need it (LLM42_EWORKSPACE).  Otherwise the call does with less, or NULL,
+ * workspace: llm42_mx4_matmul_workspace_bytes(rows, n, k) bytes, 256-byte aligned.  Rows that are not 4-byte aligned need it, and so do
+ * more than 16 that are not 16-byte aligned, are more than 2^26 elements apart or whose k is not a multiple of 32 (LLM42_EWORKSPACE).  Otherwise the call does with less, or NULL,
  * but then sums over k in one piece, which takes longer where rows and n are few (and gives other low bits). */
 llm42_status llm42_mx4_matmul_workspace_bytes(int32_t rows, int32_t n, int32_t k, size_t* out_bytes);
 llm42_status llm42_mx4_matmul(

@@ -36,12 +36,14 @@ __global__ __launch_bounds__(256) void kv4_store_kernel(const uint16_t* __restri
   const int s = at_slot / slots, slot = at_slot % slots, layer = blockIdx.y;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, h = (int)(blockIdx.x % hg) * 4 + wave;
   const int64_t first = first_[s], count = count_[s];
+  const int block = (int)(first / LLM42_KV_BLOCK) + slot;
+  // (asked for together with what the check reads)
+  const int sb_ = src.ids[(size_t)s * src.width + min(max(block, 0), src.width - 1)], db_ = dst.ids[(size_t)s * dst.width + min(max(block, 0), dst.width - 1)];
   const int status = range_status(first, count, max_count, src, dst, s, lane);
   if (seq_status && blockIdx.y == 0 && slot == 0 && h == 0 && lane == 0) seq_status[s] = status;
-  const int block = (int)(first / LLM42_KV_BLOCK) + slot;
   if (status != LLM42_SEQ_OK || (int64_t)block * LLM42_KV_BLOCK >= first + count || h >= n_kv_heads) return;
   const int lo = (int)max(first - (int64_t)block * 16, (int64_t)0), hi = (int)min(first + count - (int64_t)block * 16, (int64_t)16);
-  const size_t sb = src.ids[(size_t)s * src.width + block], db = dst.ids[(size_t)s * dst.width + block];
+  const size_t sb = sb_, db = db_;
   const size_t plane = (size_t)src.num_blocks * n_kv_heads * 16 * HD;
   const uint16_t* kt = kv + (size_t)layer * 2 * plane + (sb * n_kv_heads + h) * 16 * HD;
   char* rec = kv4 + (((size_t)layer * dst.num_blocks + db) * n_kv_heads + h) * kv_record(HD);

@@ -28,6 +28,24 @@ __device__ __forceinline__ void store_positions(const uint16_t* __restrict__ kt,
 #pragma unroll
     for (int j = 0; j < KT; ++j) vw[j] = *(const u32x4*)(vt + v_tile_off(32 * j + 2 * l16, 4 * g));
   }
+  // tokens of this lane that are in range: a byte of each word of V's codes and scales.  Other positions may share the word (this wave alone
+  // writes it): what it holds is asked for with the values.
+  uint32_t take = 0;
+#pragma unroll
+  for (int t = 0; t < 4; ++t)
+    if (4 * g + t >= lo && 4 * g + t < hi) take |= 0xFFu << (8 * t);
+  uint32_t* p = (uint32_t*)(rec + 8 * HD + lane * KT * 4);
+  uint32_t* q = (uint32_t*)(rec + 16 * HD + HD / 2 + g * KT * 4);
+  uint32_t old_c[KT], old_s[KT];
+#pragma unroll
+  for (int j = 0; j < KT; ++j) old_c[j] = old_s[j] = 0;
+  if (take && take != 0xFFFFFFFFu) {
+#pragma unroll
+    for (int j = 0; j < KT; ++j) {
+      old_c[j] = p[j];
+      old_s[j] = q[j];
+    }
+  }
   // K: lane (g, token) has features 32 j + 8 g .. + 7
   uint32_t kc[KT], ks = 0;
 #pragma unroll
@@ -66,20 +84,12 @@ __device__ __forceinline__ void store_positions(const uint16_t* __restrict__ kt,
       if (byte == 255u) vc[j] &= ~(255u << (8 * t));
     }
   }
-  // tokens of this lane that are in range: a byte of each word of codes and of scales
-  uint32_t take = 0;
-#pragma unroll
-  for (int t = 0; t < 4; ++t)
-    if (4 * g + t >= lo && 4 * g + t < hi) take |= 0xFFu << (8 * t);
   if (take) {
-    uint32_t* p = (uint32_t*)(rec + 8 * HD + lane * KT * 4);
-    uint32_t* q = (uint32_t*)(rec + 16 * HD + HD / 2 + g * KT * 4);
-    const bool part = take != 0xFFFFFFFFu;         // (other positions share the word: this wave alone writes it)
 #pragma unroll
-    for (int j = 0; j < KT; ++j) p[j] = part ? (p[j] & ~take) | (vc[j] & take) : vc[j];
+    for (int j = 0; j < KT; ++j) p[j] = (old_c[j] & ~take) | (vc[j] & take);
     if (l16 == 0) {
 #pragma unroll
-      for (int j = 0; j < KT; ++j) q[j] = part ? (q[j] & ~take) | (vs[j] & take) : vs[j];
+      for (int j = 0; j < KT; ++j) q[j] = (old_s[j] & ~take) | (vs[j] & take);
     }
   }
 }

@@ -140,15 +140,16 @@ llm42_status llm42_mx4_matmul(const void* w, size_t w_bytes, int32_t n, int32_t 
   if ((uintptr_t)x % 2) return fail(LLM42_EINVAL, "%s: x not aligned to its type", who);
   hipStream_t st = (hipStream_t)hip_stream;
   const size_t packed = packed_x_bytes(rows, k), need = packed + mx4_matmul_part_bytes(n, k, rows, num_cus());
-  const bool pack = k % 32 || (uintptr_t)x % 16 || (rows > 1 && (x_stride % 8 || x_stride > (1 << 26)));
+  const bool plain = k % 32 == 0 && (uintptr_t)x % 16 == 0 && (rows == 1 || (x_stride % 8 == 0 && x_stride <= (1 << 26)));
+  const bool loose = !plain && rows <= mx4_loose_rows() && (uintptr_t)x % 4 == 0 && (rows == 1 || x_stride % 2 == 0), pack = !plain && !loose;
   const bool room = workspace && (uintptr_t)workspace % 256 == 0 && workspace_bytes >= need;
   if (pack && !room) {
     if (!workspace || (uintptr_t)workspace % 256) return fail(LLM42_EWORKSPACE, "%s: this x needs a workspace, 256-byte aligned", who);
     return fail(LLM42_EWORKSPACE, "%s: workspace %zu < %zu bytes", who, workspace_bytes, need);
   }
   if (pack) launch_mx4_pack_x((const uint16_t*)x, x_stride, rows, k, (uint16_t*)workspace, st);
-  launch_mx4_matmul(w, n, k, (const uint16_t*)(pack ? workspace : x), pack ? 0 : x_stride, rows, out, out_type, out_stride, num_cus(),
-                    room && need > packed ? (float*)((char*)workspace + packed) : nullptr, st);
+  launch_mx4_matmul(w, n, k, (const uint16_t*)(pack ? workspace : x), pack ? 0 : x_stride, loose, rows, out, out_type, out_stride,
+                    num_cus(), room && need > packed ? (float*)((char*)workspace + packed) : nullptr, st);
   return launched(who);
 }
 

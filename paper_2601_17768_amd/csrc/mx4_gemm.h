@@ -17,6 +17,7 @@ struct X {
   const uint16_t* p;
   int64_t stride;           // 0: tiles
   int k_tiles, last_row;
+  int tail = 0;             // mx4_stream_kernel of loose rows: columns behind the k-tiles (which are the whole ones then)
   // what lane `lane` of token block `block` takes of k-tile 0, and from a k-tile to the next; rows that only pad repeat the last one
   __device__ const uint16_t* at(int block, int lane) const {
     const int row = min(block * 16 + (lane & 15), last_row);
@@ -37,9 +38,13 @@ struct X {
 
 // Up to 16 rows.  A workgroup owns FB feature blocks; its eight waves take the groups of 4 k-tiles in turn, each with
 // accumulators of its own for all of them, and are added through LDS.  Codes and activations of D groups are on their way at
-// a time; no barrier, for no two waves want the same bytes.
-constexpr int kStreamWaves = 8;
-template <int FB, int D, class Epi>
+// a time; no barrier, for no two waves want the same bytes.  LOOSE: plain
+// rows of any number of columns that are only 4-byte aligned are read as they lie (behind a launch that brings them in order first 13
+// rows of 1000 x 700 took 7.8 us instead of 4.6, 16 of 4096 x 4100 11.6 instead of 8.9); the last wave takes the columns behind
+// the last whole k-tile.  (Rows that begin in the middle of a word are brought in order: 16 rows of 4096 x 4097 took 28 us by loads of
+// 16 bytes, 13.4 by aligned words and shifts, 11.7 so.)
+constexpr int kStreamWaves = 8, kStreamRows = 16;
+template <int FB, int D, bool LOOSE, class Epi>
 __global__ __launch_bounds__(64 * kStreamWaves) void mx4_stream_kernel(const char* __restrict__ w, X x, int n_blocks, int units, Epi epi) {
   constexpr int NW = kStreamWaves;
   __shared__ f32x4 part[NW][FB * 64];
@@ -66,7 +71,11 @@ __global__ __launch_bounds__(64 * kStreamWaves) void mx4_stream_kernel(const cha
       scales[U][f] = *(const uint32_t*)(rec + kScales + (g & 1) * 4 + (lane & 15) * 8);
     }
 #pragma unroll
-    for (int j = 0; j < 4; ++j) xv[U][j] = *(const bf16x8*)(xp + (size_t)min(g * 4 + j, x.k_tiles - 1) * xs);
+    for (int j = 0; j < 4; ++j) {
+      typedef bf16x8 words __attribute__((aligned(4)));
+      const uint16_t* from = xp + (size_t)min(g * 4 + j, x.k_tiles - 1) * xs;
+      xv[U][j] = LOOSE ? (bf16x8)*(const words*)from : *(const bf16x8*)from;
+    }
   };
   auto compute = [&](auto set, int i) __attribute__((always_inline)) {
     constexpr int U = decltype(set)::value;
@@ -96,6 +105,20 @@ __global__ __launch_bounds__(64 * kStreamWaves) void mx4_stream_kernel(const cha
       step(Set0{}, i);
       step(Set1{}, i + 1);
       if constexpr (D == 3) step(Set2{}, i + 2);
+    }
+  }
+  if (LOOSE && x.tail && wave == NW - 1) {
+    const uint16_t* from = xp + (size_t)x.k_tiles * 32;
+    u32x4 v = {0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if ((lane >> 4) * 8 + i < x.tail) v[i >> 1] |= (uint32_t)from[i] << (16 * (i & 1));
+#pragma unroll
+    for (int f = 0; f < FB; ++f) {
+      const char* rec = wp[f] + (size_t)(x.k_tiles >> 3) * kRecord;
+      const uint32_t word = *(const uint32_t*)(rec + (x.k_tiles >> 2 & 1) * 1024 + lane * 16 + (x.k_tiles & 3) * 4);
+      const uint32_t byte = *(const uint8_t*)(rec + kScales + (lane & 15) * 8 + (x.k_tiles & 7));
+      acc[f] = mfma16(operand(word, scale_of(byte, 0)), __builtin_bit_cast(bf16x8, v), acc[f]);
     }
   }
 #pragma unroll
@@ -368,13 +391,15 @@ struct Plan {
 // read again by a launch that adds them (2.6 us and 2.8 TB/s; nothing but that where `joined`: the launch that follows adds two of them
 // anyway), and is taken for a tenth less (32 rows of 4096 x 14336 33.6 -> 17.1, 1024 x 4096 12.1 -> 8.7; 128 rows of 4096 x 14336
 // 38.4 -> 25.1).  Over those 402 shapes and row counts the choice takes 1.4 % more than the best of all there are, at worst 29 %.
+inline Plan stream_plan(int n_blocks, int k_tiles, int num_cus) {
+  const int g8 = (n_blocks + 7) / 8, g7 = (n_blocks + 6) / 7;
+  const bool seven = (g7 + num_cus - 1) / num_cus * 7 < (g8 + num_cus - 1) / num_cus * 8;
+  return {-1, n_blocks <= num_cus ? 1 : n_blocks <= 2 * num_cus ? 2 : seven ? 7 : 8, 1, (k_tiles + 3) / 4};
+}
 inline Plan plan(int n_blocks, int k_tiles, int rows, int num_cus, int most_parts, bool joined = false) {
   const int groups = (k_tiles + 3) / 4, blocks = (rows + 15) / 16;
-  if ((rows <= 8 || (rows <= 16 && n_blocks > 2 * num_cus)) && !(k_tiles <= 32 && n_blocks > 2 * num_cus)) {
-    const int g8 = (n_blocks + 7) / 8, g7 = (n_blocks + 6) / 7;
-    const bool seven = (g7 + num_cus - 1) / num_cus * 7 < (g8 + num_cus - 1) / num_cus * 8;
-    return {-1, n_blocks <= num_cus ? 1 : n_blocks <= 2 * num_cus ? 2 : seven ? 7 : 8, 1, groups};
-  }
+  if ((rows <= 8 || (rows <= kStreamRows && n_blocks > 2 * num_cus)) && !(k_tiles <= 32 && n_blocks > 2 * num_cus))
+    return stream_plan(n_blocks, k_tiles, num_cus);
   Plan best{-1, 0, 1, groups};
   double least = 0;
   for (int t = 0; t < kTileCount4; ++t)
@@ -394,6 +419,17 @@ inline Plan plan(int n_blocks, int k_tiles, int rows, int num_cus, int most_part
   return best;
 }
 
+template <bool LOOSE, class Epi>
+void launch_stream(const Plan& p, const char* w, int n_blocks, const X& x, const Epi& epi, hipStream_t st) {
+  const int units = (x.k_tiles + (x.tail > 0) + 7) / 8;
+  const unsigned grid = (n_blocks + p.fb - 1) / p.fb;
+  constexpr int threads = 64 * kStreamWaves;
+  if (p.fb == 1) mx4_stream_kernel<1, 3, LOOSE, Epi><<<grid, threads, 0, st>>>(w, x, n_blocks, units, epi);
+  else if (p.fb == 2) mx4_stream_kernel<2, 3, LOOSE, Epi><<<grid, threads, 0, st>>>(w, x, n_blocks, units, epi);
+  else if (p.fb == 7) mx4_stream_kernel<7, 2, LOOSE, Epi><<<grid, threads, 0, st>>>(w, x, n_blocks, units, epi);
+  else mx4_stream_kernel<8, 2, LOOSE, Epi><<<grid, threads, 0, st>>>(w, x, n_blocks, units, epi);
+}
+
 // Returns the number of arg-max partials per row (LM head).
 template <class Epi>
 int launch(const Plan& p, const void* w, int n_blocks, const X& x, int rows, Epi epi, hipStream_t st) {
@@ -405,15 +441,7 @@ int launch(const Plan& p, const void* w, int n_blocks, const X& x, int rows, Epi
     return partials;
   }
   if constexpr (is_logits<Epi>::value) epi.parts = n_blocks;
-  if constexpr (!std::is_same<Epi, StorePartialEpi>::value) {   // (never in parts)
-    const int units = (x.k_tiles + 7) / 8;
-    const unsigned grid = (n_blocks + p.fb - 1) / p.fb;
-    constexpr int threads = 64 * kStreamWaves;
-    if (p.fb == 1) mx4_stream_kernel<1, 3, Epi><<<grid, threads, 0, st>>>(wp, x, n_blocks, units, epi);
-    else if (p.fb == 2) mx4_stream_kernel<2, 3, Epi><<<grid, threads, 0, st>>>(wp, x, n_blocks, units, epi);
-    else if (p.fb == 7) mx4_stream_kernel<7, 2, Epi><<<grid, threads, 0, st>>>(wp, x, n_blocks, units, epi);
-    else mx4_stream_kernel<8, 2, Epi><<<grid, threads, 0, st>>>(wp, x, n_blocks, units, epi);
-  }
+  if constexpr (!std::is_same<Epi, StorePartialEpi>::value) launch_stream<false>(p, wp, n_blocks, x, epi, st);   // (never in parts)
   return n_blocks;
 }
 

@@ -44,8 +44,12 @@ __global__ __launch_bounds__(256) void mx4_join_kernel(const float* __restrict__
 }
 
 template <bool F32>
-void matmul(const void* w, int n, const mx4::X& x, int rows, const PlainEpi<F32>& epi, const mx4::Plan& p, float* parts, hipStream_t st) {
+void matmul(const void* w, int n, const mx4::X& x, int rows, const PlainEpi<F32>& epi, const mx4::Plan& p, bool loose, float* parts, hipStream_t st) {
   const int n_blocks = (n + 15) / 16;
+  if (loose) {
+    mx4::launch_stream<true>(p, (const char*)w, n_blocks, x, epi, st);
+    return;
+  }
   if (p.parts == 1) {
     mx4::launch(p, w, n_blocks, x, rows, epi, st);
     return;
@@ -66,12 +70,15 @@ size_t mx4_matmul_part_bytes(int n, int k, int rows, int num_cus) {
   return p.parts > 1 ? 4ull * p.parts * ((rows + 15) / 16 * 16) * ((n + 15) / 16 * 16) : 0;
 }
 
-void launch_mx4_matmul(const void* w, int n, int k, const uint16_t* x, int64_t x_stride, int rows, void* out, int out_type,
+int mx4_loose_rows() { return mx4::kStreamRows; }
+
+void launch_mx4_matmul(const void* w, int n, int k, const uint16_t* x, int64_t x_stride, bool loose, int rows, void* out, int out_type,
                        int64_t out_stride, int num_cus, float* parts, hipStream_t st) {
-  const mx4::X xs{x, x_stride, (k + 31) / 32, rows - 1};
-  const mx4::Plan p = mx4::plan((n + 15) / 16, xs.k_tiles, rows, num_cus, parts ? kMostParts : 1);
+  const mx4::X xs = loose ? mx4::X{x, x_stride, k / 32, rows - 1, k % 32} : mx4::X{x, x_stride, (k + 31) / 32, rows - 1};
+  const int n_blocks = (n + 15) / 16;
+  const mx4::Plan p = loose ? mx4::stream_plan(n_blocks, xs.k_tiles, num_cus) : mx4::plan(n_blocks, xs.k_tiles, rows, num_cus, parts ? kMostParts : 1);
   if (out_type == LLM42_F32)
-    matmul(w, n, xs, rows, PlainEpi<true>{out, out_stride, rows, n, (uintptr_t)out % 16 == 0 && out_stride % 4 == 0}, p, parts, st);
+    matmul(w, n, xs, rows, PlainEpi<true>{out, out_stride, rows, n, (uintptr_t)out % 16 == 0 && out_stride % 4 == 0}, p, loose, parts, st);
   else
-    matmul(w, n, xs, rows, PlainEpi<false>{out, out_stride, rows, n, (uintptr_t)out % 8 == 0 && out_stride % 4 == 0}, p, parts, st);
+    matmul(w, n, xs, rows, PlainEpi<false>{out, out_stride, rows, n, (uintptr_t)out % 8 == 0 && out_stride % 4 == 0}, p, loose, parts, st);
 }

@@ -42,7 +42,7 @@ class Mx4Matrix:
             out = torch.empty((x.shape[0], self.rows), dtype=dtype, device=self.data.device)
         if tuple(out.shape) != (x.shape[0], self.rows):
             raise ValueError(f"out must be [{x.shape[0]}, {self.rows}]")
-        if workspace is None and (x.shape[0] > 8 or self.cols % 32 or x.data_ptr() % 16 or x.stride(0) % 8 or x.stride(0) > 1 << 26):
+        if workspace is None and (x.shape[0] > 8 or x.data_ptr() % 4 or x.stride(0) % 2):
             workspace = torch.empty(B.llm42_mx4_matmul_workspace_bytes(x.shape[0], self.rows, self.cols), dtype=torch.uint8, device=x.device)
         B.llm42_mx4_matmul(self.data, x, out, workspace)
         return out

@@ -112,7 +112,9 @@ TILES = [(130, 33000, 260), (130, 33000, 288), (70, 33000, 260), (70, 33000, 288
          (35, 4112, 8200), (35, 4112, 8192), (35, 16400, 260), (45, 16400, 288), (130, 1000, 8200), (130, 1000, 8192), (35, 8200, 545),
          (35, 8200, 544), (130, 500, 8200), (130, 500, 8192), (9, 16400, 260), (20, 16400, 288), (70, 1000, 8200), (70, 1000, 8192),
          (20, 8200, 8192), (9, 4112, 4100), (9, 4112, 4096), (9, 40, 8200), (20, 40, 8192), (9, 40, 4100), (20, 40, 4096), (1, 40, 8200),
-         (5, 5000, 1090), (8, 5000, 1088), (9, 8200, 1090), (16, 8200, 1088), (3, 9000, 2050), (8, 33000, 1024 + 64)]
+         (5, 5000, 1090), (16, 20, 31), (1, 3, 1), (12, 40, 4100), (16, 33000, 287), (16, 33000, 4095), (7, 60, 257), (2, 8200, 223),
+         (8, 5000, 1088), (9, 8200, 1090), (16, 8200, 1088), (3, 9000, 2050), (8, 33000, 1024 + 64), (20, 33000, 260), (20, 4112, 4100),
+         (20, 40, 8200), (20, 40, 4100), (20, 16400, 260), (24, 33000, 33)]
 
 
 @pytest.mark.parametrize("rows,n,k", TILES)
@@ -222,14 +224,16 @@ def test_a_matrix_of_more_than_4_gib():
 
 
 def test_product_of_rows_far_apart():
-    """More than 2^26 elements: packed first, which needs the workspace."""
+    """More than 2^26 elements: beyond 16 rows packed first, which needs the workspace."""
     far = (1 << 26) + 8
-    x = torch.zeros(far + 64, dtype=torch.bfloat16, device=DEV).as_strided((2, 64), (far, 1))
-    x.copy_(values(2, 64, torch.bfloat16, 1, False))
+    x = torch.zeros(16 * far + 64, dtype=torch.bfloat16, device=DEV).as_strided((17, 64), (far, 1))
+    x.copy_(values(17, 64, torch.bfloat16, 1, False))
     m = Mx4Matrix.quantize(values(20, 64, torch.bfloat16, 2, False).to(DEV))
-    assert torch.equal(m.matmul(x, torch.float32), m.matmul(x.contiguous(), torch.float32))
+    for rows in (2, 16, 17):
+        want, tol = product_tolerance(x[:rows].contiguous(), m.values(torch.float32), torch.float32)
+        assert bool(((m.matmul(x[:rows], torch.float32).double() - want).abs() <= tol).all())
     with pytest.raises(B.Llm42Error) as e:
-        B.llm42_mx4_matmul(m.data, x, torch.zeros(2, 20, device=DEV))
+        B.llm42_mx4_matmul(m.data, x, torch.zeros(17, 20, device=DEV))
     assert e.value.status == B.LLM42_EWORKSPACE
 
 

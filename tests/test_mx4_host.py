@@ -56,9 +56,10 @@ MATMUL = dict(w=4096, w_bytes=1 << 20, n=16, k=64, x=4096, xs=64, rows=3, out=40
     (dict(k=0), B.LLM42_EINVAL), (dict(rows=0), B.LLM42_EINVAL), (dict(rows=B.LLM42_MAX_ROWS + 1), B.LLM42_EINVAL),
     (dict(xs=63), B.LLM42_EINVAL), (dict(os=15), B.LLM42_EINVAL), (dict(type=2), B.LLM42_EINVAL), (dict(x=4097), B.LLM42_EINVAL),
     (dict(w_bytes=2175), B.LLM42_EWORKSPACE), (dict(k=2 ** 26 + 1, xs=2 ** 27, w_bytes=2 ** 62), B.LLM42_EINVAL),
-    # rows that are not 16-byte aligned, or k not a multiple of 32, need the workspace
-    (dict(x=4098), B.LLM42_EWORKSPACE), (dict(xs=65), B.LLM42_EWORKSPACE), (dict(k=63), B.LLM42_EWORKSPACE),
-    (dict(k=63, ws=4096, ws_bytes=2 * 16 * 64 - 1), B.LLM42_EWORKSPACE), (dict(k=63, ws=4160, ws_bytes=1 << 20), B.LLM42_EWORKSPACE)])
+    # rows that are not 4-byte aligned, and more than 16 that are not 16-byte aligned or whose k is not a multiple of 32, need the workspace
+    (dict(x=4098), B.LLM42_EWORKSPACE), (dict(xs=65), B.LLM42_EWORKSPACE), (dict(rows=17, x=4100), B.LLM42_EWORKSPACE), (dict(rows=17, xs=66), B.LLM42_EWORKSPACE), (dict(rows=17, k=63), B.LLM42_EWORKSPACE),
+    (dict(rows=17, k=63, ws=4096, ws_bytes=2 * 32 * 64 - 1), B.LLM42_EWORKSPACE),
+    (dict(rows=17, k=63, ws=4160, ws_bytes=1 << 20), B.LLM42_EWORKSPACE)])
 def test_matmul_refuses(bad, code):
     assert B.load_library().llm42_mx4_matmul(*{**MATMUL, **bad}.values()) == code
 
