@@ -37,14 +37,15 @@ struct X {
 };
 
 // Up to 16 rows.  A workgroup owns FB feature blocks; its eight waves take the groups of 4 k-tiles in turn, each with
-// accumulators of its own for all of them, and are added through LDS.  Codes and activations of D groups are on their way at
-// a time; no barrier, for no two waves want the same bytes.  LOOSE: plain
+// accumulators of its own for all of them, and are added through LDS.  Codes and activations of two groups are on their way at
+// a time; no barrier, for no two waves want the same bytes.  A wave has four groups of a 4096-column matrix, so nothing is loaded past the
+// last one (1 row of 6144 x 4096 so 6.2 -> 4.6 us, from memory 7.7 -> 5.8; 28672 x 4096 15.1 -> 13.9, 4.5 TB/s).  LOOSE: plain
 // rows of any number of columns that are only 4-byte aligned are read as they lie (behind a launch that brings them in order first 13
 // rows of 1000 x 700 took 7.8 us instead of 4.6, 16 of 4096 x 4100 11.6 instead of 8.9); the last wave takes the columns behind
 // the last whole k-tile.  (Rows that begin in the middle of a word are brought in order: 16 rows of 4096 x 4097 took 28 us by loads of
 // 16 bytes, 13.4 by aligned words and shifts, 11.7 so.)
 constexpr int kStreamWaves = 8, kStreamRows = 16;
-template <int FB, int D, bool LOOSE, class Epi>
+template <int FB, bool LOOSE, class Epi>
 __global__ __launch_bounds__(64 * kStreamWaves) void mx4_stream_kernel(const char* __restrict__ w, X x, int n_blocks, int units, Epi epi) {
   constexpr int NW = kStreamWaves;
   __shared__ f32x4 part[NW][FB * 64];
@@ -58,12 +59,12 @@ __global__ __launch_bounds__(64 * kStreamWaves) void mx4_stream_kernel(const cha
   f32x4 acc[FB];
 #pragma unroll
   for (int i = 0; i < FB; ++i) acc[i] = (f32x4){0.f, 0.f, 0.f, 0.f};
-  u32x4 codes[D][FB];
-  uint32_t scales[D][FB];
-  bf16x8 xv[D][4];
-  auto load = [&](auto set, int i) __attribute__((always_inline)) {       // (past the last one: that one again)
+  u32x4 codes[2][FB];
+  uint32_t scales[2][FB];
+  bf16x8 xv[2][4];
+  auto load = [&](auto set, int i) __attribute__((always_inline)) {
     constexpr int U = decltype(set)::value;
-    const int g = min(i, mine - 1) * NW + wave;
+    const int g = i * NW + wave;
 #pragma unroll
     for (int f = 0; f < FB; ++f) {
       const char* rec = wp[f] + (size_t)(g >> 1) * kRecord;
@@ -89,23 +90,26 @@ __global__ __launch_bounds__(64 * kStreamWaves) void mx4_stream_kernel(const cha
   };
   using Set0 = std::integral_constant<int, 0>;
   using Set1 = std::integral_constant<int, 1>;
-  using Set2 = std::integral_constant<int, D == 2 ? 0 : 2>;
-  static_assert(D == 2 || D == 3, "the rounds are written out for 2 and 3 register sets");
-  if (mine > 0) {
+  if (mine >= 2) {
     load(Set0{}, 0);
     load(Set1{}, 1);
-    if constexpr (D == 3) load(Set2{}, 2);
-    for (int i = 0; i < mine; i += D) {
-      const auto step = [&](auto set, int at) __attribute__((always_inline)) {
-        __builtin_amdgcn_sched_barrier(0);
-        if (at < mine) compute(set, at);
-        __builtin_amdgcn_sched_barrier(0);
-        load(set, at + D);
-      };
-      step(Set0{}, i);
-      step(Set1{}, i + 1);
-      if constexpr (D == 3) step(Set2{}, i + 2);
+    int i = 0;
+    const auto step = [&](auto set, int at, bool more) __attribute__((always_inline)) {
+      __builtin_amdgcn_sched_barrier(0);
+      compute(set, at);
+      __builtin_amdgcn_sched_barrier(0);
+      if (more) load(set, at + 2);
+    };
+    for (; i + 4 <= mine; i += 2) {                  // (a branch around the loads would have them waited for too early)
+      step(Set0{}, i, true);
+      step(Set1{}, i + 1, true);
     }
+    step(Set0{}, i, i + 2 < mine);
+    step(Set1{}, i + 1, false);
+    if (i + 2 < mine) compute(Set0{}, i + 2);
+  } else if (mine == 1) {
+    load(Set0{}, 0);
+    compute(Set0{}, 0);
   }
   if (LOOSE && x.tail && wave == NW - 1) {
     const uint16_t* from = xp + (size_t)x.k_tiles * 32;
@@ -384,24 +388,26 @@ struct Plan {
   int fb;                  // ... by this many feature blocks
   int parts, part_groups;  // of the sum over k, and how many groups of 4 k-tiles each has
 };
-// mx4_stream_kernel for up to 8 rows, and up to 16 where there are more than two feature blocks per CU (us, it / the best tile: 1 row of
-// 4096 x 4096 6.2 / 8.6, 1 of 28672 x 4096 15 / 21, 8 of 4096 x 14336 14.4 / 16.7, 16 of 28672 x 4096 16.3 / 20.6; but 16 of 4096 x 4096
-// 10.2 / 9.1, 16 of 1024 x 1024 6.8 / 5.2) - unless many features have few columns, when its waves have a step or two each (8 rows of
-// 50304 x 1024 15.6 / 11.3).  Else the tile and the number of parts that cost least; a part has a plane of fp32 sums of its own, written and
+// mx4_stream_kernel for up to 16 rows (us, it / the best tile: 1 row of 4096 x 4096 4.8 / 9.2, 16 6.7 / 9.8; 1 of 28672 x 4096 13.1 / 19.6, 16
+// 14.6 / 19.9; 16 of 50304 x 512 7.4 / 7.9), except where more than 8 rows are summed over many columns for few features: it has but eight
+// waves for a sum, each of which takes 0.6 us and 28 ns a row for a group, a tile several workgroups (16 rows of 512 x 14336 16.1 / 10.7,
+// of 512 x 4096 6.1 / 7.7).  A workgroup per CU where eight feature blocks are enough for that, else seven or eight, whichever leave fewer
+// idle in the last round (16 rows, us by 1 / 2 / 3 / 4 / 7 / 8 of them: 8192 x 4096 11.5 / 7.6 / 8.2 / 9.0 / 11.9 / 12.9,
+// 16384 x 4096 21 / 12.5 / 14.6 / 9.7 / 12.7 / 13.7, 28672 x 4096 36 / 22 / 21 / 18 / 14.6 / 15.6, 128256 x 4096 153 / 77 / 72 / 67 / 62 / 57).
+// Else the tile and the number of parts that cost least; a part has a plane of fp32 sums of its own, written and
 // read again by a launch that adds them (2.6 us and 2.8 TB/s; nothing but that where `joined`: the launch that follows adds two of them
 // anyway), and is taken for a tenth less (32 rows of 4096 x 14336 33.6 -> 17.1, 1024 x 4096 12.1 -> 8.7; 128 rows of 4096 x 14336
 // 38.4 -> 25.1).  Over those 402 shapes and row counts the choice takes 1.4 % more than the best of all there are, at worst 29 %.
 inline Plan stream_plan(int n_blocks, int k_tiles, int num_cus) {
   const int g8 = (n_blocks + 7) / 8, g7 = (n_blocks + 6) / 7;
   const bool seven = (g7 + num_cus - 1) / num_cus * 7 < (g8 + num_cus - 1) / num_cus * 8;
-  return {-1, n_blocks <= num_cus ? 1 : n_blocks <= 2 * num_cus ? 2 : seven ? 7 : 8, 1, (k_tiles + 3) / 4};
+  return {-1, g8 <= num_cus ? (n_blocks + num_cus - 1) / num_cus : seven ? 7 : 8, 1, (k_tiles + 3) / 4};
 }
 inline Plan plan(int n_blocks, int k_tiles, int rows, int num_cus, int most_parts, bool joined = false) {
   const int groups = (k_tiles + 3) / 4, blocks = (rows + 15) / 16;
-  if ((rows <= 8 || (rows <= kStreamRows && n_blocks > 2 * num_cus)) && !(k_tiles <= 32 && n_blocks > 2 * num_cus))
-    return stream_plan(n_blocks, k_tiles, num_cus);
-  Plan best{-1, 0, 1, groups};
-  double least = 0;
+  Plan best = stream_plan(n_blocks, k_tiles, num_cus);
+  if (rows <= 8 || (rows <= kStreamRows && n_blocks > num_cus)) return best;
+  double least = rows <= kStreamRows ? 2300 + groups / 8. * (600 + 28 * rows) : 1e30;
   for (int t = 0; t < kTileCount4; ++t)
     for (int want = 1; want <= most_parts; want *= 2) {
       const int pg = (groups + want - 1) / want, parts = (groups + pg - 1) / pg;
@@ -411,7 +417,7 @@ inline Plan plan(int n_blocks, int k_tiles, int rows, int num_cus, int most_part
       const double rounds = (double)(((long long)tiles + num_cus - 1) / num_cus), full = tiles / (rounds * num_cus);
       double ns = 2100 + rounds * (q.round_ns + q.k_ns * (1 + 0.01 * q.full * full) * pg * 4);
       if (parts > 1) ns = (ns + (joined && parts == 2 ? 0 : 2600) + parts * (double)rows * n_blocks * 64 / 2840) * 1.1;
-      if (best.tile < 0 || ns < least) {
+      if (ns < least) {
         best = {t, 0, parts, pg};
         least = ns;
       }
@@ -422,12 +428,11 @@ inline Plan plan(int n_blocks, int k_tiles, int rows, int num_cus, int most_part
 template <bool LOOSE, class Epi>
 void launch_stream(const Plan& p, const char* w, int n_blocks, const X& x, const Epi& epi, hipStream_t st) {
   const int units = (x.k_tiles + (x.tail > 0) + 7) / 8;
-  const unsigned grid = (n_blocks + p.fb - 1) / p.fb;
-  constexpr int threads = 64 * kStreamWaves;
-  if (p.fb == 1) mx4_stream_kernel<1, 3, LOOSE, Epi><<<grid, threads, 0, st>>>(w, x, n_blocks, units, epi);
-  else if (p.fb == 2) mx4_stream_kernel<2, 3, LOOSE, Epi><<<grid, threads, 0, st>>>(w, x, n_blocks, units, epi);
-  else if (p.fb == 7) mx4_stream_kernel<7, 2, LOOSE, Epi><<<grid, threads, 0, st>>>(w, x, n_blocks, units, epi);
-  else mx4_stream_kernel<8, 2, LOOSE, Epi><<<grid, threads, 0, st>>>(w, x, n_blocks, units, epi);
+  const auto go = [&](auto fb) {
+    constexpr int FB = decltype(fb)::value;
+    if (p.fb == FB) mx4_stream_kernel<FB, LOOSE, Epi><<<(n_blocks + FB - 1) / FB, 64 * kStreamWaves, 0, st>>>(w, x, n_blocks, units, epi);
+  };
+  [&]<int... FB>(std::integer_sequence<int, FB...>) { (go(std::integral_constant<int, FB + 1>{}), ...); }(std::make_integer_sequence<int, 8>{});
 }
 
 // Returns the number of arg-max partials per row (LM head).
