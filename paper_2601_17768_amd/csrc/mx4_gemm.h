@@ -155,6 +155,9 @@ __device__ __forceinline__ void wait_rounds(int rounds) {
 // Plain rows are fetched in runs of CH * 64 bytes of a row and lie in LDS as they come, a row's 16-byte pieces exchanged by the row's
 // number so that the 16 rows of an operand read are in 16 different bank groups (pieces of 64 bytes, 16 rows apart by a
 // power of two, meet in few of the L2's channels; 128 rows of 28672 x 4096 so 44 us, in runs 35).
+// Many rows are bound by the matrix cores: 4096 rows of 28672 x 4096 690 us, 1.40 PFLOP/s (the library's product of the two in bf16 723), the
+// conversions hidden behind 16 products each.  128 rows 29 us (22.6 at that rate), a round of workgroups that loads and multiplies in turn;
+// 24 of 4096 x 14336 16 us, of which 14 rounds of 0.36 us in each of 8 parts, whatever the tile, the rest launches.
 template <int NW, int FB, int TB, int CH, int R, int F, int NSET, class Epi>
 __global__ __launch_bounds__(64 * (NW + F), (NW + F + 3) / 4) void mx4_tile_kernel(const char* __restrict__ w, X x, int n_blocks, int units,
                                                                                    int tiles_n, int tiles_m, int parts, int part_groups, Epi epi) {
