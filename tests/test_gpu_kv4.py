@@ -8,9 +8,11 @@ import pytest
 import torch
 
 import mx4_reference as ref
+from gpu_helpers import NOISE_FACTOR
 from helpers import orc, wl, oracle_cfg, randomize_gains
 from paper_2601_17768_amd import binding as B
 from paper_2601_17768_amd import dvr, dvr_stats, kv_layout
+from paper_2601_17768_amd.mx4 import Mx4Matrix
 from paper_2601_17768_amd.session import VerifierSession
 
 pytestmark = pytest.mark.gpu
@@ -464,6 +466,31 @@ def test_decode_step_against_the_checker_on_the_quantised_model(shape, four_bit_
         tok = nxt.clone()
     assert decided >= 30, decided
     sess.close()
+
+@pytest.mark.parametrize("num", [1, 8, 24, 128])
+def test_decode_step_at_the_8b_widths_is_the_model_of_the_quantised_values(num):
+    """Two layers: the step's token is a best one of the verifier on the weights that the 4-bit copy stands for, up to the logits' rounding
+    (both round the same operands to bf16, and differ in the order of their sums: an error of up to 3.5e-2 at these widths and two layers,
+    gpu_helpers.py, times its NOISE_FACTOR, for each of the two logits compared)."""
+    shape = wl.LLAMA_8B.replace(n_layers=2, vocab=16384)
+    to = lambda w, f: {"embed": w["embed"].to(DEV), "final_norm": w["final_norm"].to(DEV), "lm_head": f(w["lm_head"].to(DEV)),
+                       "layers": [{n: t.to(DEV) if n.endswith("norm") else f(t.to(DEV)) for n, t in lw.items()} for lw in w["layers"]]}
+    w = wl.make_weights(shape, seed=42)
+    sess = VerifierSession(shape, to(w, lambda t: t), max_position=1024, device=DEV)
+    values = VerifierSession(shape, to(w, lambda t: Mx4Matrix.quantize(t).values()), max_position=1024, device=DEV)
+    rng = wl.rng_for(5, num)
+    lens = [int(n) for n in rng.integers(1, 400, num)]
+    table, blocks = wl.make_block_table(rng, [n + 2 for n in lens], 16, spare_blocks=2)
+    bt, kv = torch.as_tensor(table, device=DEV), sess.kv_cache(blocks)
+    tok = sess.prefill(kv, bt, [wl.random_tokens(rng, n, shape.vocab) for n in lens], window=64)
+    copy = kv.clone()
+    got = sess.decode_mx4(kv, bt, i32(lens), tok)
+    logits = torch.empty((num, 1, shape.vocab), dtype=torch.float32, device=DEV)
+    values.verify(copy, bt, i32(lens), tok.view(num, 1), dump_seq_ids=i32(range(num)), out_logits=logits)
+    gap = logits[:, 0].max(1).values - logits[:, 0].gather(1, got.long().view(num, 1))[:, 0]
+    assert float(gap.max()) <= 2 * NOISE_FACTOR * 3.5e-2, gap
+    sess.close()
+    values.close()
 
 
 @pytest.mark.parametrize("num", [1, 5, 17, 40, 90, 150])
