@@ -9,6 +9,7 @@ fails loudly - there is no fallback path.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import Dict, Optional
 
@@ -314,9 +315,9 @@ _TYPES = {torch.bfloat16: LLM42_BF16, torch.float32: LLM42_F32}
 
 def _on_current_device(*tensors: Optional[torch.Tensor]) -> None:
     """The library launches on the current device and sees bare pointers only."""
-    for t in tensors:
-        if t is not None and not (t.is_cuda and t.get_device() == torch._C._cuda_getDevice()):
-            raise ValueError("expected tensors on the current device")
+    at = {t.get_device() for t in tensors if t is not None}        # (-1: not on a GPU)
+    if -1 in at or at != {torch._C._cuda_getDevice()}:
+        raise ValueError("expected tensors on the current device")
 
 
 def _matrix(t: torch.Tensor, rows: int, cols: int):
@@ -338,6 +339,7 @@ def _packed(t: torch.Tensor):
     return _ptr(t), t.numel()
 
 
+@functools.lru_cache(maxsize=1024)
 def llm42_mx4_bytes(rows: int, cols: int) -> int:
     out = ctypes.c_size_t()
     _check(load_library().llm42_mx4_bytes(rows, cols, ctypes.byref(out)))

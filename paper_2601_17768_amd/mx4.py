@@ -35,14 +35,15 @@ class Mx4Matrix:
     def matmul(self, x: torch.Tensor, dtype: torch.dtype = torch.bfloat16, out: Optional[torch.Tensor] = None,
                workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
         """One llm42_mx4_matmul call: x [m, cols] (bfloat16) times the transpose, [m, rows] in dtype (or in out's).  The workspace is allocated
-        if none is given (up to 8 rows only if the call cannot do without)."""
+        if none is given and the call makes use of one (up to 8 rows, and 16 of up to 4096 columns, are summed in one piece)."""
         if x.dim() != 2 or x.shape[1] != self.cols:
             raise ValueError(f"x must be [rows, {self.cols}]")
         if out is None:
             out = torch.empty((x.shape[0], self.rows), dtype=dtype, device=self.data.device)
         if tuple(out.shape) != (x.shape[0], self.rows):
             raise ValueError(f"out must be [{x.shape[0]}, {self.rows}]")
-        if workspace is None and (x.shape[0] > 8 or x.data_ptr() % 4 or x.stride(0) % 2):
+        few = x.shape[0] <= (16 if self.cols <= 4096 else 8) and x.data_ptr() % 4 == 0 and x.stride(0) % 2 == 0
+        if workspace is None and not few:
             workspace = torch.empty(B.llm42_mx4_matmul_workspace_bytes(x.shape[0], self.rows, self.cols), dtype=torch.uint8, device=x.device)
         B.llm42_mx4_matmul(self.data, x, out, workspace)
         return out
