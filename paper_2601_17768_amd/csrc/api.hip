@@ -310,6 +310,7 @@ void attention4(const Fast4& f4, int layer, const llm42_kv_cache* kv, int num_se
   a.head_dim = c.head_dim;
   a.window = 1;
   a.max_context = max_context;
+  a.num_cus = m->num_cus;
   a.splits = f4.splits;
   a.split_steps = f4.split_steps;
   a.part_acc = ws.part_acc;

@@ -26,7 +26,7 @@ __global__ __launch_bounds__(64) void kv4_step_check_kernel(const int32_t* __res
   }
 }
 
-constexpr int kWaves = 4;
+constexpr int kWaves = 4;   // of a workgroup, or twice as many
 constexpr int kStep = 64;   // keys
 
 // The keys of one step as they come from memory: four blocks of 16 positions.
@@ -61,7 +61,7 @@ __device__ __forceinline__ float row_sum(float v) {
   return v + __shfl_xor(v, 32);
 }
 
-// A workgroup takes RB blocks of 16 query rows of a (sequence, kv head) over one of the parts of its context; its four waves take the
+// A workgroup takes RB blocks of 16 query rows of a (sequence, kv head) over one of the parts of its context; its NW waves take the
 // part's steps of 64 keys in turn, each with a maximum and sum of its own, and are joined through LDS.
 //   scores: D[key][row] = K Q, K converted with its scales (exact in bf16);
 //   weights: p = exp2((s - ref) / sqrt(head_dim) log2 e) in fp32; ref moves to a step's maximum when that exceeds it by more than 8, so
@@ -73,11 +73,11 @@ __device__ __forceinline__ float row_sum(float v) {
 //   see may stand for NaN, and 0 NaN is NaN.
 // One block of rows is bound by memory: 128 sequences of 1024 - 8192 keys (8 kv heads of 128, group 4) 129 us, 4.9 TB/s; 1 of 512 keys is
 // launch and waiting, 7 us.
-template <int HD, int RB, bool TILES, bool NT>
-__global__ __launch_bounds__(64 * kWaves, RB == 1 ? 3 : 2) void kv4_attention_kernel(Attention4 a, float scale_log2) {
+template <int NW, int HD, int RB, bool TILES, bool NT>
+__global__ __launch_bounds__(64 * NW, NW == 4 && RB == 1 ? 3 : 2) void kv4_attention_kernel(Attention4 a, float scale_log2) {
   constexpr int KT = HD / 32, FB = HD / 16;
-  __shared__ float sh_ml[kWaves][RB][2][16];
-  __shared__ f32x4 sh_acc[kWaves][64 * FB];
+  __shared__ float sh_ml[NW][RB][2][16];
+  __shared__ f32x4 sh_acc[NW][64 * FB];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, g = lane >> 4, l16 = lane & 15;
   const int rows_all = a.group * a.window, row_groups = (rows_all + 16 * RB - 1) / (16 * RB);
   int id = blockIdx.x;
@@ -95,7 +95,7 @@ __global__ __launch_bounds__(64 * kWaves, RB == 1 ? 3 : 2) void kv4_attention_ke
     int status = len < 0 || n < 0 || n > a.window || (int64_t)len + n > a.max_context ? LLM42_SEQ_BAD_LENGTH : LLM42_SEQ_OK;
     bool bad = false;
     if (status == LLM42_SEQ_OK && n > 0)
-      for (int b = threadIdx.x; b <= (len + n - 1) / LLM42_KV_BLOCK; b += 64 * kWaves) {
+      for (int b = threadIdx.x; b <= (len + n - 1) / LLM42_KV_BLOCK; b += 64 * NW) {
         const int block = a.block_table[(size_t)s * a.max_blocks + b];
         bad |= block < 0 || block >= a.num_blocks;
       }
@@ -262,7 +262,7 @@ __global__ __launch_bounds__(64 * kWaves, RB == 1 ? 3 : 2) void kv4_attention_ke
   // The newest position of a decoding step is in the bf16 cache: the wave whose last step holds it stores it before it reads anything
   // (nobody else reads that block; a launch of its own took 5 - 7 us).
   if constexpr (TILES) {
-    if (end == steps && (end - 1 - begin) % kWaves == wave) {
+    if (end == steps && (end - 1 - begin) % NW == wave) {
       const size_t tile = ((size_t)a.row_blk[s] * a.n_kv_heads + kvh) * 16 * HD;
       const int t = len % LLM42_KV_BLOCK;
       store_positions<HD>(a.k_plane + tile, a.v_plane + tile, a.base + kvh * (int64_t)kv_record(HD) + ids[len / LLM42_KV_BLOCK] * to_block, t, t + 1, lane);
@@ -279,9 +279,9 @@ __global__ __launch_bounds__(64 * kWaves, RB == 1 ? 3 : 2) void kv4_attention_ke
     blocks_of(now, step);
     load_k(d, now);
     load_v(d, now);
-    blocks_of(now, min(step + kWaves, end - 1));
+    blocks_of(now, min(step + NW, end - 1));
     const auto one = [&](auto is_edge) __attribute__((always_inline)) {
-      blocks_of(next, min(step + 2 * kWaves, end - 1));
+      blocks_of(next, min(step + 2 * NW, end - 1));
       weights(d, step, is_edge);
       load_k(d, now);
       __builtin_amdgcn_sched_barrier(0);
@@ -290,7 +290,7 @@ __global__ __launch_bounds__(64 * kWaves, RB == 1 ? 3 : 2) void kv4_attention_ke
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int t = 0; t < 4; ++t) now[t] = next[t];
-      step += kWaves;
+      step += NW;
     };
     while (step < inner) one(std::false_type{});
     while (step < end) one(std::true_type{});
@@ -310,12 +310,12 @@ __global__ __launch_bounds__(64 * kWaves, RB == 1 ? 3 : 2) void kv4_attention_ke
 #pragma unroll
     for (int f = 0; f < FB; ++f) sh_acc[wave][f * 64 + lane] = acc[b][f];
     __syncthreads();
-    float top = -INFINITY, w[kWaves], sum = 0.f;
+    float top = -INFINITY, w[NW], sum = 0.f;
 #pragma unroll
-    for (int v = 0; v < kWaves; ++v) top = fmaxf(top, sh_ml[v][b][0][l16]);
+    for (int v = 0; v < NW; ++v) top = fmaxf(top, sh_ml[v][b][0][l16]);
     const float ref = top == -INFINITY ? 0.f : top;
 #pragma unroll
-    for (int v = 0; v < kWaves; ++v) {
+    for (int v = 0; v < NW; ++v) {
       w[v] = __builtin_amdgcn_exp2f(sh_ml[v][b][0][l16] - ref);
       sum += w[v] * sh_ml[v][b][1][l16];
     }
@@ -327,10 +327,10 @@ __global__ __launch_bounds__(64 * kWaves, RB == 1 ? 3 : 2) void kv4_attention_ke
       a.part_ml[2 * slot] = top;
       a.part_ml[2 * slot + 1] = sum;
     }
-    for (int j = wave; j < KT; j += kWaves) {                     // features 32 j + 8 g .. + 7
+    for (int j = wave; j < KT; j += NW) {                     // features 32 j + 8 g .. + 7
       f32x4 even = {0.f, 0.f, 0.f, 0.f}, odd = even;
 #pragma unroll
-      for (int v = 0; v < kWaves; ++v) {
+      for (int v = 0; v < NW; ++v) {
         even += sh_acc[v][2 * j * 64 + lane] * w[v];
         odd += sh_acc[v][(2 * j + 1) * 64 + lane] * w[v];
       }
@@ -391,9 +391,22 @@ void launch(const Attention4& a, hipStream_t st) {
   // K and V past the caches where there is no more than one block of rows to read them and they may be more than the memory-side cache holds
   // (128 sequences of 1024 - 8192 keys 149 -> 134 us, of 8192 220 -> 193; what the caches do hold is slower so, 1 x 8192 16 -> 17.6)
   const bool nt = rb == 1 && (int64_t)a.num_seqs * a.max_context * a.n_kv_heads * kv_record(HD) / LLM42_KV_BLOCK > (256 << 20);
-  if (nt) kv4_attention_kernel<HD, 1, TILES, true><<<grid, 64 * kWaves, 0, st>>>(a, scale_log2);
-  else if (rb == 1) kv4_attention_kernel<HD, 1, TILES, false><<<grid, 64 * kWaves, 0, st>>>(a, scale_log2);
-  else if constexpr (!TILES) kv4_attention_kernel<HD, 2, TILES, false><<<grid, 64 * kWaves, 0, st>>>(a, scale_log2);
+  // No more workgroups than CUs: eight waves in each, where they have more than two rounds of four waves between them (a wave alone on its SIMD
+  // waits for its own conversions: us by four / eight waves 24 x 2000 18.8 / 16.7, 32 x 4000 30.7 / 27.5, 16 x 2000 17.7 / 15.4, 1 x 1000
+  // 9.9 / 9.6; but 1 x 511 7.1 / 7.3, 48 x 2000 25.8 / 30.1)
+  const bool eight = grid <= (unsigned)a.num_cus && a.split_steps > 2 * kWaves;
+  const auto go = [&](auto waves, auto blocks, auto past) {
+    constexpr int NW = decltype(waves)::value, RB = decltype(blocks)::value;
+    kv4_attention_kernel<NW, HD, RB, TILES, decltype(past)::value><<<grid, 64 * NW, 0, st>>>(a, scale_log2);
+  };
+  const auto by_waves = [&](auto blocks, auto past) {
+    if (eight) go(std::integral_constant<int, 2 * kWaves>{}, blocks, past);
+    else go(std::integral_constant<int, kWaves>{}, blocks, past);
+  };
+  using One = std::integral_constant<int, 1>;
+  if (nt) by_waves(One{}, std::true_type{});
+  else if (rb == 1) by_waves(One{}, std::false_type{});
+  else if constexpr (!TILES) by_waves(std::integral_constant<int, 2>{}, std::false_type{});
   if (a.splits > 1) {
     const int64_t all = (int64_t)a.num_seqs * a.n_kv_heads * rows;
     kv4_merge_kernel<HD, TILES><<<(unsigned)((all + 3) / 4), 256, 0, st>>>(a);
@@ -410,8 +423,9 @@ void launch_kv4_step_check(const llm42_model* m, const llm42_kv_cache* kv4, int 
 
 // Parts of a context: two workgroups for every CU, parts of 8 steps (2 a wave) or more - if that is worth the launch that joins them: a wave's step
 // takes about 1 us, the launch 4 - 5, and a device half full of workgroups hides some of the former (us in parts / whole, sequences x
-// keys, 8 kv heads: 1 x 2000 12.8 / 15.9, 1 x 8192 16.9 / 41, 16 x 8192 34 / 50, 4 of window 64 x 4000 41.8 / 43.2; but 8 x 1000
-// 12.8 / 12.0, 24 of 16 - 2040 20.0 / 18.1, 64 x 2048 34.7 / 29.6).
+// keys, 8 kv heads: 1 x 2000 12.8 / 15.9, 1 x 8192 16.9 / 41, 16 x 8192 34 / 50; but 8 x 1000
+// 12.8 / 12.0, 64 x 2048 34.7 / 29.6).  Not where whole contexts put a workgroup of eight waves on more than half of the CUs (24 x 4000
+// 30.0 / 26.3, 24 x 8000 47.9 / 43.5, 4 of window 64 x 4000 41.4 / 36.3).
 void plan_kv4_attention(int num_seqs, int n_kv_heads, int rows, int max_context, int num_cus, int& splits, int& split_steps) {
   const int rb = rows > 16 ? 2 : 1;
   const int64_t wgs = (int64_t)num_seqs * n_kv_heads * ((rows + 16 * rb - 1) / (16 * rb));
@@ -419,7 +433,8 @@ void plan_kv4_attention(int num_seqs, int n_kv_heads, int rows, int max_context,
   const int64_t want = (2LL * num_cus + wgs - 1) / wgs;
   int part = (int)((steps + want - 1) / want);
   part = (part < 8 ? 8 : part + kWaves - 1) / kWaves * kWaves;
-  const bool split = (steps + kWaves - 1) / kWaves - part / kWaves >= (2 * wgs < num_cus ? 6 : 8);
+  const bool whole = 2 * wgs > num_cus && wgs <= num_cus;
+  const bool split = !whole && (steps + kWaves - 1) / kWaves - part / kWaves >= (2 * wgs < num_cus ? 6 : 8);
   split_steps = split ? part : steps;
   splits = (steps + split_steps - 1) / split_steps;
 }

@@ -107,6 +107,7 @@ struct Attention4 {
   int64_t q_stride, out_stride;
   bool tiles;
   int num_seqs, n_kv_heads, group, head_dim, window, max_context;
+  int num_cus;
   int splits, split_steps;     // parts of a sequence, steps of 64 keys in each
   float* part_acc;             // [seq][kv head][split][row][head_dim]
   float* part_ml;              // [seq][kv head][split][row][2]

@@ -230,6 +230,7 @@ llm42_status llm42_kv4_attention(const llm42_model* m, int32_t layer, const llm4
   a.head_dim = c.head_dim;
   a.window = window;
   a.max_context = max_context;
+  a.num_cus = m->num_cus;
   a.part_acc = ws.acc;
   a.part_ml = ws.ml;
   a.k_plane = a.v_plane = nullptr;
