@@ -36,32 +36,37 @@ struct X {
   }
 };
 
-// Up to 16 rows.  A workgroup owns FB feature blocks; its eight waves take the groups of 4 k-tiles in turn, each with
-// accumulators of its own for all of them, and are added through LDS.  Codes and activations of two groups are on their way at
+// Up to 16 or 32 rows (TB token blocks).  A workgroup owns FB feature blocks; its eight waves take the groups of 4 k-tiles in turn, each
+// with accumulators of its own for all of them, and are added through LDS.  Codes and activations of two groups are on their way at
 // a time; no barrier, for no two waves want the same bytes.  A wave has four groups of a 4096-column matrix, so nothing is loaded past the
 // last one (1 row of 6144 x 4096 so 6.2 -> 4.6 us, from memory 7.7 -> 5.8; 28672 x 4096 15.1 -> 13.9, 4.5 TB/s).  LOOSE: plain
 // rows of any number of columns that are only 4-byte aligned are read as they lie (behind a launch that brings them in order first 13
 // rows of 1000 x 700 took 7.8 us instead of 4.6, 16 of 4096 x 4100 11.6 instead of 8.9); the last wave takes the columns behind
 // the last whole k-tile.  (Rows that begin in the middle of a word are brought in order: 16 rows of 4096 x 4097 took 28 us by loads of
 // 16 bytes, 13.4 by aligned words and shifts, 11.7 so.)
-constexpr int kStreamWaves = 8, kStreamRows = 16;
-template <int FB, bool LOOSE, class Epi>
+constexpr int kStreamWaves = 8, kStreamRows = 16, kStreamWide = 4;   // (feature blocks that fit beside 32 rows)
+template <int FB, int TB, bool LOOSE, class Epi>
 __global__ __launch_bounds__(64 * kStreamWaves) void mx4_stream_kernel(const char* __restrict__ w, X x, int n_blocks, int units, Epi epi) {
   constexpr int NW = kStreamWaves;
-  __shared__ f32x4 part[NW][FB * 64];
+  static_assert(TB == 1 || !LOOSE, "loose rows are those of one token block");
+  __shared__ f32x4 part[NW][FB * TB * 64];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int n0 = blockIdx.x * FB;
   const char* wp[FB];
 #pragma unroll
   for (int i = 0; i < FB; ++i) wp[i] = w + (size_t)min(n0 + i, n_blocks - 1) * units * kRecord;
-  const uint16_t* xp = x.at(0, lane);
-  const int xs = x.step(), mine = ((x.k_tiles + 3) / 4 - wave + NW - 1) / NW;
-  f32x4 acc[FB];
+  const uint16_t* xp[TB];
 #pragma unroll
-  for (int i = 0; i < FB; ++i) acc[i] = (f32x4){0.f, 0.f, 0.f, 0.f};
+  for (int b = 0; b < TB; ++b) xp[b] = x.at(b, lane);
+  const int xs = x.step(), mine = ((x.k_tiles + 3) / 4 - wave + NW - 1) / NW;
+  f32x4 acc[FB][TB];
+#pragma unroll
+  for (int i = 0; i < FB; ++i)
+#pragma unroll
+    for (int b = 0; b < TB; ++b) acc[i][b] = (f32x4){0.f, 0.f, 0.f, 0.f};
   u32x4 codes[2][FB];
   uint32_t scales[2][FB];
-  bf16x8 xv[2][4];
+  bf16x8 xv[2][4][TB];
   auto load = [&](auto set, int i) __attribute__((always_inline)) {
     constexpr int U = decltype(set)::value;
     const int g = i * NW + wave;
@@ -72,11 +77,13 @@ __global__ __launch_bounds__(64 * kStreamWaves) void mx4_stream_kernel(const cha
       scales[U][f] = *(const uint32_t*)(rec + kScales + (g & 1) * 4 + (lane & 15) * 8);
     }
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      typedef bf16x8 words __attribute__((aligned(4)));
-      const uint16_t* from = xp + (size_t)min(g * 4 + j, x.k_tiles - 1) * xs;
-      xv[U][j] = LOOSE ? (bf16x8)*(const words*)from : *(const bf16x8*)from;
-    }
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int b = 0; b < TB; ++b) {
+        typedef bf16x8 words __attribute__((aligned(4)));
+        const uint16_t* from = xp[b] + (size_t)min(g * 4 + j, x.k_tiles - 1) * xs;
+        xv[U][j][b] = LOOSE ? (bf16x8)*(const words*)from : *(const bf16x8*)from;
+      }
   };
   auto compute = [&](auto set, int i) __attribute__((always_inline)) {
     constexpr int U = decltype(set)::value;
@@ -85,7 +92,11 @@ __global__ __launch_bounds__(64 * kStreamWaves) void mx4_stream_kernel(const cha
     for (int j = 0; j < 4; ++j) {
       if (k0 + j >= x.k_tiles) break;                // (columns that only pad: X has none there)
 #pragma unroll
-      for (int f = 0; f < FB; ++f) acc[f] = mfma16(operand(codes[U][f][j], scale_of(scales[U][f], j)), xv[U][j], acc[f]);
+      for (int f = 0; f < FB; ++f) {
+        const bf16x8 a = operand(codes[U][f][j], scale_of(scales[U][f], j));
+#pragma unroll
+        for (int b = 0; b < TB; ++b) acc[f][b] = mfma16(a, xv[U][j][b], acc[f][b]);
+      }
     }
   };
   using Set0 = std::integral_constant<int, 0>;
@@ -112,7 +123,7 @@ __global__ __launch_bounds__(64 * kStreamWaves) void mx4_stream_kernel(const cha
     compute(Set0{}, 0);
   }
   if (LOOSE && x.tail && wave == NW - 1) {
-    const uint16_t* from = xp + (size_t)x.k_tiles * 32;
+    const uint16_t* from = xp[0] + (size_t)x.k_tiles * 32;
     u32x4 v = {0, 0, 0, 0};
 #pragma unroll
     for (int i = 0; i < 8; ++i)
@@ -122,17 +133,21 @@ __global__ __launch_bounds__(64 * kStreamWaves) void mx4_stream_kernel(const cha
       const char* rec = wp[f] + (size_t)(x.k_tiles >> 3) * kRecord;
       const uint32_t word = *(const uint32_t*)(rec + (x.k_tiles >> 2 & 1) * 1024 + lane * 16 + (x.k_tiles & 3) * 4);
       const uint32_t byte = *(const uint8_t*)(rec + kScales + (lane & 15) * 8 + (x.k_tiles & 7));
-      acc[f] = mfma16(operand(word, scale_of(byte, 0)), __builtin_bit_cast(bf16x8, v), acc[f]);
+      acc[f][0] = mfma16(operand(word, scale_of(byte, 0)), __builtin_bit_cast(bf16x8, v), acc[f][0]);
     }
   }
 #pragma unroll
-  for (int i = 0; i < FB; ++i) part[wave][i * 64 + lane] = acc[i];
+  for (int i = 0; i < FB; ++i)
+#pragma unroll
+    for (int b = 0; b < TB; ++b) part[wave][(i * TB + b) * 64 + lane] = acc[i][b];
   __syncthreads();
-  if (wave < FB && n0 + wave < n_blocks) {
+  const int nb = n0 + wave / TB, row = wave % TB * 16 + (lane & 15);
+  static_assert(FB * TB <= NW, "a wave adds up one block");
+  if (wave < FB * TB && nb < n_blocks) {
     f32x4 sum = part[0][wave * 64 + lane];
 #pragma unroll
     for (int v = 1; v < NW; ++v) sum += part[v][wave * 64 + lane];
-    epi(n0 + wave, lane, lane & 15, sum, epi.pre(n0 + wave, lane, lane & 15, epi.row_info(lane & 15)));
+    epi(nb, lane, row, sum, epi.pre(nb, lane, row, epi.row_info(row)));
   }
 }
 
@@ -394,7 +409,9 @@ struct Plan {
 // mx4_stream_kernel for up to 16 rows (us, it / the best tile: 1 row of 4096 x 4096 4.8 / 9.2, 16 6.7 / 9.8; 1 of 28672 x 4096 13.1 / 19.6, 16
 // 14.6 / 19.9; 16 of 50304 x 512 7.4 / 7.9), except where more than 8 rows are summed over many columns for few features: it has but eight
 // waves for a sum, each of which takes 0.6 us and 28 ns a row for a group, a tile several workgroups (16 rows of 512 x 14336 16.1 / 10.7,
-// of 512 x 4096 6.1 / 7.7).  A workgroup per CU where eight feature blocks are enough for that, else seven or eight, whichever leave fewer
+// of 512 x 4096 6.1 / 7.7).  Up to 32 rows where four feature blocks a workgroup put one on every CU, by a like rule (24 rows of 1024 x 1024
+// 3.8 / 5.3, 6144 x 4096 9.8 / 13.6 in one piece, 16384 x 4096 12.4 / 15.3; 32 of 4096 x 4096 10.3 / 8.9: every wave reads its columns of all
+// rows, which bounds it).  A workgroup per CU where eight feature blocks are enough for that, else seven or eight, whichever leave fewer
 // idle in the last round (16 rows, us by 1 / 2 / 3 / 4 / 7 / 8 of them: 8192 x 4096 11.5 / 7.6 / 8.2 / 9.0 / 11.9 / 12.9,
 // 16384 x 4096 21 / 12.5 / 14.6 / 9.7 / 12.7 / 13.7, 28672 x 4096 36 / 22 / 21 / 18 / 14.6 / 15.6, 128256 x 4096 153 / 77 / 72 / 67 / 62 / 57).
 // Else the tile and the number of parts that cost least; a part has a plane of fp32 sums of its own, written and
@@ -410,7 +427,9 @@ inline Plan plan(int n_blocks, int k_tiles, int rows, int num_cus, int most_part
   const int groups = (k_tiles + 3) / 4, blocks = (rows + 15) / 16;
   Plan best = stream_plan(n_blocks, k_tiles, num_cus);
   if (rows <= 8 || (rows <= kStreamRows && n_blocks > num_cus)) return best;
-  double least = rows <= kStreamRows ? 2300 + groups / 8. * (600 + 28 * rows) : 1e30;
+  double least = rows <= kStreamRows                                      ? 2300 + groups / 8. * (600 + 28 * rows)
+                 : rows <= 2 * kStreamRows && n_blocks <= kStreamWide * num_cus ? 2600 + groups / 8. * (150 + 250 * best.fb + 50 * rows)
+                                                                              : 1e30;
   for (int t = 0; t < kTileCount4; ++t)
     for (int want = 1; want <= most_parts; want *= 2) {
       const int pg = (groups + want - 1) / want, parts = (groups + pg - 1) / pg;
@@ -433,7 +452,12 @@ void launch_stream(const Plan& p, const char* w, int n_blocks, const X& x, const
   const int units = (x.k_tiles + (x.tail > 0) + 7) / 8;
   const auto go = [&](auto fb) {
     constexpr int FB = decltype(fb)::value;
-    if (p.fb == FB) mx4_stream_kernel<FB, LOOSE, Epi><<<(n_blocks + FB - 1) / FB, 64 * kStreamWaves, 0, st>>>(w, x, n_blocks, units, epi);
+    const unsigned grid = (n_blocks + FB - 1) / FB, threads = 64 * kStreamWaves;
+    if (p.fb != FB) return;
+    if constexpr (!LOOSE && FB <= kStreamWide) {
+      if (x.last_row >= kStreamRows) return mx4_stream_kernel<FB, 2, false, Epi><<<grid, threads, 0, st>>>(w, x, n_blocks, units, epi);
+    }
+    mx4_stream_kernel<FB, 1, LOOSE, Epi><<<grid, threads, 0, st>>>(w, x, n_blocks, units, epi);
   };
   [&]<int... FB>(std::integer_sequence<int, FB...>) { (go(std::integral_constant<int, FB + 1>{}), ...); }(std::make_integer_sequence<int, 8>{});
 }
