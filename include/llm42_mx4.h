@@ -69,8 +69,9 @@ llm42_status llm42_mx4_dequantize(
  * a bf16), summed in fp32 in an order that depends on the sizes; out is rounded once.  x[i] at x + i * x_stride elements and
  * out[i] at out + i * out_stride; what lies between the rows of out is left as it was.  out must not overlap x or w.
  * workspace: llm42_mx4_matmul_workspace_bytes(rows, n, k) bytes, 256-byte aligned.  Rows that are not 4-byte aligned need it, and so do
- * more than 16 that are not 16-byte aligned, are more than 2^26 elements apart or whose k is not a multiple of 32 (LLM42_EWORKSPACE).  Otherwise the call does with less, or NULL,
- * but then sums over k in one piece, which takes longer where rows and n are few (and gives other low bits). */
+ * more than 16 that are not 16-byte aligned, are more than 2^26 elements apart or whose k is not a multiple of 32 (LLM42_EWORKSPACE).
+ * Otherwise the call does with less, or NULL, but then sums over k in one piece, which takes longer where rows and n are few (and
+ * gives other low bits). */
 llm42_status llm42_mx4_matmul_workspace_bytes(int32_t rows, int32_t n, int32_t k, size_t* out_bytes);
 llm42_status llm42_mx4_matmul(
     const void* w,                 /* dev                                                 */
@@ -98,7 +99,7 @@ llm42_status llm42_kv4_bytes(const llm42_model* model, int64_t num_blocks, size_
 /* K and V of positions first[s] .. first[s] + count[s] - 1 of every sequence, all layers, from the bf16 cache into the 4-bit
  * one.  Behind a verifier pass and its commit: first = the length before, count = the committed tokens; behind a prefill: 0 and
  * the length.  No other position is written; no two of a call's blocks of positions may lie in the same 4-bit block.
- * first[s] < 0 or beyond a table's capacity, count[s] outside 0 .. max_count: LLM42_SEQ_BAD_LENGTH; a needed entry of either
+ * first[s] < 0, positions beyond a table's capacity, count[s] outside 0 .. max_count: LLM42_SEQ_BAD_LENGTH; a needed entry of either
  * table out of range: LLM42_SEQ_BAD_BLOCK; nothing of such a sequence is stored. */
 llm42_status llm42_kv4_store(
     const llm42_model*    model,
@@ -164,10 +165,11 @@ llm42_status llm42_mx4_model_create(const llm42_model* model, llm42_mx4_model** 
 void         llm42_mx4_model_destroy(llm42_mx4_model* mx4);
 
 /* llm42_decode_step_sampled by the 4-bit copy: the same arguments, effects, errors and status.  K and V of the input tokens are
- * written to the bf16 cache as there.  workspace: llm42_decode_step_mx4_workspace_bytes, 256-byte aligned.  kv4_cache NULL: attention over the bf16 cache.  Else they are stored into the 4-bit cache as
- * well, and attention reads that: positions 0 .. seq_lens[s] - 1 must have been stored, and its block table needs entries for
- * position seq_lens[s] too (a block that no other sequence of the call has there; max_context up to 2^30).  The verifier overwrites the window's entries of the bf16 cache; those of the 4-bit cache are
- * overwritten by llm42_kv4_store behind the commit. */
+ * written to the bf16 cache as there.  workspace: llm42_decode_step_mx4_workspace_bytes, 256-byte aligned.
+ * kv4_cache NULL: attention over the bf16 cache.  Else they are stored into the 4-bit cache as well, and attention reads that: positions
+ * 0 .. seq_lens[s] - 1 must have been stored, and its block table needs entries for position seq_lens[s] too (a block that no other
+ * sequence of the call has; max_context up to 2^30).  The verifier overwrites the window's entries of the bf16 cache; those of the
+ * 4-bit cache are overwritten by llm42_kv4_store behind the commit. */
 llm42_status llm42_decode_step_mx4_workspace_bytes(const llm42_mx4_model* mx4, int32_t max_seqs, int32_t max_context,
                                                    size_t* out_bytes);
 llm42_status llm42_decode_step_mx4(

@@ -125,7 +125,8 @@ void launch_mx4_pack_x(const uint16_t* x, int64_t stride, int rows, int k, uint1
 
 // Up to this many rows of x are read as they lie if they are 4-byte aligned (loose).
 int mx4_loose_rows();
-// x: row-major (x_stride > 0; loose, or 16-byte aligned and k a multiple of 32) or tile layout (0).  parts: mx4_matmul_part_bytes bytes, or null: the sum is not split.
+// x: row-major (x_stride > 0; loose, or 16-byte aligned and k a multiple of 32) or tile layout (0).  parts:
+// mx4_matmul_part_bytes bytes, or null: the sum is not split.
 size_t mx4_matmul_part_bytes(int n, int k, int rows, int num_cus);
 void launch_mx4_matmul(const void* w, int n, int k, const uint16_t* x, int64_t x_stride, bool loose, int rows, void* out, int out_type,
                        int64_t out_stride, int num_cus, float* parts, hipStream_t st);
