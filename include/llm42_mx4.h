@@ -130,7 +130,7 @@ llm42_status llm42_kv4_read(
 /* Attention of one layer over the 4-bit cache.  Row (s, i), i < n_valid[s], is the query at position seq_lens[s] + i and sees
  * positions 0 .. seq_lens[s] + i, all of which must have been stored; its head h uses kv head h / (n_q_heads / n_kv_heads):
  * out = softmax(q . k / sqrt(head_dim)) v.  Weights are rounded to bf16 before they multiply V; sums are fp32, of weights up to 2^8,
- * so that magnitudes of V up to about 2^119 / max_context stay in range.
+ * so that magnitudes of V up to about 2^119 / max_context stay in range (and those below 2^-110 may count as zero).
  * q and out: bf16 rows of n_q_heads * head_dim, row (s, i) at (s * window + i) * stride elements; both 16-byte aligned, strides
  * multiples of 8 and at least that long.  Rows that take no part (i >= n_valid[s]; a sequence whose status is not
  * LLM42_SEQ_OK; n_valid[s] may be 0) are left as they were.  max_context: as in llm42_verify_window, up to 2^30.

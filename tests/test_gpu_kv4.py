@@ -296,6 +296,53 @@ def test_attention_rows_do_not_see_a_later_nan(hd):
     sess.close()
 
 
+def test_attention_of_the_longest_window_and_the_most_sequences():
+    sess = session(2, 8, 64)
+    check_attention(sess, [0, 700], [B.LLM42_MAX_WINDOW, 500], B.LLM42_MAX_WINDOW)
+    c = Cache(sess, [33, 20])
+    kv4, num = c.mirror(sess), B.LLM42_MAX_ROWS                  # (as many as a call takes, on the blocks of two)
+    q = torch.randn(num, 1, 16, 64, device=DEV).to(torch.bfloat16)
+    lens = i32([32, 19]).repeat(num // 2)
+    got = sess.kv4_attention(1, kv4, c.bt.repeat(num // 2, 1), q, lens)
+    for at in (0, 31000, num - 2):                               # (one step of keys: the same sums alone)
+        assert torch.equal(got[at:at + 2], sess.kv4_attention(1, kv4, c.bt, q[at:at + 2].contiguous(), lens[:2].contiguous()))
+    sess.close()
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+def test_store_and_read_of_many_sequences_and_in_a_graph(hd):
+    sess = session(3, 2, hd)
+    c, num = Cache(sess, [40]), 30000                            # every sequence reads the one cache; the first of them stores
+    kv4 = c.mirror(sess)
+    first, count = i32([7] * num), i32([0] * (num - 1) + [30])
+    k, v = sess.kv4_read(kv4, c.bt.repeat(num, 1), first, count, 30)
+    assert torch.equal(k[:, -1].cpu(), ref.quantized(c.k[0][:, 7:37]).to(torch.bfloat16))
+    assert torch.equal(v[:, -1].cpu(), ref.quantized(c.v[0][:, 7:37]).to(torch.bfloat16)) and not bool(k[:, :-1].any())
+    status = i32([9] * num)
+    kv4.fill_(255)
+    sess.kv4_store(c.kv, kv4, c.bt.repeat(num, 1), first, count, 30, seq_status=status)
+    assert not bool(status.any())
+    a, n = i32([0]), i32([40])
+    ko, vo = (torch.zeros(2, 1, 40, 3, hd, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    graph = torch.cuda.CUDAGraph()
+    sess.kv4_store(c.kv, kv4, c.bt, a, n, 40)
+    with torch.cuda.graph(graph):
+        sess.kv4_store(c.kv, kv4, c.bt, a, n, 40)
+        sess.kv4_read(kv4, c.bt, a, n, 40, ko, vo)
+    for lo, cnt, scale in ((0, 40, 1.0), (16, 16, 2.0), (39, 1, -0.5), (3, 0, 4.0), (5, 30, 1.0)):
+        before = sess.kv4_read(kv4, c.bt, i32([0]), i32([40]), 40)
+        kv_layout.write_tokens(c.kv, c.bt[0], c.k[0] * scale, c.v[0] * scale)
+        a.fill_(lo), n.fill_(cnt), ko.fill_(1.0), vo.fill_(1.0)
+        graph.replay()
+        after = sess.kv4_read(kv4, c.bt, i32([0]), i32([40]), 40)
+        for x, out, old, new in ((c.k[0], ko, before[0], after[0]), (c.v[0], vo, before[1], after[1])):
+            want = ref.quantized(x * scale).to(torch.bfloat16)[:, lo:lo + cnt]
+            assert torch.equal(out[:, 0, :cnt].cpu(), want) and bool((out[:, 0, cnt:] == 1.0).all())
+            old[:, 0, lo:lo + cnt] = want.to(DEV)
+            assert torch.equal(new, old)
+    sess.close()
+
+
 def test_attention_of_empty_windows_in_parts():
     sess = session(2, 4, 128)
     check_attention(sess, [5000, 0, 4000, 77], [0, 0, 1, 3], 5)

@@ -115,7 +115,7 @@ TILES = [(130, 33000, 260), (130, 33000, 288), (70, 33000, 260), (70, 33000, 288
          (5, 5000, 1090), (16, 20, 31), (1, 3, 1), (12, 40, 4100), (16, 33000, 287), (16, 33000, 4095), (7, 60, 257), (2, 8200, 223),
          (8, 5000, 1088), (9, 8200, 1090), (16, 8200, 1088), (3, 9000, 2050), (8, 33000, 1024 + 64), (20, 33000, 260), (20, 4112, 4100),
          (20, 40, 8200), (20, 40, 4100), (20, 16400, 260), (24, 33000, 33), (9, 14336, 260), (6, 24000, 96),
-         (3, 61000, 40), (20, 5000, 288), (30, 9000, 1024), (32, 16000, 2048), (17, 15000, 4100), (31, 300, 64), (17, 16, 33)]
+         (3, 61000, 40), (20, 5000, 288), (30, 9000, 1024), (32, 16000, 2048), (17, 15000, 4100), (31, 300, 64), (17, 16, 33), (65536, 48, 96), (65536, 17, 1030), (30000, 16, 4128)]
 
 
 @pytest.mark.parametrize("rows,n,k", TILES)
