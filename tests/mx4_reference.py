@@ -40,7 +40,7 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, first: int):
 
 
 class QuantizingKV:
-    """A cache for the checker's forward pass that holds what is written to it in MXFP4."""
+    """A cache for the oracle's forward pass that holds what is written to it in MXFP4."""
 
     class Plane:
         def __init__(self, shape):

@@ -477,8 +477,8 @@ HEADS128 = wl.ModelShape(n_layers=2, d_model=256, n_q_heads=6, n_kv_heads=2, hea
 
 @pytest.mark.parametrize("shape", [wl.TINY, HEADS128], ids=["hd64", "hd128"])
 @pytest.mark.parametrize("four_bit_cache", [False, True], ids=["bf16_cache", "4bit_cache"])
-def test_decode_step_against_the_checker_on_the_quantised_model(shape, four_bit_cache):
-    """The checker run on the weights that the 4-bit copy stands for, with a cache that holds what the 4-bit one does: the same token
+def test_decode_step_against_the_oracle_on_the_quantised_model(shape, four_bit_cache):
+    """The oracle run on the weights that the 4-bit copy stands for, with a cache that holds what the 4-bit one does: the same token
     wherever its two best logits are further apart than twice the small model's tolerance."""
     w = randomize_gains(wl.make_weights(shape, seed=11))
     cfg, wq = oracle_cfg(shape), ref.quantized_weights(w)
