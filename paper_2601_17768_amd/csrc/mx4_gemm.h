@@ -172,7 +172,7 @@ __device__ __forceinline__ void wait_rounds(int rounds) {
 // power of two, meet in few of the L2's channels; 128 rows of 28672 x 4096 so 44 us, in runs 35).
 // Many rows are bound by the matrix cores: 4096 rows of 28672 x 4096 690 us, 1.40 PFLOP/s (the library's product of the two in bf16 723), the
 // conversions hidden behind 16 products each.  128 rows 29 us (22.6 at that rate), a round of workgroups that loads and multiplies in turn;
-// 24 of 4096 x 14336 16 us, of which 14 rounds of 0.36 us in each of 8 parts, whatever the tile, the rest launches.
+// 24 of 4096 x 14336 15 us, of which 14 rounds of 0.36 us in each of 8 parts, whatever the tile, the rest launches.
 template <int NW, int FB, int TB, int CH, int R, int F, int NSET, class Epi>
 __global__ __launch_bounds__(64 * (NW + F), (NW + F + 3) / 4) void mx4_tile_kernel(const char* __restrict__ w, X x, int n_blocks, int units,
                                                                                    int tiles_n, int tiles_m, int parts, int part_groups, Epi epi) {
@@ -189,6 +189,10 @@ __global__ __launch_bounds__(64 * (NW + F), (NW + F + 3) / 4) void mx4_tile_kern
   const int panel = at / (tiles_n * PANEL), in = at - panel * tiles_n * PANEL, width = min(PANEL, tiles_m - panel * PANEL);
   const int n0 = in / width * TBN, m0 = (panel * PANEL + in % width) * TB;
   const int k_begin = part * part_groups * 4, k_tiles = min(x.k_tiles - k_begin, part_groups * 4), rounds = (k_tiles + CH - 1) / CH;
+  // Up to 32 rows the workgroups of an XCD begin at different columns, so that they do not all ask one L2 channel for the same activations
+  // (24 rows of 4096 x 14336 15.9 -> 14.9 us, of 28672 x 4096 18.6 -> 17.8; 64 of 6144 x 4096 12.0 -> 12.6, 512 of 4096 x 14336 54 -> 60:
+  // with several tiles of rows they share what each has just fetched)
+  const int turn = TB > 2 || tiles_m > 1 || k_tiles % 4 ? 0 : (int)((uint32_t)(blockIdx.x >> 3) * (uint32_t)(k_tiles / 4) / (uint32_t)per_xcd);
   if (wave >= NW) {
     const int fw = wave - NW;
     const uint32_t dst = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)&ring[0][0] + fw * PW * 1024;
@@ -219,9 +223,10 @@ __global__ __launch_bounds__(64 * (NW + F), (NW + F + 3) / 4) void mx4_tile_kern
     }
     const uint32_t run = CH * x.step() * 2, most = x.stride ? k_tiles * 64u - 16u : (k_tiles - 1) * 1024u;
     auto fetch = [&](int r) {                        // (past the last k-tile: within it)
+      const int from = r + turn * SUB < rounds ? r + turn * SUB : r + turn * SUB - rounds;
 #pragma unroll
       for (int i = 0; i < PW; ++i)
-        lds_fetch_1k(src[i / CH], min((uint32_t)r * run + piece[i % CH], most) + off[i], dst + (uint32_t)((r % R) * CH * TB + i) * 1024u);
+        lds_fetch_1k(src[i / CH], min((uint32_t)from * run + piece[i % CH], most) + off[i], dst + (uint32_t)((r % R) * CH * TB + i) * 1024u);
     };
     for (int r = 0; r < min(R - 1, rounds); ++r) fetch(r);
     wait_rounds<R - 3, PW>(min(R - 3, rounds - 2));
@@ -251,7 +256,7 @@ __global__ __launch_bounds__(64 * (NW + F), (NW + F + 3) / 4) void mx4_tile_kern
   const int groups = (k_tiles + 3) / 4;
   auto load = [&](auto set, int g) __attribute__((always_inline)) {   // (groups past the range re-read the last one)
     constexpr int U = decltype(set)::value;
-    const int c = min(g, groups - 1) + first_group;
+    const int to = min(g, groups - 1) + turn, c = (to < groups ? to : to - groups) + first_group;
 #pragma unroll
     for (int i = 0; i < FB; ++i) {
       const char* rec = wp[i] + (size_t)(c >> 1) * kRecord;
