@@ -38,7 +38,8 @@ extern "C" {
 /* ---- matrices ------------------------------------------------------------------------------------------ */
 
 /* Bytes of a rows x cols matrix in MXFP4, rows 1 .. 2^30 and cols 1 .. 2^26.  The layout inside is the library's own (tiles of 16 rows x
- * 256 columns, padded with zeros: about 4.25 bits a value where cols is a multiple of 256). */
+ * 256 columns, padded with zeros: about 4.25 bits a value where cols is a multiple of 256).  A call takes matrices of up to
+ * 2^26 - 4 tiles: LLM42_EINVAL beyond. */
 llm42_status llm42_mx4_bytes(int32_t rows, int32_t cols, size_t* out_bytes);
 
 /* src[r][c] at src + r * src_stride + c elements of type src_type; blocks run along c.  dst: 16-byte aligned,
@@ -71,7 +72,8 @@ llm42_status llm42_mx4_dequantize(
  * workspace: llm42_mx4_matmul_workspace_bytes(rows, n, k) bytes, 256-byte aligned.  Rows that are not 4-byte aligned need it, and so do
  * more than 16 that are not 16-byte aligned, are more than 2^26 elements apart or whose k is not a multiple of 32 (LLM42_EWORKSPACE).
  * Otherwise the call does with less, or NULL, but then sums over k in one piece, which takes longer where rows and n are few (and
- * gives other low bits). */
+ * gives other low bits).  LLM42_EINVAL where rows * n (past 2^28), or rows * k of rows that need the workspace (about 2^35), ask for more
+ * threads than one launch takes (2^32). */
 llm42_status llm42_mx4_matmul_workspace_bytes(int32_t rows, int32_t n, int32_t k, size_t* out_bytes);
 llm42_status llm42_mx4_matmul(
     const void* w,                 /* dev                                                 */

@@ -123,11 +123,15 @@ void launch_mx4_dequantize(const void* src, int rows, int cols, void* dst, int t
 // x to the tile layout, columns padded with zeros to a multiple of 32
 void launch_mx4_pack_x(const uint16_t* x, int64_t stride, int rows, int k, uint16_t* dst, hipStream_t st);
 
+// HIP takes fewer than 2^32 threads along x: so many workgroups of 256.
+constexpr unsigned kMostGroups256 = 0xFFFFFFFFu / 256;
+
 // Up to this many rows of x are read as they lie if they are 4-byte aligned (loose).
 int mx4_loose_rows();
 // x: row-major (x_stride > 0; loose, or 16-byte aligned and k a multiple of 32) or tile layout (0).  parts:
 // mx4_matmul_part_bytes bytes, or null: the sum is not split.
 size_t mx4_matmul_part_bytes(int n, int k, int rows, int num_cus);
+bool mx4_matmul_fits(int n, int k, int rows, bool loose, int num_cus, bool parts);   // ... what a launch takes
 void launch_mx4_matmul(const void* w, int n, int k, const uint16_t* x, int64_t x_stride, bool loose, int rows, void* out, int out_type,
                        int64_t out_stride, int num_cus, float* parts, hipStream_t st);
 void launch_mx4_qkv(const llm42_mx4_model* m4, int layer, const llm42_kv_cache* kv, const Workspace& ws, hipStream_t st);

@@ -20,7 +20,7 @@ int num_cus() {
   return cus;
 }
 
-// Largest matrix and context: index arithmetic in 32 bits stays in range below them.
+// Largest matrix: index arithmetic in 32 bits stays in range below it.
 constexpr int32_t kMostRows = 1 << 30, kMostCols = 1 << 26;
 
 bool known_type(int32_t t) { return t == LLM42_BF16 || t == LLM42_F32; }
@@ -42,7 +42,7 @@ llm42_status check_matrix(const char* who, const void* packed, size_t bytes, int
   if ((uintptr_t)plain % size_of(type)) return fail(LLM42_EINVAL, "%s: plain array not aligned to its type", who);
   if ((uintptr_t)packed % 16) return fail(LLM42_EINVAL, "%s: 4-bit matrix not 16-byte aligned", who);
   const size_t need = mx4::matrix_bytes(rows, cols);
-  if (need / mx4::kRecord / 4 >= 0x7FFFFFFFu) return fail(LLM42_EINVAL, "%s: matrix too large", who);
+  if (need / mx4::kRecord > 4 * kMostGroups256) return fail(LLM42_EINVAL, "%s: a matrix of more than %u records of 16 x 256", who, 4 * kMostGroups256);
   if (bytes < need) return fail(LLM42_EWORKSPACE, "%s: 4-bit matrix of %zu < %zu bytes", who, bytes, need);
   return LLM42_OK;
 }
@@ -147,6 +147,11 @@ llm42_status llm42_mx4_matmul(const void* w, size_t w_bytes, int32_t n, int32_t 
     if (!workspace || (uintptr_t)workspace % 256) return fail(LLM42_EWORKSPACE, "%s: this x needs a workspace, 256-byte aligned", who);
     return fail(LLM42_EWORKSPACE, "%s: workspace %zu < %zu bytes", who, workspace_bytes, need);
   }
+  if (pack && align_up(rows, 16) * align_up(k, 32) / 8 > (size_t)kMostGroups256 * 256)
+    return fail(LLM42_EINVAL, "%s: rows * k too large for rows that are not aligned", who);
+  // (up to 2^28 values any tile's workgroups, at most eight parts of 384 threads for 64 x 32 of them, are within a launch)
+  if ((int64_t)rows * n > (1 << 28) && !mx4_matmul_fits(n, k, rows, loose, num_cus(), room && need > packed))
+    return fail(LLM42_EINVAL, "%s: rows * features too large for one launch", who);
   if (pack) launch_mx4_pack_x((const uint16_t*)x, x_stride, rows, k, (uint16_t*)workspace, st);
   launch_mx4_matmul(w, n, k, (const uint16_t*)(pack ? workspace : x), pack ? 0 : x_stride, loose, rows, out, out_type, out_stride,
                     num_cus(), room && need > packed ? (float*)((char*)workspace + packed) : nullptr, st);

@@ -482,6 +482,14 @@ int launch(const Plan& p, const void* w, int n_blocks, const X& x, int rows, Epi
   return n_blocks;
 }
 
+// Threads of a plan's product along x.
+inline int64_t threads_of(const Plan& p, int n_blocks, int rows) {
+  if (p.tile < 0) return ((int64_t)n_blocks + p.fb - 1) / p.fb * 64 * kStreamWaves;
+  const Tile4& q = kTiles4[p.tile];
+  const int64_t tiles = ((int64_t)n_blocks + q.bn() - 1) / q.bn() * ((rows + 16 * q.tb - 1) / (16 * q.tb)) * p.parts;
+  return (tiles + 7) / 8 * 8 * 64 * (q.nw + q.f);
+}
+
 inline X tiles_of(const uint16_t* x, int k, const Workspace& ws) { return {x, 0, k / 32, ws.m_rows - 1}; }
 
 }  // namespace mx4

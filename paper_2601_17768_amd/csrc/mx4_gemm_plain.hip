@@ -63,7 +63,18 @@ void matmul(const void* w, int n, const mx4::X& x, int rows, const PlainEpi<F32>
 
 constexpr int kMostParts = 8;
 
+mx4::Plan matmul_plan(int n, int k, int rows, bool loose, int num_cus, bool parts) {
+  const int n_blocks = (n + 15) / 16;
+  return loose ? mx4::stream_plan(n_blocks, k / 32, num_cus) : mx4::plan(n_blocks, (k + 31) / 32, rows, num_cus, parts ? kMostParts : 1);
+}
+
 }  // namespace
+
+bool mx4_matmul_fits(int n, int k, int rows, bool loose, int num_cus, bool parts) {
+  const mx4::Plan p = matmul_plan(n, k, rows, loose, num_cus, parts);
+  return mx4::threads_of(p, (n + 15) / 16, rows) <= 0xFFFFFFFFll &&
+         (p.parts == 1 || (int64_t)rows * ((n + 15) / 16 * 4) <= (int64_t)kMostGroups256 * 256);
+}
 
 size_t mx4_matmul_part_bytes(int n, int k, int rows, int num_cus) {
   const mx4::Plan p = mx4::plan((n + 15) / 16, (k + 31) / 32, rows, num_cus, kMostParts);
@@ -75,8 +86,7 @@ int mx4_loose_rows() { return mx4::kStreamRows; }
 void launch_mx4_matmul(const void* w, int n, int k, const uint16_t* x, int64_t x_stride, bool loose, int rows, void* out, int out_type,
                        int64_t out_stride, int num_cus, float* parts, hipStream_t st) {
   const mx4::X xs = loose ? mx4::X{x, x_stride, k / 32, rows - 1, k % 32} : mx4::X{x, x_stride, (k + 31) / 32, rows - 1};
-  const int n_blocks = (n + 15) / 16;
-  const mx4::Plan p = loose ? mx4::stream_plan(n_blocks, xs.k_tiles, num_cus) : mx4::plan(n_blocks, xs.k_tiles, rows, num_cus, parts ? kMostParts : 1);
+  const mx4::Plan p = matmul_plan(n, k, rows, loose, num_cus, parts != nullptr);
   if (out_type == LLM42_F32)
     matmul(w, n, xs, rows, PlainEpi<true>{out, out_stride, rows, n, (uintptr_t)out % 16 == 0 && out_stride % 4 == 0}, p, loose, parts, st);
   else
