@@ -26,17 +26,17 @@ __device__ inline int range_status(int64_t first, int64_t count, int max_count, 
   return __any(bad) ? LLM42_SEQ_BAD_BLOCK : LLM42_SEQ_OK;
 }
 
-// One wave per (block of 16 positions, kv head), four heads of a block to a workgroup; blockIdx.y: layer.  A record is its wave's alone, so
-// a partly covered one needs no atomics.  Long runs are bound by memory (4 x 1500 - 2048 tokens of 32 layers of 8 heads of 128, stored
+// One wave per (block of 16 positions, kv head), four heads of a block to a workgroup, the launch's first workgroup being `group0`;
+// blockIdx.y: layer.  A record is its wave's alone, so a partly covered one needs no atomics.  Long runs are bound by memory (4 x 1500 - 2048 tokens of 32 layers of 8 heads of 128, stored
 // and read back: 2.4 GB in 445 us, 5.4 TB/s), a single token by three loads that wait for each other (24 sequences 7 us).
 template <int HD>
 __global__ __launch_bounds__(256) void kv4_store_kernel(const uint16_t* __restrict__ kv, Table src, char* __restrict__ kv4, Table dst,
                                                         int n_kv_heads, const int32_t* __restrict__ first_,
                                                         const int32_t* __restrict__ count_, int max_count, int slots,
-                                                        int32_t* __restrict__ seq_status) {
-  const int hg = (n_kv_heads + 3) / 4, at_slot = blockIdx.x / hg;
+                                                        int32_t* __restrict__ seq_status, unsigned group0) {
+  const int hg = (n_kv_heads + 3) / 4, group = (int)(group0 + blockIdx.x), at_slot = group / hg;
   const int s = at_slot / slots, slot = at_slot % slots, layer = blockIdx.y;
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, h = (int)(blockIdx.x % hg) * 4 + wave;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, h = group % hg * 4 + wave;
   const int64_t first = first_[s], count = count_[s];
   const int block = (int)(first / LLM42_KV_BLOCK) + slot;
   // (asked for together with what the check reads)
@@ -58,12 +58,13 @@ template <int HD>
 __global__ __launch_bounds__(256) void kv4_read_kernel(const char* __restrict__ kv4, Table src, int n_kv_heads,
                                                        const int32_t* __restrict__ first_, const int32_t* __restrict__ count_,
                                                        int num_seqs, int max_count, int slots, uint16_t* __restrict__ out_k,
-                                                       uint16_t* __restrict__ out_v, int32_t* __restrict__ seq_status) {
+                                                       uint16_t* __restrict__ out_v, int32_t* __restrict__ seq_status,
+                                                       unsigned group0) {
   constexpr int KT = HD / 32, ROW = HD / 8, PER = 64 / ROW;       // 16-byte pieces of a row, rows that a wave stores at once
   __shared__ u32x4 rows[4][16 * (ROW + 1)];                       // (a piece between the rows: 16 rows start in different banks)
-  const int hg = (n_kv_heads + 3) / 4, at_slot = blockIdx.x / hg;
+  const int hg = (n_kv_heads + 3) / 4, group = (int)(group0 + blockIdx.x), at_slot = group / hg;
   const int s = at_slot / slots, slot = at_slot % slots, layer = blockIdx.y;
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, g = lane >> 4, l16 = lane & 15, h = (int)(blockIdx.x % hg) * 4 + wave;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, g = lane >> 4, l16 = lane & 15, h = group % hg * 4 + wave;
   const int64_t first = first_[s], count = count_[s];
   const int status = range_status(first, count, max_count, src, src, s, lane);
   if (seq_status && blockIdx.y == 0 && slot == 0 && h == 0 && lane == 0) seq_status[s] = status;
@@ -107,6 +108,13 @@ __global__ __launch_bounds__(256) void kv4_read_kernel(const char* __restrict__ 
 // Blocks that a run of max_count positions can touch, of those that a table names.
 int slots_of(int max_count, int width) { return (int)std::min<int64_t>(((int64_t)max_count + 14) / 16 + 1, width); }
 
+// As many launches as the workgroups need.
+template <class Go>
+void in_launches(const llm42_model* m, int num_seqs, int slots, const Go& go) {
+  const unsigned groups = (unsigned)(num_seqs * slots * ((m->cfg.n_kv_heads + 3) / 4));
+  for (unsigned at = 0; at < groups; at += kMostGroups256) go(dim3(std::min(groups - at, kMostGroups256), m->cfg.n_layers), at);
+}
+
 Table table_of(const llm42_kv_cache* c) { return {c->block_table, c->max_blocks_per_seq, c->num_blocks}; }
 
 }  // namespace
@@ -114,10 +122,11 @@ Table table_of(const llm42_kv_cache* c) { return {c->block_table, c->max_blocks_
 void launch_kv4_store(const llm42_model* m, const llm42_kv_cache* kv, const llm42_kv_cache* kv4, const int32_t* first,
                       const int32_t* count, int num_seqs, int max_count, int32_t* seq_status, hipStream_t st) {
   const int slots = slots_of(max_count, std::min(kv->max_blocks_per_seq, kv4->max_blocks_per_seq));
-  const dim3 grid((unsigned)(num_seqs * slots * ((m->cfg.n_kv_heads + 3) / 4)), m->cfg.n_layers);
   const auto go = [&](auto kernel) {
-    kernel<<<grid, 256, 0, st>>>((const uint16_t*)kv->kv_base, table_of(kv), (char*)kv4->kv_base, table_of(kv4), m->cfg.n_kv_heads,
-                                 first, count, max_count, slots, seq_status);
+    in_launches(m, num_seqs, slots, [&](dim3 grid, unsigned at) {
+      kernel<<<grid, 256, 0, st>>>((const uint16_t*)kv->kv_base, table_of(kv), (char*)kv4->kv_base, table_of(kv4), m->cfg.n_kv_heads,
+                                   first, count, max_count, slots, seq_status, at);
+    });
   };
   if (m->cfg.head_dim == 128) go(kv4_store_kernel<128>);
   else go(kv4_store_kernel<64>);
@@ -126,10 +135,11 @@ void launch_kv4_store(const llm42_model* m, const llm42_kv_cache* kv, const llm4
 void launch_kv4_read(const llm42_model* m, const llm42_kv_cache* kv4, const int32_t* first, const int32_t* count, int num_seqs,
                      int max_count, uint16_t* out_k, uint16_t* out_v, int32_t* seq_status, hipStream_t st) {
   const int slots = slots_of(max_count, kv4->max_blocks_per_seq);
-  const dim3 grid((unsigned)(num_seqs * slots * ((m->cfg.n_kv_heads + 3) / 4)), m->cfg.n_layers);
   const auto go = [&](auto kernel) {
-    kernel<<<grid, 256, 0, st>>>((const char*)kv4->kv_base, table_of(kv4), m->cfg.n_kv_heads, first, count, num_seqs, max_count, slots,
-                                 out_k, out_v, seq_status);
+    in_launches(m, num_seqs, slots, [&](dim3 grid, unsigned at) {
+      kernel<<<grid, 256, 0, st>>>((const char*)kv4->kv_base, table_of(kv4), m->cfg.n_kv_heads, first, count, num_seqs, max_count, slots,
+                                   out_k, out_v, seq_status, at);
+    });
   };
   if (m->cfg.head_dim == 128) go(kv4_read_kernel<128>);
   else go(kv4_read_kernel<64>);
