@@ -18,6 +18,8 @@ def _to_device(weights: Dict, device) -> Dict:
 
 
 class VerifierSession:
+    """A model on one device and the workspace that its calls share: eager calls follow each other, whatever their streams."""
+
     def __init__(self, shape, weights: Dict, max_position: int, device: str = "cuda:0"):
         if not torch.cuda.is_available():
             raise RuntimeError("the verifier needs a GPU; there is no CPU path")
@@ -33,6 +35,8 @@ class VerifierSession:
         self._ws = None
         self._ws_key = None
         self._ws_captured, self._ws_kept = False, []
+        self._index = torch.cuda.current_device()
+        self._ws_stream, self._ws_handle = None, None            # the last call's, and its handle
 
     def close(self):
         if self.model:
@@ -59,12 +63,23 @@ class VerifierSession:
         return self._room(B.llm42_workspace_bytes(self.model, num_seqs, window, max_context))
 
     def _room(self, need: int) -> torch.Tensor:
-        """The session's workspace, of `need` bytes or more.  One that a captured call uses is kept when it is outgrown: the graph still writes it."""
+        """The session's workspace, of `need` bytes or more.  One that a captured call uses is kept when it is outgrown: the graph still writes it.
+        Calls share it, so one on another stream than the last waits for that, and an outgrown one is free behind the work of every
+        stream that used it.  (What a graph does when it is replayed is not seen here: replays are ordered by their caller.)"""
+        capturing = torch.cuda.is_current_stream_capturing()
         if self._ws is None or self._ws.numel() < need:
             if self._ws_captured:
                 self._ws_kept.append(self._ws)
             self._ws, self._ws_captured = torch.empty(need, dtype=torch.uint8, device=self.device), False
-        self._ws_captured |= torch.cuda.is_current_stream_capturing()
+        self._ws_captured |= capturing
+        handle = torch._C._cuda_getCurrentRawStream(self._index)
+        if handle != self._ws_handle and not capturing:
+            stream = torch.cuda.current_stream(self._index)
+            if self._ws_stream is not None:
+                stream.wait_stream(self._ws_stream)
+            if not self._ws_captured:
+                self._ws.record_stream(stream)
+            self._ws_stream, self._ws_handle = stream, handle
         return self._ws
 
     def verify(self, kv: torch.Tensor, block_table: torch.Tensor, seq_lens: torch.Tensor,

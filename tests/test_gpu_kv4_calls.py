@@ -45,3 +45,43 @@ def test_store_and_read_of_more_workgroups_than_a_launch_takes(hd):
         got[:, at] = 5.0
         assert bool((got == 5.0).all())
     sess.close()
+
+
+def test_calls_of_a_session_on_two_streams_follow_each_other():
+    """They share its workspace.  A stream that is held back is used first, then another one: the second call ends behind the first, and a
+    workspace that the held-back stream still uses is not handed out when it is outgrown."""
+    sess = session(2, 4, 128, 1)
+    g = torch.Generator().manual_seed(1)
+    kv = torch.randn(tuple(sess.kv_cache(300).shape), generator=g).to(torch.bfloat16).to(DEV)
+    kv4, bt = sess.kv4_cache(300), torch.arange(300, dtype=torch.int32, device=DEV).view(1, 300)
+    sess.kv4_store(kv, kv4, bt, i32([0]), i32([4800]), 4800)
+    q = [torch.randn(1, w, 8, 128, generator=g).to(torch.bfloat16).to(DEV) for w in (1, 1, 40)]
+    lens, out = i32([4700]), [torch.zeros_like(x) for x in q]
+    want = [sess.kv4_attention(0, kv4, bt, x, lens) for x in q]
+    sess._ws, side = None, torch.cuda.Stream()
+    sess.kv4_attention(0, kv4, bt, q[0], lens, out=out[0])       # (in parts: the workspace is written)
+    first = sess._ws.data_ptr(), sess._ws.numel()
+    assert first[1] > 8 * 128 * 4 * 4
+    torch.cuda.synchronize()
+    ends = [torch.cuda.Event(), torch.cuda.Event()]
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(400_000_000)
+        sess.kv4_attention(0, kv4, bt, q[0], lens, out=out[0])
+        ends[0].record()
+    sess.kv4_attention(0, kv4, bt, q[1], lens, out=out[1])
+    ends[1].record()
+    ends[1].synchronize()
+    assert ends[0].query()
+    torch.cuda.synchronize()
+    assert torch.equal(out[0], want[0]) and torch.equal(out[1], want[1])
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(400_000_000)
+        sess.kv4_attention(0, kv4, bt, q[0], lens, out=out[0])
+        ends[0].record()
+        sess.kv4_attention(0, kv4, bt, q[2], lens, out=out[2])   # outgrows the workspace, which the default stream allocated
+    taken = [torch.empty(first[1], dtype=torch.uint8, device=DEV) for _ in range(4)]
+    pending = not ends[0].query()
+    assert sess._ws.data_ptr() != first[0] and pending and all(t.data_ptr() != first[0] for t in taken)
+    torch.cuda.synchronize()
+    assert torch.equal(out[0], want[0]) and torch.equal(out[2], want[2])
+    sess.close()
