@@ -100,7 +100,8 @@ llm42_status llm42_kv4_bytes(const llm42_model* model, int64_t num_blocks, size_
 
 /* K and V of positions first[s] .. first[s] + count[s] - 1 of every sequence, all layers, from the bf16 cache into the 4-bit
  * one.  Behind a verifier pass and its commit: first = the length before, count = the committed tokens; behind a prefill: 0 and
- * the length.  No other position is written; no two of a call's blocks of positions may lie in the same 4-bit block.
+ * the length.  No other position is written.  No two sequences of a call may have positions in the same 4-bit block, unless both cover all
+ * 16 of it from the same K and V (a shared prefix: they write the same bytes).
  * first[s] < 0, positions beyond a table's capacity, count[s] outside 0 .. max_count: LLM42_SEQ_BAD_LENGTH; a needed entry of either
  * table out of range: LLM42_SEQ_BAD_BLOCK; nothing of such a sequence is stored.  LLM42_EINVAL where num_seqs times the blocks that
  * max_count positions can touch, times a quarter of the kv heads, rounded up, exceeds 2^31 - 1. */

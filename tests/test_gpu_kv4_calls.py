@@ -5,7 +5,7 @@ import torch
 
 import mx4_reference as ref
 from helpers import wl
-from paper_2601_17768_amd import kv_layout
+from paper_2601_17768_amd import dvr, kv_layout
 from paper_2601_17768_amd.session import VerifierSession
 
 pytestmark = pytest.mark.gpu
@@ -84,4 +84,34 @@ def test_calls_of_a_session_on_two_streams_follow_each_other():
     assert sess._ws.data_ptr() != first[0] and pending and all(t.data_ptr() != first[0] for t in taken)
     torch.cuda.synchronize()
     assert torch.equal(out[0], want[0]) and torch.equal(out[2], want[2])
+    sess.close()
+
+
+def test_a_shared_prefix_is_stored_from_every_sequence_and_the_loop_runs_on_it():
+    """Three sequences whose tables begin with the same three blocks: the cache holds what one of them stores alone, and the loop releases the
+    verifier's stream."""
+    shape = wl.TINY
+    sess = VerifierSession(shape, wl.make_weights(shape, seed=42), max_position=512, device=DEV)
+    rng = wl.rng_for(7, 1)
+    common, tails = wl.random_tokens(rng, 48, shape.vocab), [wl.random_tokens(rng, n, shape.vocab) for n in (5, 22, 16)]
+    bt = torch.arange(36, dtype=torch.int32, device=DEV).view(3, 12)
+    bt[1:, :3] = bt[0, :3]
+
+    def state():
+        kv = sess.kv_cache(36)
+        sess.prefill(kv, bt[:1].contiguous(), [common], window=16)
+        first = sess.prefill(kv, bt, tails, window=16, cached=i32([48] * 3))
+        return kv, bt, i32([48 + len(t) for t in tails]), first
+
+    kv, _, lens, first = state()
+    kv4, alone = sess.kv4_cache(36), sess.kv4_cache(36)
+    for cache in (kv4, alone):
+        cache.fill_(255)
+    sess.kv4_store(kv, kv4, bt, i32([0] * 3), lens, 80)
+    sess.kv4_store(kv, alone, bt[:1].contiguous(), i32([0]), lens[:1].contiguous(), 80)
+    sess.kv4_store(kv, alone, bt, i32([48] * 3), lens - 48, 80)
+    assert torch.equal(kv4, alone)
+    want = dvr.generate_verifier_only(sess, *state(), 24)
+    got, _ = dvr.generate(sess, *state(), 24, 8, fast="mx4_cache")
+    assert torch.equal(got, want)
     sess.close()
