@@ -61,8 +61,10 @@ class Sampling(ctypes.Structure):
 
 
 def make_sampling(temperature: float, seed: int, request_ids: Optional[torch.Tensor] = None) -> Sampling:
-    """request_ids: int64 device tensor [num_seqs] or None (then the index in the call is the id)."""
-    return Sampling(float(temperature), int(seed) & ((1 << 64) - 1), _ptr(request_ids, torch.int64))
+    """request_ids: int64 device tensor [num_seqs] or None (then the index in the call is the id); the result keeps it."""
+    sampling = Sampling(float(temperature), int(seed) & ((1 << 64) - 1), _ptr(request_ids, torch.int64))
+    sampling.ids_tensor = request_ids                # (the struct holds a bare address)
+    return sampling
 
 
 class KVCache(ctypes.Structure):
