@@ -25,14 +25,10 @@ struct X {
                   : p + ((size_t)(row >> 4) * k_tiles * 64 + (lane >> 4) * 16 + (row & 15)) * 8;
   }
   __device__ int step() const { return stride ? 32 : 512; }
-  // the same as a wave-uniform address and a lane's byte offset
+  // where token block `block` begins: the wave-uniform part of an address; a block past the last one repeats it
   __device__ const uint16_t* block_base(int block) const {
     const int b = min(block, last_row >> 4);
     return p + (stride ? (int64_t)b * 16 * stride : (int64_t)b * k_tiles * 512);
-  }
-  __device__ uint32_t lane_offset(int block, int lane) const {
-    const int r = min(lane & 15, last_row - min(block, last_row >> 4) * 16);
-    return stride ? (uint32_t)r * (uint32_t)stride * 2u + (lane >> 4) * 16u : (uint32_t)((lane >> 4) * 16 + r) * 16u;
   }
 };
 
