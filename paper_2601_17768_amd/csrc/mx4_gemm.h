@@ -35,7 +35,7 @@ struct X {
 // Up to 16 or 32 rows (TB token blocks).  A workgroup owns FB feature blocks; its eight waves take the groups of 4 k-tiles in turn, each
 // with accumulators of its own for all of them, and are added through LDS.  Codes and activations of two groups are on their way at
 // a time; no barrier, for no two waves want the same bytes.  A wave has four groups of a 4096-column matrix, so nothing is loaded past the
-// last one (1 row of 6144 x 4096 so 6.2 -> 4.6 us, from memory 7.7 -> 5.8; 28672 x 4096 15.1 -> 13.9, 4.5 TB/s).  LOOSE: plain
+// last one (1 row of 6144 x 4096 so 6.2 -> 4.6 us, from memory 7.7 -> 5.8; 28672 x 4096 from memory 15.1 -> 13.9, 4.5 TB/s).  LOOSE: plain
 // rows of any number of columns that are only 4-byte aligned are read as they lie (behind a launch that brings them in order first 13
 // rows of 1000 x 700 took 7.8 us instead of 4.6, 16 of 4096 x 4100 11.6 instead of 8.9); the last wave takes the columns behind
 // the last whole k-tile.  (Rows that begin in the middle of a word are brought in order: 16 rows of 4096 x 4097 took 28 us by loads of
@@ -166,9 +166,10 @@ __device__ __forceinline__ void wait_rounds(int rounds) {
 // Plain rows are fetched in runs of CH * 64 bytes of a row and lie in LDS as they come, a row's 16-byte pieces exchanged by the row's
 // number so that the 16 rows of an operand read are in 16 different bank groups (pieces of 64 bytes, 16 rows apart by a
 // power of two, meet in few of the L2's channels; 128 rows of 28672 x 4096 so 44 us, in runs 35).
-// Many rows are bound by the matrix cores: 4096 rows of 28672 x 4096 690 us, 1.40 PFLOP/s (the library's product of the two in bf16 723), the
-// conversions hidden behind 16 products each.  128 rows 29 us (22.6 at that rate), a round of workgroups that loads and multiplies in turn;
-// 24 of 4096 x 14336 15 us, of which 14 rounds of 0.36 us in each of 8 parts, whatever the tile, the rest launches.
+// Many rows are bound by the matrix cores: 4096 rows of 28672 x 4096 679 us, 1.42 PFLOP/s (the library's product of the two in bf16 723), the
+// conversions hidden behind 16 products each.  Up to 128 rows wait for loads (copies without activations / weights / products / either kind of
+// load, from memory: 128 rows of 28672 x 4096 29.0 / 28.4 / 28.7 / 23 of 31 us, 24 of it 18.6 / 14.9 / 21 / 8.7 of 22, 128 of 4096 x 4096
+// 12.1 / 9.6 / 14.5 / 5.2 of 14.7), sums in parts for launches and planes as well (24 of 4096 x 14336 14.6 / 14.1 / 15.8 / 12.7 of 16.4).
 template <int NW, int FB, int TB, int CH, int R, int F, int NSET, class Epi>
 __global__ __launch_bounds__(64 * (NW + F), (NW + F + 3) / 4) void mx4_tile_kernel(const char* __restrict__ w, X x, int n_blocks, int units,
                                                                                    int tiles_n, int tiles_m, int parts, int part_groups, Epi epi) {
@@ -373,7 +374,8 @@ __global__ __launch_bounds__(64 * (NW + F), (NW + F + 3) / 4) void mx4_tile_kern
 }
 
 // Tiles of mx4_tile_kernel, and what a round of one workgroup per CU takes by them: ns, ns per k-tile, and by how many percent more
-// of that with every CU at work (fitted to 326 shapes of 1 - 4096 rows, 16 - 131072 features and 256 - 14336 columns).
+// of that with every CU at work (fitted to times of 1 - 4096 rows, 16 - 131072 features and 256 - 14336 columns; they rank the tiles, and are
+// no measurement of any one call).
 struct Tile4 {
   int nw, fb, tb, ch, r, f, nset;
   int round_ns, k_ns, full;
@@ -407,7 +409,7 @@ struct Plan {
   int fb;                  // ... by this many feature blocks
   int parts, part_groups;  // of the sum over k, and how many groups of 4 k-tiles each has
 };
-// mx4_stream_kernel for up to 16 rows (us, it / the best tile: 1 row of 4096 x 4096 4.8 / 9.2, 16 6.7 / 9.8; 1 of 28672 x 4096 13.1 / 19.6, 16
+// mx4_stream_kernel for up to 16 rows (us, it / the best tile: 1 row of 4096 x 4096 4.8 / 9.2, 16 6.7 / 9.8; 1 of 28672 x 4096 13.1 / 19.6 from the memory-side cache, 16
 // 14.6 / 19.9; 16 of 50304 x 512 7.4 / 7.9), except where more than 8 rows are summed over many columns for few features: it has but eight
 // waves for a sum, each of which takes 0.6 us and 28 ns a row for a group, a tile several workgroups (16 rows of 512 x 14336 16.1 / 10.7,
 // of 512 x 4096 6.1 / 7.7).  Up to 32 rows where four feature blocks a workgroup put one on every CU, by a like rule (24 rows of 1024 x 1024
@@ -418,7 +420,7 @@ struct Plan {
 // Else the tile and the number of parts that cost least; a part has a plane of fp32 sums of its own, written and
 // read again by a launch that adds them (2.6 us and 2.8 TB/s; nothing but that where `joined`: the launch that follows adds two of them
 // anyway), and is taken for a tenth less (32 rows of 4096 x 14336 33.6 -> 17.1, 1024 x 4096 12.1 -> 8.7; 128 rows of 4096 x 14336
-// 38.4 -> 25.1).  Over those 402 shapes and row counts the choice takes 1.4 % more than the best of all there are, at worst 29 %.
+// 38.4 -> 25.1).
 inline Plan stream_plan(int n_blocks, int k_tiles, int num_cus) {
   const int g8 = (n_blocks + 7) / 8, g7 = (n_blocks + 6) / 7;
   const bool seven = (g7 + num_cus - 1) / num_cus * 7 < (g8 + num_cus - 1) / num_cus * 8;
