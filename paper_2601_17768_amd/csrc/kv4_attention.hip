@@ -65,8 +65,10 @@ __device__ __forceinline__ float row_sum(float v) {
 // part's steps of 64 keys in turn, each with a maximum and sum of its own, and are joined through LDS.
 //   scores: D[key][row] = K Q, K converted with its scales (exact in bf16);
 //   weights: p = exp2((s - ref) / sqrt(head_dim) log2 e) in fp32; ref moves to a step's maximum when that exceeds it by more than 8, so
-//   that most steps rescale nothing and p stays below 2^8; rounded to bf16 (2^-8 of a weight: what the matrix instruction takes), their sum
-//   is taken before that.  D's layout is that of the P V operand: no exchange between lanes;
+//   that most steps rescale nothing and p stays below 2^8; rounded to bf16 (2^-8 of a weight: what the matrix instruction takes, and what the
+//   bf16 attention does), their sum is taken before that.  Outputs are off by up to 0.0023 of their size so, 0.0017 by their own rounding;
+//   a second operand with what the first lacks is exact to 2^-17, for twice the P V products (us without / with: 1 x 512 7.0 / 7.4,
+//   24 x 4000 25.5 / 28, 128 x 4000 103 / 111, 4 windows of 64 x 4000 34 / 40).  D's layout is that of the P V operand: no exchange between lanes;
 //   output: D[feature][row] = V P.  An operand holds 8 keys of one feature, and a scale belongs to 32 features of one key: two neighbouring
 //   features of a key are converted together, with its scale, and the halves of 8 keys gathered into the operands of the one and
 //   the other feature.  Where a row does not see all keys of the step, the scales go into its weights instead (the same products): V that a row must not
