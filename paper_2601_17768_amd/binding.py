@@ -1,4 +1,4 @@
-"""ctypes binding of the verifier library (include/llm42.h, include/llm42_mx4.h).
+"""ctypes binding of the verifier library (include/llm42.h, include/llm42_mx4.h, include/llm42_paged.h).
 
 Argument marshalling only: every function here has the name and meaning of the
 C entry point it wraps, takes torch tensors where the C call takes device
@@ -24,6 +24,9 @@ LLM42_MAX_WINDOW = 512
 LLM42_MAX_ROWS = 65536
 LLM42_STATIC_SCRATCH_BYTES = 64 << 20
 LLM42_BF16, LLM42_F32 = 0, 1
+LLM42_ROPE_HALF, LLM42_ROPE_INTERLEAVED = 0, 1
+LLM42_ROPE_NONE, LLM42_ROPE_LINEAR, LLM42_ROPE_LLAMA3, LLM42_ROPE_YARN = 0, 1, 2, 3
+LLM42_MAX_SELECTED = 4096
 LLM42_SEQ_OK, LLM42_SEQ_BAD_LENGTH, LLM42_SEQ_BAD_BLOCK, LLM42_SEQ_BAD_TOKEN = 0, 1, 2, 4
 
 EXPORTS = ("llm42_model_create", "llm42_model_destroy", "llm42_kv_bytes", "llm42_workspace_bytes",
@@ -32,7 +35,10 @@ EXPORTS = ("llm42_model_create", "llm42_model_destroy", "llm42_kv_bytes", "llm42
            "llm42_decode_step_sampled", "llm42_prefill", "llm42_prefill_workspace_bytes",
            "llm42_mx4_bytes", "llm42_mx4_quantize", "llm42_mx4_dequantize", "llm42_mx4_matmul_workspace_bytes", "llm42_mx4_matmul",
            "llm42_kv4_bytes", "llm42_kv4_store", "llm42_kv4_read", "llm42_kv4_attention_workspace_bytes", "llm42_kv4_attention",
-           "llm42_mx4_model_create", "llm42_mx4_model_destroy", "llm42_decode_step_mx4_workspace_bytes", "llm42_decode_step_mx4")
+           "llm42_mx4_model_create", "llm42_mx4_model_destroy", "llm42_decode_step_mx4_workspace_bytes", "llm42_decode_step_mx4",
+           "llm42_heads_kv_bytes", "llm42_rope_create", "llm42_rope_destroy", "llm42_kv_append", "llm42_kv_bounds_bytes", "llm42_kv_bounds_store",
+           "llm42_kv_bounds_read", "llm42_kv_select_workspace_bytes", "llm42_kv_select", "llm42_kv_sparse_attention_workspace_bytes",
+           "llm42_kv_sparse_attention")
 KERNEL_CLASSES = ("prepare", "embed", "rmsnorm", "qkv", "attention", "o_proj", "gate_up", "down", "lm_head",
                   "argmax", "commit")
 
@@ -70,6 +76,16 @@ def make_sampling(temperature: float, seed: int, request_ids: Optional[torch.Ten
 class KVCache(ctypes.Structure):
     _fields_ = [("kv_base", ctypes.c_void_p), ("num_blocks", ctypes.c_int64), ("block_table", ctypes.c_void_p),
                 ("max_blocks_per_seq", ctypes.c_int32)]
+
+
+class Heads(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_layers", "n_q_heads", "n_kv_heads", "head_dim")]
+
+
+class RopeConfig(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("rot_dim", "layout", "scaling", "max_position", "original_max_position")] + \
+               [(n, ctypes.c_double) for n in ("theta", "factor", "low_freq_factor", "high_freq_factor", "beta_fast", "beta_slow",
+                                               "attention_factor")]
 
 
 _lib = None
@@ -137,6 +153,22 @@ def load_library(path: Optional[str] = None):
             "llm42_decode_step_mx4": [vp, kvp, kvp, vp, vp, i32, i32, vp, vp, vp, size, vp, ctypes.POINTER(Sampling)]}.items():
         getattr(lib, name).argtypes = args
         getattr(lib, name).restype = i32
+    hp, f32 = ctypes.POINTER(Heads), ctypes.c_float
+    for name, args in {
+            "llm42_heads_kv_bytes": [hp, i64, size_p],
+            "llm42_rope_create": [ctypes.POINTER(RopeConfig), ctypes.POINTER(vp)],
+            "llm42_kv_append": [hp, i32, kvp, vp, vp, i64, vp, i64, vp, i64, i32, vp, vp, f32, vp, vp, i32, vp, i32, i32, vp, i64, vp, vp],
+            "llm42_kv_bounds_bytes": [hp, i64, size_p],
+            "llm42_kv_bounds_store": [hp, i32, kvp, vp, vp, vp, i32, i32, vp, vp],
+            "llm42_kv_bounds_read": [hp, vp, i64, vp, i32, vp, vp, vp],
+            "llm42_kv_select_workspace_bytes": [hp, i32, i32, i32, i32, size_p],
+            "llm42_kv_select": [hp, i32, kvp, vp, vp, i64, vp, i32, vp, i32, i32, i32, i32, i32, vp, vp, vp, size, vp],
+            "llm42_kv_sparse_attention_workspace_bytes": [hp, i32, i32, i32, size_p],
+            "llm42_kv_sparse_attention": [hp, i32, kvp, vp, i64, vp, i32, vp, i32, i32, vp, i32, f32, vp, i64, vp, vp, size, vp]}.items():
+        getattr(lib, name).argtypes = args
+        getattr(lib, name).restype = i32
+    lib.llm42_rope_destroy.argtypes = [vp]
+    lib.llm42_rope_destroy.restype = None
     lib.llm42_mx4_model_destroy.argtypes = [vp]
     lib.llm42_mx4_model_destroy.restype = None
     lib.llm42_last_error.argtypes = []
@@ -500,6 +532,164 @@ def llm42_decode_step_mx4(model: int, mx4: int, kv_base: torch.Tensor, num_block
                                                 _per_seq(seq_status, num_seqs), _ptr(workspace),
                                                 workspace.numel() * workspace.element_size(), _stream_handle(stream),
                                                 ctypes.byref(sampling) if sampling is not None else None))
+
+
+def _head_rows(t: torch.Tensor, num_seqs: int, window: int, heads: int, head_dim: int):
+    """(pointer, type, stride) of rows [num_seqs, window, heads, head_dim] at one distance from each other, their heads side by side."""
+    if t.shape != (num_seqs, window, heads, head_dim):
+        raise ValueError(f"expected [{num_seqs}, {window}, {heads}, {head_dim}], got {list(t.shape)}")
+    kind = _TYPES.get(t.dtype)
+    if kind is None:
+        raise ValueError(f"expected bfloat16 or float32, got {t.dtype}")
+    of_seq, of_row, of_head, near = t.stride()
+    row = of_row if window > 1 else of_seq if num_seqs > 1 else heads * head_dim
+    if near != 1 or (heads > 1 and of_head != head_dim) or (num_seqs > 1 and window > 1 and of_seq != window * row):
+        raise ValueError("rows (sequence, token) must lie at one distance from each other, their heads side by side")
+    return t.data_ptr(), kind, row
+
+
+def _paged_view(heads: Heads, kv: Optional[torch.Tensor], num_blocks: int, block_table: torch.Tensor, num_seqs: int) -> KVCache:
+    if block_table.dim() != 2 or block_table.shape[0] != num_seqs:
+        raise ValueError("block_table must be [num_seqs, max_blocks_per_seq]")
+    if kv is not None and kv.numel() * kv.element_size() < llm42_heads_kv_bytes(heads, num_blocks):
+        raise ValueError(f"kv holds {kv.numel() * kv.element_size()} bytes, {num_blocks} blocks need {llm42_heads_kv_bytes(heads, num_blocks)}")
+    return KVCache(_ptr(kv), num_blocks, _ptr(block_table, torch.int32), block_table.shape[1])
+
+
+def _bounds(heads: Heads, bounds: torch.Tensor, num_blocks: int) -> int:
+    if bounds.dtype != torch.uint8:
+        raise ValueError(f"bounds are a uint8 tensor, got {bounds.dtype}")
+    if bounds.numel() < llm42_kv_bounds_bytes(heads, num_blocks):
+        raise ValueError(f"bounds hold {bounds.numel()} bytes, {num_blocks} blocks need {llm42_kv_bounds_bytes(heads, num_blocks)}")
+    return _ptr(bounds)
+
+
+def _workspace(t: Optional[torch.Tensor]):
+    return _ptr(t), 0 if t is None else t.numel() * t.element_size()
+
+
+def _lists(t: torch.Tensor, num_seqs: int, window: int, kv_heads: int) -> int:
+    if t.dim() != 4 or tuple(t.shape[:3]) != (num_seqs, window, kv_heads):
+        raise ValueError(f"lists of blocks must be [{num_seqs}, {window}, {kv_heads}, entries], got {list(t.shape)}")
+    return _ptr(t, torch.int32)
+
+
+def _asked(call, *args) -> int:
+    out = ctypes.c_size_t()
+    _check(call(*args, ctypes.byref(out)))
+    return out.value
+
+
+def llm42_heads_kv_bytes(heads: Heads, num_blocks: int) -> int:
+    return _asked(load_library().llm42_heads_kv_bytes, ctypes.byref(heads), num_blocks)
+
+
+def llm42_kv_bounds_bytes(heads: Heads, num_blocks: int) -> int:
+    return _asked(load_library().llm42_kv_bounds_bytes, ctypes.byref(heads), num_blocks)
+
+
+def llm42_rope_create(cfg: RopeConfig) -> int:
+    handle = ctypes.c_void_p()
+    _check(load_library().llm42_rope_create(ctypes.byref(cfg), ctypes.byref(handle)))
+    return handle.value
+
+
+def llm42_rope_destroy(rope: int) -> None:
+    load_library().llm42_rope_destroy(rope)
+
+
+def llm42_kv_append(heads: Heads, layer: int, kv: torch.Tensor, num_blocks: int, block_table: torch.Tensor, bounds: Optional[torch.Tensor],
+                    q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, q_norm: Optional[torch.Tensor], k_norm: Optional[torch.Tensor],
+                    norm_eps: float, rope: Optional[int], seq_lens: torch.Tensor, n_valid: Optional[torch.Tensor], max_context: int,
+                    q_out: Optional[torch.Tensor], seq_status: Optional[torch.Tensor] = None, stream=None) -> None:
+    """k, v [num_seqs, window, n_kv_heads, head_dim] and q [num_seqs, window, n_q_heads, head_dim]: bfloat16 or float32, all the same; q_out bfloat16.
+    rope: a handle of llm42_rope_create."""
+    num_seqs = seq_lens.numel()
+    _on_current_device(kv, block_table, bounds, q, k, v, q_norm, k_norm, seq_lens, n_valid, q_out, seq_status)
+    if k.dim() != 4:
+        raise ValueError("k must be [num_seqs, window, n_kv_heads, head_dim]")
+    window, hd = k.shape[1], heads.head_dim
+    kp, kind, ks = _head_rows(k, num_seqs, window, heads.n_kv_heads, hd)
+    vp, v_kind, vs = _head_rows(v, num_seqs, window, heads.n_kv_heads, hd)
+    qp, q_kind, qs = (None, kind, 0) if q is None else _head_rows(q, num_seqs, window, heads.n_q_heads, hd)
+    op, o_kind, os_ = (None, LLM42_BF16, 0) if q_out is None else _head_rows(q_out, num_seqs, window, heads.n_q_heads, hd)
+    if kind != v_kind or kind != q_kind or o_kind != LLM42_BF16:
+        raise ValueError("q, k and v must be of one type, q_out bfloat16")
+    for t in (q_norm, k_norm):
+        if t is not None and t.numel() != hd:
+            raise ValueError(f"gains hold {hd} values")
+    view = _paged_view(heads, kv, num_blocks, block_table, num_seqs)
+    _check(load_library().llm42_kv_append(
+        ctypes.byref(heads), layer, ctypes.byref(view), None if bounds is None else _bounds(heads, bounds, num_blocks), qp, qs, kp, ks, vp, vs, kind,
+        _ptr(q_norm, torch.bfloat16), _ptr(k_norm, torch.bfloat16), norm_eps, rope, _per_seq(seq_lens, num_seqs), window,
+        _per_seq(n_valid, num_seqs), num_seqs, max_context, op, os_, _per_seq(seq_status, num_seqs), _stream_handle(stream)))
+
+
+def llm42_kv_bounds_store(heads: Heads, layer: int, kv: torch.Tensor, num_blocks: int, block_table: torch.Tensor, bounds: torch.Tensor,
+                          first: torch.Tensor, count: torch.Tensor, max_count: int, seq_status: Optional[torch.Tensor] = None, stream=None) -> None:
+    """layer -1: all."""
+    num_seqs = first.numel()
+    _on_current_device(kv, block_table, bounds, first, count, seq_status)
+    view = _paged_view(heads, kv, num_blocks, block_table, num_seqs)
+    _check(load_library().llm42_kv_bounds_store(ctypes.byref(heads), layer, ctypes.byref(view), _bounds(heads, bounds, num_blocks),
+                                                _per_seq(first, num_seqs), _per_seq(count, num_seqs), num_seqs, max_count,
+                                                _per_seq(seq_status, num_seqs), _stream_handle(stream)))
+
+
+def llm42_kv_bounds_read(heads: Heads, bounds: torch.Tensor, num_blocks: int, block_ids: torch.Tensor, out_lo: torch.Tensor,
+                         out_hi: torch.Tensor, stream=None) -> None:
+    """out_lo, out_hi: bfloat16 [n_layers, len(block_ids), n_kv_heads, head_dim]."""
+    _on_current_device(bounds, block_ids, out_lo, out_hi)
+    shape = (heads.n_layers, block_ids.numel(), heads.n_kv_heads, heads.head_dim)
+    if out_lo.shape != shape or out_hi.shape != shape:
+        raise ValueError(f"out_lo and out_hi must be {list(shape)}")
+    _check(load_library().llm42_kv_bounds_read(ctypes.byref(heads), _bounds(heads, bounds, num_blocks), num_blocks, _ptr(block_ids, torch.int32),
+                                               block_ids.numel(), _ptr(out_lo, torch.bfloat16), _ptr(out_hi, torch.bfloat16),
+                                               _stream_handle(stream)))
+
+
+def llm42_kv_select_workspace_bytes(heads: Heads, num_seqs: int, window: int, max_context: int, budget: int) -> int:
+    return _asked(load_library().llm42_kv_select_workspace_bytes, ctypes.byref(heads), num_seqs, window, max_context, budget)
+
+
+def llm42_kv_select(heads: Heads, layer: int, num_blocks: int, block_table: torch.Tensor, bounds: torch.Tensor, q: torch.Tensor,
+                    seq_lens: torch.Tensor, n_valid: Optional[torch.Tensor], max_context: int, sink: int, recent: int, selected: torch.Tensor,
+                    workspace: Optional[torch.Tensor], seq_status: Optional[torch.Tensor] = None, stream=None) -> None:
+    """selected: int32 [num_seqs, window, n_kv_heads, budget]."""
+    num_seqs = seq_lens.numel()
+    _on_current_device(block_table, bounds, q, seq_lens, n_valid, selected, workspace, seq_status)
+    if q.dim() != 4 or q.dtype != torch.bfloat16:
+        raise ValueError("q must be bfloat16 [num_seqs, window, n_q_heads, head_dim]")
+    window = q.shape[1]
+    qp, _, qs = _head_rows(q, num_seqs, window, heads.n_q_heads, heads.head_dim)
+    view = _paged_view(heads, None, num_blocks, block_table, num_seqs)
+    _check(load_library().llm42_kv_select(
+        ctypes.byref(heads), layer, ctypes.byref(view), _bounds(heads, bounds, num_blocks), qp, qs, _per_seq(seq_lens, num_seqs), window,
+        _per_seq(n_valid, num_seqs), num_seqs, max_context, selected.shape[-1], sink, recent,
+        _lists(selected, num_seqs, window, heads.n_kv_heads), _per_seq(seq_status, num_seqs), *_workspace(workspace), _stream_handle(stream)))
+
+
+def llm42_kv_sparse_attention_workspace_bytes(heads: Heads, num_seqs: int, window: int, width: int) -> int:
+    return _asked(load_library().llm42_kv_sparse_attention_workspace_bytes, ctypes.byref(heads), num_seqs, window, width)
+
+
+def llm42_kv_sparse_attention(heads: Heads, layer: int, kv: torch.Tensor, num_blocks: int, block_table: torch.Tensor, q: torch.Tensor,
+                              seq_lens: torch.Tensor, n_valid: Optional[torch.Tensor], max_context: int, selected: torch.Tensor, scale: float,
+                              out: torch.Tensor, workspace: Optional[torch.Tensor], seq_status: Optional[torch.Tensor] = None,
+                              stream=None) -> None:
+    """q, out: bfloat16 [num_seqs, window, n_q_heads, head_dim]; selected: int32 [num_seqs, window, n_kv_heads, width]; scale 0: 1 / sqrt(head_dim)."""
+    num_seqs = seq_lens.numel()
+    _on_current_device(kv, block_table, q, seq_lens, n_valid, selected, out, workspace, seq_status)
+    if q.dim() != 4 or q.dtype != torch.bfloat16 or out.dtype != torch.bfloat16:
+        raise ValueError("q and out must be bfloat16 [num_seqs, window, n_q_heads, head_dim]")
+    window = q.shape[1]
+    qp, _, qs = _head_rows(q, num_seqs, window, heads.n_q_heads, heads.head_dim)
+    op, _, os_ = _head_rows(out, num_seqs, window, heads.n_q_heads, heads.head_dim)
+    view = _paged_view(heads, kv, num_blocks, block_table, num_seqs)
+    _check(load_library().llm42_kv_sparse_attention(
+        ctypes.byref(heads), layer, ctypes.byref(view), qp, qs, _per_seq(seq_lens, num_seqs), window, _per_seq(n_valid, num_seqs), num_seqs,
+        max_context, _lists(selected, num_seqs, window, heads.n_kv_heads), selected.shape[-1], scale, op, os_, _per_seq(seq_status, num_seqs),
+        *_workspace(workspace), _stream_handle(stream)))
 
 
 def llm42_commit_rollback(candidates: torch.Tensor, out_tokens: torch.Tensor, n_valid: Optional[torch.Tensor],

@@ -32,6 +32,7 @@ FLAGS = [
 FILE_FLAGS = {
     "attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     "kv4_attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+    "kv_sparse.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
 }
 
 

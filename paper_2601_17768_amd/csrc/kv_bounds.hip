@@ -1,0 +1,98 @@
+// Bounds of the cached keys: from the bf16 cache, and what they stand for.
+#include <algorithm>
+
+#include "paged.h"
+
+using namespace paged;
+
+namespace {
+
+// One wave per (block of 16 positions, kv head), four to a workgroup; blockIdx.y: layer.
+template <int HD>
+__global__ __launch_bounds__(256) void bounds_store_kernel(const uint16_t* __restrict__ k_plane, int64_t layer_stride, char* __restrict__ bounds,
+                                                           const int32_t* __restrict__ table, int width, int64_t num_blocks, int n_kv_heads,
+                                                           const int32_t* __restrict__ first_, const int32_t* __restrict__ count_, int num_seqs,
+                                                           int max_count, int slots, int32_t* __restrict__ seq_status) {
+  constexpr int LANES = HD / 8, N = HD / 32;
+  const int lane = threadIdx.x & 63;
+  const int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int h = (int)(item % n_kv_heads), slot = (int)(item / n_kv_heads % slots), s = (int)(item / n_kv_heads / slots), layer = blockIdx.y;
+  if (s >= num_seqs) return;
+  const int64_t first = first_[s], count = count_[s];
+  int status = LLM42_SEQ_OK;
+  const int begin = (int)(first / LLM42_KV_BLOCK), end = (int)min((first + count) / LLM42_KV_BLOCK, (int64_t)width);   // whole blocks end here
+  if (first < 0 || count < 0 || count > max_count || first + count > (int64_t)width * LLM42_KV_BLOCK) {
+    status = LLM42_SEQ_BAD_LENGTH;
+  } else if (count > 0) {
+    bool bad = false;
+    for (int b = begin + lane; b < end; b += 64) {
+      const int id = table[(size_t)s * width + b];
+      bad |= id < 0 || id >= num_blocks;
+    }
+    if (__any(bad)) status = LLM42_SEQ_BAD_BLOCK;
+  }
+  if (seq_status && layer == 0 && slot == 0 && h == 0 && lane == 0) seq_status[s] = status;
+  const int block = begin + slot;
+  if (status != LLM42_SEQ_OK || count == 0 || block >= end) return;
+  const size_t at = (size_t)table[(size_t)s * width + block] * n_kv_heads + h;
+  const uint16_t* tile = k_plane + layer * layer_stride + at * 16 * HD;
+  u32x4 key[N];
+  const int c = lane % LANES, t0 = lane / LANES;
+#pragma unroll
+  for (int i = 0; i < N; ++i) key[i] = *(const u32x4*)(tile + (c * 16 + t0 + i * (64 / LANES)) * 8);
+  write_bounds<HD>(key, bounds + ((size_t)layer * num_blocks * n_kv_heads + at) * bounds_record(HD), lane);
+}
+
+// A thread per 8 features of a (block, kv head); blockIdx.y: layer.
+template <int HD>
+__global__ __launch_bounds__(256) void bounds_read_kernel(const char* __restrict__ bounds, int64_t num_blocks, int n_kv_heads,
+                                                          const int32_t* __restrict__ ids, int num_ids, uint16_t* __restrict__ out_lo,
+                                                          uint16_t* __restrict__ out_hi) {
+  constexpr int LANES = HD / 8;
+  const int64_t item = (int64_t)blockIdx.x * 256 + threadIdx.x, head = item / LANES;
+  const int c = (int)(item % LANES), h = (int)(head % n_kv_heads);
+  const int64_t j = head / n_kv_heads;
+  if (j >= num_ids) return;
+  const int id = ids[j];
+  if (id < 0 || id >= num_blocks) return;
+  const char* rec = bounds + (((size_t)blockIdx.y * num_blocks + id) * n_kv_heads + h) * bounds_record(HD);
+  const int e = *(const uint8_t*)(rec + 2 * HD);
+  const bool none = e == kBoundsNone;
+  const float unit = none ? 0.f : power_of_two(e - kBoundsBias);
+  const size_t at = (((size_t)blockIdx.y * num_ids + j) * n_kv_heads + h) * HD + c * 8;
+#pragma unroll
+  for (int part = 0; part < 2; ++part) {
+    const u32x2 w = *(const u32x2*)(rec + part * HD + c * 8);
+    const float inf = part ? -INFINITY : INFINITY;
+    float x[8];
+#pragma unroll
+    for (int f = 0; f < 8; ++f) x[f] = none ? inf : (float)(int8_t)(w[f >> 2] >> (8 * (f & 3))) * unit;
+    u32x4 o;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = pack2_bf16(x[2 * i], x[2 * i + 1]);
+    *(u32x4*)((part ? out_lo : out_hi) + at) = o;
+  }
+}
+
+}  // namespace
+
+void launch_bounds_store(int n_layers, int n_kv_heads, int head_dim, const uint16_t* k_plane, int64_t layer_stride, char* bounds,
+                         const int32_t* block_table, int width, int64_t num_blocks, const int32_t* first, const int32_t* count, int num_seqs,
+                         int max_count, int32_t* seq_status, hipStream_t st) {
+  const int slots = slots_of(max_count, width);
+  const dim3 grid((unsigned)(((int64_t)num_seqs * slots * n_kv_heads + 3) / 4), n_layers);
+  const auto go = [&](auto kernel) {
+    kernel<<<grid, 256, 0, st>>>(k_plane, layer_stride, bounds, block_table, width, num_blocks, n_kv_heads, first, count, num_seqs, max_count,
+                                 slots, seq_status);
+  };
+  if (head_dim == 128) go(bounds_store_kernel<128>);
+  else go(bounds_store_kernel<64>);
+}
+
+void launch_bounds_read(int n_layers, int n_kv_heads, int head_dim, const char* bounds, int64_t num_blocks, const int32_t* ids, int num_ids,
+                        uint16_t* out_lo, uint16_t* out_hi, hipStream_t st) {
+  const dim3 grid((unsigned)(((int64_t)num_ids * n_kv_heads * (head_dim / 8) + 255) / 256), n_layers);
+  const auto go = [&](auto kernel) { kernel<<<grid, 256, 0, st>>>(bounds, num_blocks, n_kv_heads, ids, num_ids, out_lo, out_hi); };
+  if (head_dim == 128) go(bounds_read_kernel<128>);
+  else go(bounds_read_kernel<64>);
+}

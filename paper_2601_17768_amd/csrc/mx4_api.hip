@@ -8,18 +8,6 @@ namespace {
 
 inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
-// Compute units of the current device (asked for once per device).
-int num_cus() {
-  constexpr int kMax = 64;
-  static std::atomic<int> known[kMax];
-  int dev = 0, cus = 0;
-  if (hipGetDevice(&dev) != hipSuccess || dev < 0) return 256;
-  if (dev < kMax && (cus = known[dev].load(std::memory_order_relaxed)) > 0) return cus;
-  if (hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || cus < 1) cus = 256;
-  if (dev < kMax) known[dev].store(cus, std::memory_order_relaxed);
-  return cus;
-}
-
 // Largest matrix: index arithmetic in 32 bits stays in range below it.
 constexpr int32_t kMostRows = 1 << 30, kMostCols = 1 << 26;
 
@@ -97,6 +85,18 @@ llm42_status check_attention(const char* who, const llm42_model* m, int32_t num_
 
 }  // namespace
 
+// Compute units of the current device (asked for once per device).
+int current_cus() {
+  constexpr int kMax = 64;
+  static std::atomic<int> known[kMax];
+  int dev = 0, cus = 0;
+  if (hipGetDevice(&dev) != hipSuccess || dev < 0) return 256;
+  if (dev < kMax && (cus = known[dev].load(std::memory_order_relaxed)) > 0) return cus;
+  if (hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || cus < 1) cus = 256;
+  if (dev < kMax) known[dev].store(cus, std::memory_order_relaxed);
+  return cus;
+}
+
 extern "C" {
 
 llm42_status llm42_mx4_bytes(int32_t rows, int32_t cols, size_t* out_bytes) {
@@ -125,7 +125,7 @@ llm42_status llm42_mx4_matmul_workspace_bytes(int32_t rows, int32_t n, int32_t k
   if (!out_bytes) return fail(LLM42_EINVAL, "mx4_matmul_workspace_bytes: null argument");
   if (rows < 1 || rows > LLM42_MAX_ROWS || n < 1 || k < 1 || n > kMostRows || k > kMostCols)
     return fail(LLM42_EINVAL, "mx4_matmul_workspace_bytes: sizes out of range");
-  *out_bytes = packed_x_bytes(rows, k) + mx4_matmul_part_bytes(n, k, rows, num_cus());
+  *out_bytes = packed_x_bytes(rows, k) + mx4_matmul_part_bytes(n, k, rows, current_cus());
   return LLM42_OK;
 }
 
@@ -139,7 +139,7 @@ llm42_status llm42_mx4_matmul(const void* w, size_t w_bytes, int32_t n, int32_t 
   if (x_stride < k) return fail(LLM42_EINVAL, "%s: x_stride %lld is less than k", who, (long long)x_stride);
   if ((uintptr_t)x % 2) return fail(LLM42_EINVAL, "%s: x not aligned to its type", who);
   hipStream_t st = (hipStream_t)hip_stream;
-  const size_t packed = packed_x_bytes(rows, k), need = packed + mx4_matmul_part_bytes(n, k, rows, num_cus());
+  const size_t packed = packed_x_bytes(rows, k), need = packed + mx4_matmul_part_bytes(n, k, rows, current_cus());
   const bool plain = k % 32 == 0 && (uintptr_t)x % 16 == 0 && (rows == 1 || (x_stride % 8 == 0 && x_stride <= (1 << 26)));
   const bool loose = !plain && rows <= mx4_loose_rows() && (uintptr_t)x % 4 == 0 && (rows == 1 || x_stride % 2 == 0), pack = !plain && !loose;
   const bool room = workspace && (uintptr_t)workspace % 256 == 0 && workspace_bytes >= need;
@@ -150,11 +150,11 @@ llm42_status llm42_mx4_matmul(const void* w, size_t w_bytes, int32_t n, int32_t 
   if (pack && align_up(rows, 16) * align_up(k, 32) / 8 > (size_t)kMostGroups256 * 256)
     return fail(LLM42_EINVAL, "%s: rows * k too large for rows that are not aligned", who);
   // (up to 2^28 values any tile's workgroups, at most eight parts of 384 threads for 64 x 32 of them, are within a launch)
-  if ((int64_t)rows * n > (1 << 28) && !mx4_matmul_fits(n, k, rows, loose, num_cus(), room && need > packed))
+  if ((int64_t)rows * n > (1 << 28) && !mx4_matmul_fits(n, k, rows, loose, current_cus(), room && need > packed))
     return fail(LLM42_EINVAL, "%s: rows * features too large for one launch", who);
   if (pack) launch_mx4_pack_x((const uint16_t*)x, x_stride, rows, k, (uint16_t*)workspace, st);
   launch_mx4_matmul(w, n, k, (const uint16_t*)(pack ? workspace : x), pack ? 0 : x_stride, loose, rows, out, out_type, out_stride,
-                    num_cus(), room && need > packed ? (float*)((char*)workspace + packed) : nullptr, st);
+                    current_cus(), room && need > packed ? (float*)((char*)workspace + packed) : nullptr, st);
   return launched(who);
 }
 
