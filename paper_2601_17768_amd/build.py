@@ -33,6 +33,7 @@ FILE_FLAGS = {
     "attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     "kv4_attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     "kv_sparse.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+    "kv_select.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
 }
 
 

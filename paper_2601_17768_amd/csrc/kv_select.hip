@@ -16,9 +16,14 @@ __device__ inline uint32_t key_of(float score) {
   return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
 
-// Query heads as operands of the scores: column l16 of the product is head l16 % group of tile row l16 / group.  Lane (g, l16) has features 64 c + 16 g .. + 15
-// of its column, positive values in one operand and negative ones in the other: the first meets the upper bounds, the other the
-// lower ones, and their sum is the sum of the larger products.
+// The value of another lane of the same 16: of lane l ^ 1, l ^ 2, or, mirrored, of the other four or eight.
+template <int CTRL>
+__device__ inline uint32_t other_lane(uint32_t x) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, true); }
+constexpr int kXor1 = 0xB1, kXor2 = 0x4E, kMirror8 = 0x141, kMirror16 = 0x140;
+
+// Query heads as operands of the scores: column l16 of the product is head l16 % cols of tile row l16 / cols, `cols` the group rounded up to a power of two (what is
+// behind the group repeats its last head).  Lane (g, l16) has features 64 c + 16 g .. + 15 of its column, positive values in one operand and negative ones in
+// the other: the first meets the upper bounds, the other the lower ones, and their sum is the sum of the larger products.
 template <int HD>
 struct Query {
   i32x4 pos[HD / 64], neg[HD / 64];
@@ -51,83 +56,137 @@ __device__ inline void quantize(Query<HD>& d, const uint16_t* const (&src)[HD / 
   const bool none = e > kMostExponent;
   const float inverse = none ? 0.f : power_of_two(-e);
   d.unit = none ? 0.f : power_of_two(e);
+  // x / 2^e rounded to a whole number, ties to even, in the low byte of x / 2^e + 1.5 * 2^23
 #pragma unroll
   for (int c = 0; c < C; ++c)
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      uint32_t p = 0, n = 0;
+      uint32_t r[4];
 #pragma unroll
       for (int b = 0; b < 4; ++b) {
         const uint32_t x = w[c][j >> 1][(j & 1) * 2 + (b >> 1)];
-        const int q = none ? 0 : (int)rintf((b & 1 ? hi_bf16(x) : lo_bf16(x)) * inverse);
-        p |= (uint32_t)max(q, 0) << (8 * b);
-        n |= ((uint32_t)min(q, 0) & 255u) << (8 * b);
+        r[b] = __float_as_uint(fmaf(b & 1 ? hi_bf16(x) : lo_bf16(x), inverse, 12582912.0f));
       }
-      d.pos[c][j] = (int)p;
-      d.neg[c][j] = (int)n;
+      const uint32_t q = none ? 0 : __builtin_amdgcn_perm(__builtin_amdgcn_perm(r[3], r[2], 0x0C0C0400u), __builtin_amdgcn_perm(r[1], r[0], 0x0C0C0400u), 0x05040100u);
+      const uint32_t sign = q >> 7 & 0x01010101u, minus = (sign << 8) - sign;     // 255 in the bytes below zero
+      d.pos[c][j] = (int)(q & ~minus);
+      d.neg[c][j] = (int)(q & minus);
     }
 }
 
-// Keys of 16 blocks, of which lane l16 of every group of 16 has the record: lane (g, column) gets those of blocks 4 g .. 4 g + 3 for its column's tile row (the largest
-// over the columns of the same tile row).
+// What lane (g, l16) holds of the bounds of block l16.
 template <int HD>
-__device__ inline void score16(uint32_t (&key)[4], const char* rec, const Query<HD>& q, int group, int lane) {
+struct Record {
+  i32x4 up[HD / 64], down[HD / 64];
+  int e;
+  __device__ inline void load(const char* rec, int g) {
+#pragma unroll
+    for (int c = 0; c < HD / 64; ++c) {
+      up[c] = *(const i32x4*)(rec + c * 64 + g * 16);
+      down[c] = *(const i32x4*)(rec + HD + c * 64 + g * 16);
+    }
+    e = *(const uint8_t*)(rec + 2 * HD);
+  }
+};
+
+// Keys of U times 16 blocks, of which lane l16 of every group of 16 has the records: lane (g, column) gets those of blocks 4 g .. 4 g + 3 for its column's tile row (the
+// largest over the columns of the same tile row).
+template <int HD, int COLS, int U>
+__device__ inline void score16(u32x4 (&key)[U], const Record<HD> (&d)[U], const Query<HD>& q, int lane) {
   constexpr int C = HD / 64;
-  const int g = lane >> 4, l16 = lane & 15;
-  i32x4 up[C], down[C];
+  const int g = lane >> 4;
+  i32x4 acc[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) acc[u] = (i32x4){0, 0, 0, 0};
 #pragma unroll
   for (int c = 0; c < C; ++c) {
-    up[c] = *(const i32x4*)(rec + c * 64 + g * 16);
-    down[c] = *(const i32x4*)(rec + HD + c * 64 + g * 16);
+#pragma unroll
+    for (int u = 0; u < U; ++u) acc[u] = __builtin_amdgcn_mfma_i32_16x16x64_i8(d[u].up[c], q.pos[c], acc[u], 0, 0, 0);
+#pragma unroll
+    for (int u = 0; u < U; ++u) acc[u] = __builtin_amdgcn_mfma_i32_16x16x64_i8(d[u].down[c], q.neg[c], acc[u], 0, 0, 0);
   }
-  const int e = *(const uint8_t*)(rec + 2 * HD);
-  i32x4 acc = {0, 0, 0, 0};
+  int e[U][4];
 #pragma unroll
-  for (int c = 0; c < C; ++c) {
-    acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(up[c], q.pos[c], acc, 0, 0, 0);
-    acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(down[c], q.neg[c], acc, 0, 0, 0);
-  }
-  float s[4];
+  for (int u = 0; u < U; ++u)
 #pragma unroll
-  for (int i = 0; i < 4; ++i) s[i] = (float)acc[i] * q.unit;
-  const int first = lane - l16 % group;                           // (columns behind the last tile row: whatever they get is not used)
-  if ((group & (group - 1)) == 0) {
-    for (int d = 1; d < group; d *= 2)
+    for (int i = 0; i < 4; ++i) e[u][i] = __shfl(d[u].e, g * 4 + i);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) s[i] = fmaxf(s[i], __shfl_xor(s[i], d));
-  } else {
-    float m[4] = {s[0], s[1], s[2], s[3]};
-    for (int d = 0; d < group; ++d)
+  for (int u = 0; u < U; ++u)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) m[i] = fmaxf(m[i], __shfl(s[i], first + d));
-#pragma unroll
-    for (int i = 0; i < 4; ++i) s[i] = m[i];
-  }
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int eb = __shfl(e, g * 4 + i);
-    key[i] = eb == kBoundsNone ? 0xFFFFFFFFu : key_of(s[i] * power_of_two(eb - kBoundsBias));
-  }
+    for (int i = 0; i < 4; ++i) {
+      float s = (float)acc[u][i] * q.unit;
+      const auto with = [&](uint32_t x) __attribute__((always_inline)) { s = fmaxf(s, __uint_as_float(x)); };
+      if constexpr (COLS > 1) with(other_lane<kXor1>(__float_as_uint(s)));
+      if constexpr (COLS > 2) with(other_lane<kXor2>(__float_as_uint(s)));
+      if constexpr (COLS > 4) with(other_lane<kMirror8>(__float_as_uint(s)));
+      if constexpr (COLS > 8) with(other_lane<kMirror16>(__float_as_uint(s)));
+      key[u][i] = e[u][i] == kBoundsNone ? 0xFFFFFFFFu : key_of(s * power_of_two(e[u][i] - kBoundsBias));
+    }
 }
 
 struct Scratch {
-  int hist[256], bin, need, gt[kWaves * 4], eq[kWaves * 4];
+  int hist[256], bin, need;
+  uint32_t all, any, counts[256];
 };
 
+// The bits in which the keys of a row differ (the scores of a row share their sign and most of their exponent, and are whole numbers times a power of
+// two: a third of the bits or more are the same), asked by a wave.
+__device__ inline void reduce_bits(uint32_t& all, uint32_t& any) {
+  all &= other_lane<kXor1>(all), any |= other_lane<kXor1>(any);
+  all &= other_lane<kXor2>(all), any |= other_lane<kXor2>(any);
+  all &= other_lane<kMirror8>(all), any |= other_lane<kMirror8>(any);
+  all &= other_lane<kMirror16>(all), any |= other_lane<kMirror16>(any);
+  const u32x2 a16 = __builtin_amdgcn_permlane16_swap(all, all, false, false), o16 = __builtin_amdgcn_permlane16_swap(any, any, false, false);
+  all = a16.x & a16.y, any = o16.x | o16.y;
+  const u32x2 a32 = __builtin_amdgcn_permlane32_swap(all, all, false, false), o32 = __builtin_amdgcn_permlane32_swap(any, any, false, false);
+  all = a32.x & a32.y, any = o32.x | o32.y;
+}
+
 // The `k` highest of keys[begin .. end - 1], the lowest index on ties, ascending to out; the whole workgroup of T threads together.  The k-th highest key is
-// found a byte at a time, from counts of the keys that agree with it so far; then one pass in order.
-template <int T>
+// found eight bits at a time, among those that differ, from counts of the keys that agree with it so far; then one pass in order.  R keys to a thread are held in
+// registers; R 0: any number of them, read again in every pass.
+template <int T, int R>
 __device__ inline void pick(const uint32_t* keys, int begin, int end, int k, int32_t* out, Scratch& sh) {
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-  uint32_t prefix = 0, mask = 0;
+  uint32_t u[R ? R : 1], all = 0xFFFFFFFFu, any = 0;
+  if constexpr (R > 0) {
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const int i = begin + r * T + tid;
+      u[r] = i < end ? keys[i] : 0;                               // (no key is 0: that is the pattern of a NaN)
+    }
+  }
+  const auto each = [&](const auto& f) __attribute__((always_inline)) {
+    if constexpr (R > 0) {
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+        if (begin + r * T + tid < end) f(u[r]);
+    } else {
+      for (int i = begin + tid; i < end; i += T) f(keys[i]);
+    }
+  };
+  each([&](uint32_t x) { all &= x, any |= x; });
+  reduce_bits(all, any);
+  if (tid == 0) {
+    sh.all = 0xFFFFFFFFu;
+    sh.any = 0;
+  }
+  __syncthreads();
+  if (lane == 0) {
+    atomicAnd(&sh.all, all);
+    atomicOr(&sh.any, any);
+  }
+  __syncthreads();
+  const uint32_t differ = sh.all ^ sh.any;
+  uint32_t prefix = sh.all & ~differ, mask = ~differ;
   int need = k;
-  for (int shift = 24; shift >= 0; shift -= 8) {
+  for (int top = differ ? 31 - __clz((int)differ) : -1; top >= 0;) {
+    const int shift = max(top - 7, 0), bins = (2 << (top - shift)) - 1;
     for (int i = tid; i < 256; i += T) sh.hist[i] = 0;
     __syncthreads();
-    for (int i = begin + tid; i < end; i += T) {
-      const uint32_t u = keys[i];
-      if ((u & mask) == prefix) atomicAdd(&sh.hist[u >> shift & 255], 1);
-    }
+    each([&](uint32_t x) {
+      if ((x & mask) == (prefix & mask)) atomicAdd(&sh.hist[x >> shift & bins], 1);
+    });
     __syncthreads();
     if (wave == 0) {                                              // bins from the highest down, four to a lane
       int c[4], sum = 0;
@@ -150,55 +209,131 @@ __device__ inline void pick(const uint32_t* keys, int begin, int end, int k, int
       }
     }
     __syncthreads();
-    prefix |= (uint32_t)sh.bin << shift;
-    mask |= 255u << shift;
+    prefix = (prefix & ~((uint32_t)bins << shift)) | (uint32_t)sh.bin << shift;
+    mask |= (uint32_t)bins << shift;
     need = sh.need;
+    const uint32_t below = differ & ((1u << shift) - 1);
+    top = below ? 31 - __clz((int)below) : -1;
   }
-  int gt_before = 0, eq_before = 0;
-  for (int base = begin; base < end; base += T) {
-    const int i = base + tid;
-    const uint32_t u = i < end ? keys[i] : 0;
-    const bool gt = i < end && u > prefix, eq = i < end && u == prefix;
-    const uint64_t bg = __ballot(gt), be = __ballot(eq), below = (1ull << lane) - 1;
-    __syncthreads();
-    if (lane == 0) {
-      sh.gt[wave] = __popcll(bg);
-      sh.eq[wave] = __popcll(be);
+  // in order: counts of every wave's 64 keys (those above in the low half, those that are the k-th itself in the high one: R * T is below 2^16), what comes before each, places
+  constexpr int S = R ? R : 1, W = T / 64, E = S * W;
+  static_assert(E <= 256 && S * T < 65536);
+  const uint64_t below = (1ull << lane) - 1;
+  uint32_t base = 0;
+  for (int from = begin; from < end; from += S * T) {
+    uint64_t bg[S], be[S];
+#pragma unroll
+    for (int r = 0; r < S; ++r) {
+      const int i = from + r * T + tid;
+      uint32_t x;
+      if constexpr (R > 0) x = u[r];
+      else x = i < end ? keys[i] : 0;
+      bg[r] = __ballot(i < end && x > prefix);
+      be[r] = __ballot(i < end && x == prefix);
+      if (lane == 0) sh.counts[r * W + wave] = (uint32_t)__popcll(be[r]) << 16 | (uint32_t)__popcll(bg[r]);
     }
     __syncthreads();
-    int ng = gt_before + __popcll(bg & below), ne = eq_before + __popcll(be & below);
-    for (int v = 0; v < T / 64; ++v) {
-      if (v < wave) {
-        ng += sh.gt[v];
-        ne += sh.eq[v];
+    if (wave == 0) {
+      constexpr int C = (E + 63) / 64;
+      uint32_t c[C], sum = 0;
+#pragma unroll
+      for (int j = 0; j < C; ++j) sum += c[j] = lane * C + j < E ? sh.counts[lane * C + j] : 0;
+      uint32_t before = sum;
+#pragma unroll
+      for (int d = 1; d < 64; d *= 2) {
+        const uint32_t x = (uint32_t)__shfl_up((int)before, d);
+        if (lane >= d) before += x;
       }
-      gt_before += sh.gt[v];
-      eq_before += sh.eq[v];
+      if (lane == 63) sh.any = before;
+      before -= sum;
+#pragma unroll
+      for (int j = 0; j < C; ++j) {
+        if (lane * C + j < E) sh.counts[lane * C + j] = before;
+        before += c[j];
+      }
     }
-    if (gt || (eq && ne < need)) out[ng + min(ne, need)] = i;
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < S; ++r) {
+      const uint32_t before = sh.counts[r * W + wave];
+      const int ng = (int)(base & 0xFFFFu) + (int)(before & 0xFFFFu) + __popcll(bg[r] & below);
+      const int ne = (int)(base >> 16) + (int)(before >> 16) + __popcll(be[r] & below);
+      const bool gt = bg[r] >> lane & 1, eq = be[r] >> lane & 1;
+      if (gt || (eq && ne < need)) out[ng + min(ne, need)] = from + r * T + tid;
+    }
+    // (what is above is fewer than k, at most 4096; of the k-th itself no more than that have to be told apart)
+    const uint32_t total = sh.any, e = min((base >> 16) + (total >> 16), 32767u);
+    base = e << 16 | ((base + total) & 0xFFFFu);
+    __syncthreads();
   }
 }
 
-// What a row selects, given the keys of its blocks (keys[b], read where it sees more than the budget).
+// The same by one wave with its keys in registers, R to a lane: the k-th highest key a bit at a time.  (A key is never 0: that is the pattern of a NaN.)
+template <int R>
+__device__ inline void pick_by_wave(const uint32_t* keys, int begin, int end, int k, int32_t* out, int lane) {
+  uint32_t u[R], all = 0xFFFFFFFFu, any = 0;
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const int i = begin + r * 64 + lane;
+    u[r] = i < end ? keys[i] : 0;
+    all &= i < end ? u[r] : 0xFFFFFFFFu;
+    any |= u[r];
+  }
+  reduce_bits(all, any);
+  uint32_t differ = __builtin_amdgcn_readfirstlane(all ^ any), least = __builtin_amdgcn_readfirstlane(all) & ~differ;
+  auto at_least = [&](uint32_t x) __attribute__((always_inline)) {
+    int n = 0;
+#pragma unroll
+    for (int r = 0; r < R; ++r) n += __popcll(__ballot(u[r] >= x));
+    return n;
+  };
+  int need = 0;                                                   // of the keys that are `least` itself
+  bool exact = false;
+  while (differ) {
+    const uint32_t bit = 0x80000000u >> __clz((int)differ);
+    differ ^= bit;
+    const int n = at_least(least | bit);
+    if (n >= k) least |= bit;
+    if (n == k) {
+      exact = true;
+      break;
+    }
+  }
+  if (exact) --least;
+  else need = k - at_least(least + 1);
+  int ng = 0, ne = 0;
+  const uint64_t below = (1ull << lane) - 1;
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const bool gt = u[r] > least, eq = u[r] == least;
+    const uint64_t bg = __ballot(gt), be = __ballot(eq);
+    const int rank = ne + __popcll(be & below);
+    if (gt || (eq && rank < need)) out[ng + __popcll(bg & below) + min(rank, need)] = begin + r * 64 + lane;
+    ng += __popcll(bg);
+    ne += __popcll(be);
+  }
+}
+
+// What a row selects without a look at scores, by T threads; returns how many it selects by them.
 template <int T>
-__device__ inline void select_row(const Select& a, const uint32_t* keys, int own, int32_t* out, Scratch& sh) {
+__device__ inline int select_plain(const Select& a, int own, int32_t* out, int tid) {
   const int seen = own + 1;
   if (seen <= a.budget) {
-    for (int j = threadIdx.x; j < a.budget; j += T) out[j] = j < seen ? j : -1;
-    return;
+    for (int j = tid; j < a.budget; j += T) out[j] = j < seen ? j : -1;
+    return 0;
   }
   const int k = a.budget - a.sink - a.recent;
-  for (int j = threadIdx.x; j < a.sink + a.recent; j += T) {
+  for (int j = tid; j < a.sink + a.recent; j += T) {
     if (j < a.sink) out[j] = j;
     else out[k + j] = own - a.recent + 1 + (j - a.sink);
   }
-  if (k > 0) pick<T>(keys, a.sink, seen - a.recent, k, out + a.sink, sh);
+  return k;
 }
 
 // Pointers to the query of column l16 of a tile of rows i0 .. i0 + rows - 1, features 64 c + 16 g + 8 p.
-template <int HD>
+template <int HD, int COLS>
 __device__ inline void query_of(const uint16_t* (&src)[HD / 64][2], const Select& a, int s, int kvh, int i0, int rows, int lane) {
-  const int g = lane >> 4, l16 = lane & 15, i = min(i0 + l16 / a.group, i0 + rows - 1), h = l16 % a.group;
+  const int g = lane >> 4, l16 = lane & 15, i = min(i0 + l16 / COLS, i0 + rows - 1), h = min(l16 % COLS, a.group - 1);
 #pragma unroll
   for (int c = 0; c < HD / 64; ++c)
 #pragma unroll
@@ -221,55 +356,94 @@ __device__ inline int whole_status(const Rows& r, int s, int len, int n) {
   return __syncthreads_or(bad) ? LLM42_SEQ_BAD_BLOCK : status;
 }
 
-// Keys of blocks begin .. end - 1 (of the sequence) for a tile of rows, by the waves of a workgroup in turn; keys of tile row r at keys + r * stride.
-template <int HD>
-__device__ inline void score_blocks(const Select& a, int s, int kvh, int i0, int rows, int begin, int end, uint32_t* keys, int64_t stride) {
+// Keys of blocks begin .. end - 1 (of the sequence) for a tile of rows, by the waves of a workgroup in turn, four times 16 blocks at once; keys of tile row r at
+// keys + r * stride, a multiple of 16 (those around begin and end - 1 may be anything).  id_of(b): the physical block.
+template <int HD, int COLS, class Ids>
+__device__ inline void score_blocks(const Select& a, const Query<HD>& q, int kvh, int rows, int begin, int end, uint32_t* keys, int64_t stride, Ids id_of) {
+  constexpr int U = 4;
   const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6, lane = threadIdx.x & 63, g = lane >> 4, l16 = lane & 15;
-  const uint16_t* src[HD / 64][2];
-  query_of<HD>(src, a, s, kvh, i0, rows, lane);
-  Query<HD> q;
-  quantize<HD>(q, src);
-  const int32_t* ids = a.rows.block_table + (size_t)s * a.rows.width;
-  for (int t = begin / 16 + wave; t * 16 < end; t += waves) {
-    const int b = min(max(t * 16 + l16, begin), end - 1);
-    const char* rec = a.bounds + ((size_t)ids[b] * a.n_kv_heads + kvh) * bounds_record(HD);
-    uint32_t key[4];
-    score16<HD>(key, rec, q, a.group, lane);
-    if (l16 % a.group == 0 && l16 / a.group < rows) {
+  const int end_tile = (end + 15) / 16;
+  for (int t0 = begin / 16 + wave * U; t0 < end_tile; t0 += waves * U) {
+    Record<HD> d[U];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int at = t * 16 + g * 4 + i;
-        if (at >= begin && at < end) keys[(l16 / a.group) * stride + at] = key[i];
-      }
+    for (int u = 0; u < U; ++u) {
+      const int b = min(max((t0 + u) * 16 + l16, begin), end - 1);
+      d[u].load(a.bounds + ((size_t)id_of(b) * a.n_kv_heads + kvh) * bounds_record(HD), g);
+    }
+    __builtin_amdgcn_sched_barrier(0);                            // (all of them asked for before the first is waited for)
+    u32x4 key[U];
+    score16<HD, COLS, U>(key, d, q, lane);
+    if (l16 % COLS == 0 && l16 / COLS < rows) {
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (t0 + u < end_tile) *(u32x4*)(keys + (l16 / COLS) * stride + (t0 + u) * 16 + g * 4) = key[u];
     }
   }
 }
 
-// Scores in LDS: a workgroup per (sequence, tile of 16 / group rows), blockIdx.y: kv head.
-template <int HD>
+template <int HD, int COLS>
+__device__ inline Query<HD> query(const Select& a, int s, int kvh, int i0, int rows) {
+  const uint16_t* src[HD / 64][2];
+  query_of<HD, COLS>(src, a, s, kvh, i0, rows, threadIdx.x & 63);
+  Query<HD> q;
+  quantize<HD>(q, src);
+  return q;
+}
+
+// Scores in LDS: a workgroup per (sequence, tile of 16 / group rows), blockIdx.y: kv head.  The ids of the blocks wait in the first row's place in LDS until
+// their scores take it (a wave reads and writes the same 64 of them).
+template <int HD, int COLS>
 __global__ __launch_bounds__(kThreads) void select_kernel(Select a, int tile_rows, int tiles, int stride) {
-  extern __shared__ uint32_t sh_keys[];
+  extern __shared__ __align__(16) uint32_t sh_keys[];
   __shared__ Scratch sh;
   const Rows& r = a.rows;
   const int s = blockIdx.x / tiles, i0 = blockIdx.x % tiles * tile_rows, kvh = blockIdx.y;
   const int len = r.seq_len[s], n = r.seq_n ? r.seq_n[s] : r.window;
-  const int status = whole_status(r, s, len, n);
+  int status = length_status(r, len, n);
+  const int rows = min(tile_rows, n - i0), last = (len + i0 + rows - 1) / LLM42_KV_BLOCK, scored = last + 1 - a.recent;
+  const bool scores = status == LLM42_SEQ_OK && rows > 0 && last + 1 > a.budget && a.budget > a.sink + a.recent;
+  bool bad = false;
+  if (status == LLM42_SEQ_OK && n > 0)
+    for (int b = threadIdx.x; b <= (len + n - 1) / LLM42_KV_BLOCK; b += kThreads) {
+      const int id = r.block_table[(size_t)s * r.width + b];
+      bad |= id < 0 || id >= r.num_blocks;
+      if (scores && b < scored) sh_keys[b] = (uint32_t)id;
+    }
+  Query<HD> q;
+  if (scores) q = query<HD, COLS>(a, s, kvh, i0, rows);
+  if (__syncthreads_or(bad)) status = LLM42_SEQ_BAD_BLOCK;
   if (a.seq_status && i0 == 0 && kvh == 0 && threadIdx.x == 0) a.seq_status[s] = status;
-  if (status != LLM42_SEQ_OK || i0 >= n) return;
-  const int rows = min(tile_rows, n - i0), last = (len + i0 + rows - 1) / LLM42_KV_BLOCK;
-  if (last + 1 > a.budget && a.budget > a.sink + a.recent) {
-    score_blocks<HD>(a, s, kvh, i0, rows, a.sink, last + 1 - a.recent, sh_keys, stride);
+  if (status != LLM42_SEQ_OK || rows <= 0) return;
+  if (scores) {
+    score_blocks<HD, COLS>(a, q, kvh, rows, a.sink, scored, sh_keys, stride, [&](int b) { return sh_keys[b]; });
     __syncthreads();
   }
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const auto out_of = [&](int i) { return a.selected + (((size_t)s * r.window + i0 + i) * a.n_kv_heads + kvh) * a.budget; };
+  const int most = scored - a.sink;
+  if (!scores || most <= 1024) {                                  // a row to a wave
+    for (int i = wave; i < rows; i += kWaves) {
+      const int own = (len + i0 + i) / LLM42_KV_BLOCK, end = own + 1 - a.recent;
+      int32_t* out = out_of(i);
+      const int k = select_plain<64>(a, own, out, lane);
+      const uint32_t* keys = sh_keys + i * stride;
+      if (k == 0) continue;
+      if (most <= 256) pick_by_wave<4>(keys, a.sink, end, k, out + a.sink, lane);
+      else if (most <= 512) pick_by_wave<8>(keys, a.sink, end, k, out + a.sink, lane);
+      else pick_by_wave<16>(keys, a.sink, end, k, out + a.sink, lane);
+    }
+    return;
+  }
   for (int i = 0; i < rows; ++i) {
-    select_row<kThreads>(a, sh_keys + i * stride, (len + i0 + i) / LLM42_KV_BLOCK,
-                         a.selected + (((size_t)s * r.window + i0 + i) * a.n_kv_heads + kvh) * a.budget, sh);
+    const int own = (len + i0 + i) / LLM42_KV_BLOCK;
+    const int k = select_plain<kThreads>(a, own, out_of(i), threadIdx.x);
+    if (k) pick<kThreads, 0>(sh_keys + i * stride, a.sink, own + 1 - a.recent, k, out_of(i) + a.sink, sh);
     __syncthreads();
   }
 }
 
 // Scores through the workspace, first launch: a workgroup per (sequence, tile of rows) and chunk of blocks (blockIdx.z).
-template <int HD>
+template <int HD, int COLS>
 __global__ __launch_bounds__(kThreads) void score_kernel(Select a, int tile_rows, int tiles, int64_t stride, int chunk) {
   const Rows& r = a.rows;
   const int s = blockIdx.x / tiles, i0 = blockIdx.x % tiles * tile_rows, kvh = blockIdx.y;
@@ -285,8 +459,9 @@ __global__ __launch_bounds__(kThreads) void score_kernel(Select a, int tile_rows
     bad |= id < 0 || id >= r.num_blocks;
   }
   if (__syncthreads_or(bad)) return;                              // (the second launch sees it too)
-  score_blocks<HD>(a, s, kvh, i0, rows, begin, end, a.keys + (((size_t)s * r.window + i0) * a.n_kv_heads + kvh) * stride,
-                   a.n_kv_heads * stride);
+  const int32_t* ids = r.block_table + (size_t)s * r.width;
+  score_blocks<HD, COLS>(a, query<HD, COLS>(a, s, kvh, i0, rows), kvh, rows, begin, end, a.keys + (((size_t)s * r.window + i0) * a.n_kv_heads + kvh) * stride,
+                   a.n_kv_heads * stride, [&](int b) { return ids[b]; });
 }
 
 // ... and second: a workgroup per row, blockIdx.y: kv head.
@@ -300,19 +475,35 @@ __global__ __launch_bounds__(kPickThreads) void pick_kernel(Select a, int64_t st
   if (a.seq_status && i == 0 && kvh == 0 && threadIdx.x == 0) a.seq_status[s] = status;
   if (status != LLM42_SEQ_OK || i >= n) return;
   const size_t at = ((size_t)s * r.window + i) * a.n_kv_heads + kvh;
-  select_row<kPickThreads>(a, a.keys + at * stride, (len + i) / LLM42_KV_BLOCK, a.selected + at * a.budget, sh);
+  const int own = (len + i) / LLM42_KV_BLOCK;
+  int32_t* out = a.selected + at * a.budget;
+  const int k = select_plain<kPickThreads>(a, own, out, threadIdx.x);
+  if (k == 0) return;
+  const uint32_t* keys = a.keys + at * stride;
+  const int end = own + 1 - a.recent, most = end - a.sink;
+  if (most <= 2 * kPickThreads) pick<kPickThreads, 2>(keys, a.sink, end, k, out + a.sink, sh);
+  else if (most <= 8 * kPickThreads) pick<kPickThreads, 8>(keys, a.sink, end, k, out + a.sink, sh);
+  else pick<kPickThreads, 0>(keys, a.sink, end, k, out + a.sink, sh);
 }
 
-// Keys of a tile row, one for each block that max_context positions can have.
-int64_t keys_of(int max_context) { return (max_context + 15) / 16; }
-int tile_rows_of(int group, int window) { return std::min(16 / group, window); }
+// Keys of a tile row, one for each block that max_context positions can have, a multiple of 16.
+int64_t keys_of(int max_context) { return ((int64_t)max_context + 255) / 256 * 16; }
+int cols_of(int group) { return group > 8 ? 16 : group > 4 ? 8 : group > 2 ? 4 : group; }
+int tile_rows_of(int group, int window) { return std::min(16 / cols_of(group), window); }
 constexpr int64_t kMostLdsKeys = 12288;      // 48 KiB
 
 }  // namespace
 
 size_t select_workspace(int num_seqs, int window, int n_kv_heads, int group, int max_context, int budget, int num_cus) {
   const int64_t keys = keys_of(max_context);
-  if (keys <= budget || tile_rows_of(group, window) * keys <= kMostLdsKeys) return 0;
+  const int tile_rows = tile_rows_of(group, window);
+  const int64_t wgs = (int64_t)num_seqs * ((window + tile_rows - 1) / tile_rows) * n_kv_heads;
+  if (keys <= budget) return 0;
+  // A workgroup gets about 20 bytes a ns from memory, whatever it has in flight, so few of them with long contexts leave the device idle: their scores go through the
+  // workspace, 256 blocks to a workgroup, and a second launch picks (us so / in LDS, sequences x positions, 8 kv heads of 128, group 4: 1 x 8192
+  // 13.6 / 13.7, 1 x 16384 14.4 / 21, 8 x 16384 14.7 / 21, 16 x 32768 26 / 34, 1 x 131072 25 / 106, 1 window of 64 x 30000 33 / 58; but 32 x 32768
+  // 39 / 36, 128 x 8192 56 / 34, 4 windows of 32 x 8000 36 / 17).  Those of a tile of rows that LDS does not hold go there too.
+  if (tile_rows * keys <= kMostLdsKeys && (2 * wgs > num_cus || keys <= 512)) return 0;
   return 4ull * num_seqs * window * n_kv_heads * keys;
 }
 
@@ -320,17 +511,26 @@ void launch_kv_select(const Select& a, hipStream_t st) {
   const Rows& r = a.rows;
   const int tile_rows = tile_rows_of(a.group, r.window), tiles = (r.window + tile_rows - 1) / tile_rows;
   const int64_t keys = keys_of(r.max_context);
-  const auto go = [&](auto hd) {
-    constexpr int HD = decltype(hd)::value;
+  const auto go = [&](auto hd, auto cols) {
+    constexpr int HD = decltype(hd)::value, COLS = decltype(cols)::value;
     if (!a.keys) {
       const size_t lds = keys <= a.budget ? 0 : 4 * tile_rows * keys;
-      select_kernel<HD><<<dim3(r.num_seqs * tiles, a.n_kv_heads), kThreads, lds, st>>>(a, tile_rows, tiles, (int)keys);
+      select_kernel<HD, COLS><<<dim3(r.num_seqs * tiles, a.n_kv_heads), kThreads, lds, st>>>(a, tile_rows, tiles, (int)keys);
       return;
     }
-    const int chunk = (int)std::max<int64_t>(256, (keys + 4095) / 4096);
-    score_kernel<HD><<<dim3(r.num_seqs * tiles, a.n_kv_heads, (unsigned)((keys + chunk - 1) / chunk)), kThreads, 0, st>>>(a, tile_rows, tiles, keys, chunk);
+    const int chunk = (int)std::max<int64_t>(256, (keys + 65535) / 65536 * 16);
+    score_kernel<HD, COLS><<<dim3(r.num_seqs * tiles, a.n_kv_heads, (unsigned)((keys + chunk - 1) / chunk)), kThreads, 0, st>>>(a, tile_rows, tiles, keys, chunk);
     pick_kernel<<<dim3(r.num_seqs * r.window, a.n_kv_heads), kPickThreads, 0, st>>>(a, keys);
   };
-  if (a.head_dim == 128) go(std::integral_constant<int, 128>{});
-  else go(std::integral_constant<int, 64>{});
+  const auto by_cols = [&](auto hd) {
+    switch (cols_of(a.group)) {
+      case 1: return go(hd, std::integral_constant<int, 1>{});
+      case 2: return go(hd, std::integral_constant<int, 2>{});
+      case 4: return go(hd, std::integral_constant<int, 4>{});
+      case 8: return go(hd, std::integral_constant<int, 8>{});
+      default: return go(hd, std::integral_constant<int, 16>{});
+    }
+  };
+  if (a.head_dim == 128) by_cols(std::integral_constant<int, 128>{});
+  else by_cols(std::integral_constant<int, 64>{});
 }
