@@ -137,7 +137,7 @@ llm42_status llm42_kv_bounds_store(
     void*                 hip_stream);
 
 /* What the bounds of the physical blocks block_ids[j] stand for, all layers (each value is a bf16): out_lo and out_hi are bf16
- * [n_layers][num_ids][n_kv_heads][head_dim], 16-byte aligned; an id out of range leaves its values as they were. */
+ * [n_layers][num_ids][n_kv_heads][head_dim], 16-byte aligned; an id out of range gives zeros. */
 llm42_status llm42_kv_bounds_read(
     const llm42_heads*    heads,
     const void*           kv_bounds,       /* dev                                          */

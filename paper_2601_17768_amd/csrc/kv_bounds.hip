@@ -7,16 +7,19 @@ using namespace paged;
 
 namespace {
 
-// One wave per (block of 16 positions, kv head), four to a workgroup; blockIdx.y: layer.
-template <int HD>
+// One wave per (block of 16 positions, kv head) and L layers (blockIdx.y), the next layer's keys asked for before this one's are looked at; four waves to a
+// workgroup.  Bound by memory: the keys of 4 x 1500 - 2048 tokens of 32 layers of 8 heads of 128, 461 MB, and their bounds take 109 us, 4.5 TB/s
+// (a layer to a wave 130: three loads that wait for each other stand before every 4 KiB; where there are few waves that costs less than
+// four layers in turn, 24 x 1 - 32 tokens 12.2 / 14.6).
+template <int HD, int L>
 __global__ __launch_bounds__(256) void bounds_store_kernel(const uint16_t* __restrict__ k_plane, int64_t layer_stride, char* __restrict__ bounds,
                                                            const int32_t* __restrict__ table, int width, int64_t num_blocks, int n_kv_heads,
                                                            const int32_t* __restrict__ first_, const int32_t* __restrict__ count_, int num_seqs,
-                                                           int max_count, int slots, int32_t* __restrict__ seq_status) {
+                                                           int max_count, int slots, int n_layers, int32_t* __restrict__ seq_status) {
   constexpr int LANES = HD / 8, N = HD / 32;
   const int lane = threadIdx.x & 63;
   const int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int h = (int)(item % n_kv_heads), slot = (int)(item / n_kv_heads % slots), s = (int)(item / n_kv_heads / slots), layer = blockIdx.y;
+  const int h = (int)(item % n_kv_heads), slot = (int)(item / n_kv_heads % slots), s = (int)(item / n_kv_heads / slots), layer = blockIdx.y * L;
   if (s >= num_seqs) return;
   const int64_t first = first_[s], count = count_[s];
   int status = LLM42_SEQ_OK;
@@ -35,12 +38,23 @@ __global__ __launch_bounds__(256) void bounds_store_kernel(const uint16_t* __res
   const int block = begin + slot;
   if (status != LLM42_SEQ_OK || count == 0 || block >= end) return;
   const size_t at = (size_t)table[(size_t)s * width + block] * n_kv_heads + h;
-  const uint16_t* tile = k_plane + layer * layer_stride + at * 16 * HD;
-  u32x4 key[N];
   const int c = lane % LANES, t0 = lane / LANES;
+  const uint16_t* tile = k_plane + layer * layer_stride + at * 16 * HD + (c * 16 + t0) * 8;
+  char* rec = bounds + ((size_t)layer * num_blocks * n_kv_heads + at) * bounds_record(HD);
+  const size_t rec_stride = (size_t)num_blocks * n_kv_heads * bounds_record(HD);
+  u32x4 key[2][N];
+  const auto load = [&](u32x4 (&d)[N], int l) __attribute__((always_inline)) {
 #pragma unroll
-  for (int i = 0; i < N; ++i) key[i] = *(const u32x4*)(tile + (c * 16 + t0 + i * (64 / LANES)) * 8);
-  write_bounds<HD>(key, bounds + ((size_t)layer * num_blocks * n_kv_heads + at) * bounds_record(HD), lane);
+    for (int i = 0; i < N; ++i) d[i] = *(const u32x4*)(tile + l * layer_stride + i * (64 / LANES) * 8);
+  };
+  const int layers = min(L, n_layers - layer);
+  load(key[0], 0);
+#pragma unroll
+  for (int l = 0; l < L; ++l) {
+    if (l >= layers) break;
+    if (L > 1) load(key[(l + 1) & 1], min(l + 1, layers - 1));
+    write_bounds<HD>(key[l & 1], rec + l * rec_stride, lane);
+  }
 }
 
 // A thread per 8 features of a (block, kv head); blockIdx.y: layer.
@@ -54,8 +68,8 @@ __global__ __launch_bounds__(256) void bounds_read_kernel(const char* __restrict
   const int64_t j = head / n_kv_heads;
   if (j >= num_ids) return;
   const int id = ids[j];
-  if (id < 0 || id >= num_blocks) return;
-  const char* rec = bounds + (((size_t)blockIdx.y * num_blocks + id) * n_kv_heads + h) * bounds_record(HD);
+  const bool there = id >= 0 && id < num_blocks;
+  const char* rec = bounds + (((size_t)blockIdx.y * num_blocks + (there ? id : 0)) * n_kv_heads + h) * bounds_record(HD);
   const int e = *(const uint8_t*)(rec + 2 * HD);
   const bool none = e == kBoundsNone;
   const float unit = none ? 0.f : power_of_two(e - kBoundsBias);
@@ -66,7 +80,7 @@ __global__ __launch_bounds__(256) void bounds_read_kernel(const char* __restrict
     const float inf = part ? -INFINITY : INFINITY;
     float x[8];
 #pragma unroll
-    for (int f = 0; f < 8; ++f) x[f] = none ? inf : (float)(int8_t)(w[f >> 2] >> (8 * (f & 3))) * unit;
+    for (int f = 0; f < 8; ++f) x[f] = !there ? 0.f : none ? inf : (float)(int8_t)(w[f >> 2] >> (8 * (f & 3))) * unit;
     u32x4 o;
 #pragma unroll
     for (int i = 0; i < 4; ++i) o[i] = pack2_bf16(x[2 * i], x[2 * i + 1]);
@@ -80,13 +94,14 @@ void launch_bounds_store(int n_layers, int n_kv_heads, int head_dim, const uint1
                          const int32_t* block_table, int width, int64_t num_blocks, const int32_t* first, const int32_t* count, int num_seqs,
                          int max_count, int32_t* seq_status, hipStream_t st) {
   const int slots = slots_of(max_count, width);
-  const dim3 grid((unsigned)(((int64_t)num_seqs * slots * n_kv_heads + 3) / 4), n_layers);
-  const auto go = [&](auto kernel) {
-    kernel<<<grid, 256, 0, st>>>(k_plane, layer_stride, bounds, block_table, width, num_blocks, n_kv_heads, first, count, num_seqs, max_count,
-                                 slots, seq_status);
+  const int64_t items = (int64_t)num_seqs * slots * n_kv_heads;
+  const auto go = [&](auto kernel, int layers) {
+    kernel<<<dim3((unsigned)((items + 3) / 4), (n_layers + layers - 1) / layers), 256, 0, st>>>(
+        k_plane, layer_stride, bounds, block_table, width, num_blocks, n_kv_heads, first, count, num_seqs, max_count, slots, n_layers, seq_status);
   };
-  if (head_dim == 128) go(bounds_store_kernel<128>);
-  else go(bounds_store_kernel<64>);
+  const bool few = items * n_layers <= 32768;
+  if (head_dim == 128) few ? go(bounds_store_kernel<128, 1>, 1) : go(bounds_store_kernel<128, 4>, 4);
+  else few ? go(bounds_store_kernel<64, 1>, 1) : go(bounds_store_kernel<64, 4>, 4);
 }
 
 void launch_bounds_read(int n_layers, int n_kv_heads, int head_dim, const char* bounds, int64_t num_blocks, const int32_t* ids, int num_ids,

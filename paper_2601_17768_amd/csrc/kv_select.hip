@@ -16,11 +16,6 @@ __device__ inline uint32_t key_of(float score) {
   return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
 
-// The value of another lane of the same 16: of lane l ^ 1, l ^ 2, or, mirrored, of the other four or eight.
-template <int CTRL>
-__device__ inline uint32_t other_lane(uint32_t x) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, true); }
-constexpr int kXor1 = 0xB1, kXor2 = 0x4E, kMirror8 = 0x141, kMirror16 = 0x140;
-
 // Query heads as operands of the scores: column l16 of the product is head l16 % cols of tile row l16 / cols, `cols` the group rounded up to a power of two (what is
 // behind the group repeats its last head).  Lane (g, l16) has features 64 c + 16 g .. + 15 of its column, positive values in one operand and negative ones in
 // the other: the first meets the upper bounds, the other the lower ones, and their sum is the sum of the larger products.

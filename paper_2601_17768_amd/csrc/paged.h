@@ -48,6 +48,19 @@ __device__ inline float power_of_two(int e) { return __uint_as_float((uint32_t)(
 __device__ inline float lo_bf16(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ inline float hi_bf16(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 
+// The value of another lane of the same 16: l ^ 1, l ^ 2, the mirrored one of its 8 or 16, l ^ 8.
+template <int CTRL>
+__device__ inline uint32_t other_lane(uint32_t x) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, true); }
+constexpr int kXor1 = 0xB1, kXor2 = 0x4E, kMirror8 = 0x141, kMirror16 = 0x140, kXor8 = 0x128;
+// f over a value and the same lanes' of the other 16 of its 32, and of the other 32: for all of the wave's groups of 16 lanes alike.
+template <class F>
+__device__ inline float over_rows(float x, F f) {
+  const u32x2 a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = f(__uint_as_float(a.x), __uint_as_float(a.y));
+  const u32x2 b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return f(__uint_as_float(b.x), __uint_as_float(b.y));
+}
+
 // Writes the bounds of a block of keys, of which this lane has features 8 c .. 8 c + 7 (c = lane % (HD / 8)) of HD / 32 tokens: one maximum and minimum a feature over
 // all tokens, the block's power of two, and both in whole multiples of it.  Exact throughout (bf16 keys, powers of two).
 template <int HD>
@@ -71,18 +84,24 @@ __device__ inline void write_bounds(const u32x4 (&key)[HD / 32], char* rec, int 
       mx[2 * w + 1] = fmaxf(mx[2 * w + 1], hi_bf16(x));
       mn[2 * w + 1] = fminf(mn[2 * w + 1], hi_bf16(x));
     }
-#pragma unroll
-  for (int d = LANES; d < 64; d *= 2)
-#pragma unroll
-    for (int f = 0; f < 8; ++f) {
-      mx[f] = fmaxf(mx[f], __shfl_xor(mx[f], d));
-      mn[f] = fminf(mn[f], __shfl_xor(mn[f], d));
-    }
+  const auto larger = [](float a, float b) { return fmaxf(a, b); };
+  const auto smaller = [](float a, float b) { return fminf(a, b); };
   float top = 0.f;
 #pragma unroll
-  for (int f = 0; f < 8; ++f) top = fmaxf(top, fmaxf(mx[f], -mn[f]));
-#pragma unroll
-  for (int d = 1; d < LANES; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
+  for (int f = 0; f < 8; ++f) {
+    if constexpr (LANES == 8) {
+      mx[f] = fmaxf(mx[f], __uint_as_float(other_lane<kXor8>(__float_as_uint(mx[f]))));
+      mn[f] = fminf(mn[f], __uint_as_float(other_lane<kXor8>(__float_as_uint(mn[f]))));
+    }
+    mx[f] = over_rows(mx[f], larger);
+    mn[f] = over_rows(mn[f], smaller);
+    top = fmaxf(top, fmaxf(mx[f], -mn[f]));
+  }
+  const auto with = [&](uint32_t x) { top = fmaxf(top, __uint_as_float(x)); };
+  with(other_lane<kXor1>(__float_as_uint(top)));
+  with(other_lane<kXor2>(__float_as_uint(top)));
+  with(other_lane<kMirror8>(__float_as_uint(top)));
+  if constexpr (LANES == 16) with(other_lane<kMirror16>(__float_as_uint(top)));
   const int e = __any(bad) ? kMostExponent + 1 : bounds_exponent(top);
   const bool none = e > kMostExponent;
   const float unit = none ? 0.f : power_of_two(-e);

@@ -118,7 +118,7 @@ class PagedCache:
         """One llm42_kv_bounds_read call: (smallest, largest) of the physical blocks, bfloat16 [n_layers, len(block_ids), n_kv_heads, head_dim];
         zeros where an id is out of range."""
         h = self.heads
-        lo, hi = (torch.zeros((h.n_layers, block_ids.numel(), h.n_kv_heads, h.head_dim), dtype=torch.bfloat16, device=self.kv.device)
+        lo, hi = (torch.empty((h.n_layers, block_ids.numel(), h.n_kv_heads, h.head_dim), dtype=torch.bfloat16, device=self.kv.device)
                   for _ in range(2))
         B.llm42_kv_bounds_read(h, self._kept_bounds(), self.num_blocks, block_ids, lo, hi)
         return lo, hi
