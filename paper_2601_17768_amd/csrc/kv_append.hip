@@ -8,6 +8,10 @@ using namespace paged;
 
 namespace {
 
+#ifndef Q_HEADS
+#define Q_HEADS 8
+#endif
+
 // One thread per (position, pair): the angle and its functions in 64 bits.
 __global__ __launch_bounds__(256) void rope_table_kernel(const double* __restrict__ freq, double factor, int pairs, int64_t all,
                                                          float2* __restrict__ table) {
@@ -44,91 +48,128 @@ __device__ inline u32x4 pack8(const float (&x)[8]) {
   return w;
 }
 
-// A head of HD features in HD / 8 lanes, features 8 c .. 8 c + 7 in lane c of them: its norm and its rotation, fp32.  `room`: 512 floats of
-// LDS that are this wave's own; every lane of the wave takes part.  The partner of a feature may be in any lane and at any place there (rot_dim / 2 is any
-// number), so a head goes through LDS once, element e of lane l at e * 64 + l: all lanes of a half look at one e at a time, no bank conflicts.
-template <int HD>
-__device__ inline void norm_and_rotate(float (&x)[8], const uint16_t* gain, float eps, const float2* rope, int pos, int rot_dim, int layout,
-                                       float* room, int lane) {
-  constexpr int LANES = HD / 8;
-  const int c = lane % LANES, base = lane - c;
-  if (gain) {
-    float sum = 0.f;
-#pragma unroll
-    for (int f = 0; f < 8; ++f) sum = fmaf(x[f], x[f], sum);
-#pragma unroll
-    for (int d = 1; d < LANES; d *= 2) sum += __shfl_xor(sum, d);
-    const float r = 1.0f / sqrtf(sum / HD + eps);
-    float g[8];
-    load8(g, gain + c * 8);
-#pragma unroll
-    for (int f = 0; f < 8; ++f) x[f] = x[f] * r * g[f];
-  }
-  if (!rope) return;
+// How features are paired: not at all, neighbours, halves of the whole head, halves of a part of it.
+enum class Pairs { NONE, NEAR, HALVES, PART };
+
+// What a lane with features 8 c .. 8 c + 7 needs to turn them: feature f becomes x[f] * cos[f] + partner * sin[f] (the sign of its place in the pair in sin).
+struct Turn {
+  float cos[8], sin[8];
+};
+__device__ inline void load_turn(Turn& d, Pairs pairs, const float2* rope, int pos, int rot_dim, int c) {
+  if (pairs == Pairs::NONE) return;
   const int half = rot_dim / 2;
   const float2* cs = rope + (size_t)pos * half;
-  if (layout == LLM42_ROPE_INTERLEAVED) {
-#pragma unroll
-    for (int f = 0; f < 8; f += 2) {
-      const int j = c * 4 + f / 2;
-      if (j >= half) break;
-      const float2 t = cs[j];
-      const float a = x[f], b = x[f + 1];
-      x[f] = a * t.x - b * t.y;
-      x[f + 1] = b * t.x + a * t.y;
-    }
-    return;
-  }
-#pragma unroll
-  for (int f = 0; f < 8; ++f) room[f * 64 + lane] = x[f];
-  __builtin_amdgcn_wave_barrier();
 #pragma unroll
   for (int f = 0; f < 8; ++f) {
     const int at = c * 8 + f;
-    if (at >= rot_dim) break;
-    const bool first = at < half;
-    const int other = first ? at + half : at - half;
-    const float2 t = cs[first ? at : other];
-    const float y = room[(other & 7) * 64 + base + (other >> 3)];
-    x[f] = first ? x[f] * t.x - y * t.y : x[f] * t.x + y * t.y;
+    const bool first = pairs == Pairs::NEAR ? !(f & 1) : at < half;
+    const int j = pairs == Pairs::NEAR ? at / 2 : first ? at : at - half;
+    const float2 t = cs[min(j, half - 1)];                        // (features behind rot_dim make no use of theirs)
+    d.cos[f] = t.x;
+    d.sin[f] = first ? -t.y : t.y;
   }
-  __builtin_amdgcn_wave_barrier();
 }
 
-// Status of a sequence, asked by the `lanes` neighbouring lanes that work for one row or block of it (all lanes of the wave ask together).
-__device__ inline int sequence_status(const Rows& r, int s, int len, int n, int lane, int lanes) {
-  int status = length_status(r, len, n);
+template <int LANES>
+__device__ inline float head_sum(float v) {
+  const auto with = [&](uint32_t x) __attribute__((always_inline)) { v += __uint_as_float(x); };
+  with(other_lane<kXor1>(__float_as_uint(v)));
+  with(other_lane<kXor2>(__float_as_uint(v)));
+  with(other_lane<kMirror8>(__float_as_uint(v)));
+  if constexpr (LANES == 16) with(other_lane<kMirror16>(__float_as_uint(v)));
+  return v;
+}
+
+// The norm of a head of HD features in HD / 8 lanes, fp32.
+template <int HD>
+__device__ inline void norm(float (&x)[8], const float (&gain)[8], float eps) {
+  float sum = 0.f;
+#pragma unroll
+  for (int f = 0; f < 8; ++f) sum = fmaf(x[f], x[f], sum);
+  const float r = 1.0f / sqrtf(head_sum<HD / 8>(sum) / HD + eps);
+#pragma unroll
+  for (int f = 0; f < 8; ++f) x[f] = x[f] * r * gain[f];
+}
+
+// Its rotation, fp32; every lane of the wave takes part.  Halves of the whole head: the partner is at the same place of the lane half a head away.  Of a part: it may be in any
+// lane and at any place there (rot_dim / 2 is any number), so a head goes through `room`, 512 floats of LDS that are this wave's own, element e of lane l
+// at e * 64 + l: all lanes of a half look at one e at a time, no bank conflicts.
+template <int HD>
+__device__ inline void rotate(float (&x)[8], const Turn& t, Pairs pairs, int rot_dim, float* room, int lane) {
+  constexpr int LANES = HD / 8;
+  const int c = lane % LANES, base = lane - c, half = rot_dim / 2;
+  float y[8];
+  if (pairs == Pairs::NONE) return;
+  if (pairs == Pairs::NEAR) {
+#pragma unroll
+    for (int f = 0; f < 8; ++f) y[f] = x[f ^ 1];
+  } else if (pairs == Pairs::HALVES) {
+#pragma unroll
+    for (int f = 0; f < 8; ++f) {
+      const uint32_t u = __float_as_uint(x[f]);
+      y[f] = __uint_as_float(LANES == 16 ? other_lane<kXor8>(u) : other_lane<kMirror4>(other_lane<kMirror8>(u)));
+    }
+  } else {
+#pragma unroll
+    for (int f = 0; f < 8; ++f) room[f * 64 + lane] = x[f];
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int f = 0; f < 8; ++f) {
+      const int at = c * 8 + f, other = at < half ? at + half : at < rot_dim ? at - half : at;
+      y[f] = room[(other & 7) * 64 + base + (other >> 3)];
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+#pragma unroll
+  for (int f = 0; f < 8; ++f)
+    if (c * 8 + f < rot_dim) x[f] = fmaf(y[f], t.sin[f], x[f] * t.cos[f]);
+}
+
+// Whether a block that a row of a sequence (in order by its lengths, or without rows) lies in has no entry in the table, asked by the `lanes` neighbouring lanes that work
+// for it (all lanes of the wave ask together).
+__device__ inline bool bad_block(const Rows& r, int s, int len, int n, int lane, int lanes) {
   bool bad = false;
-  if (status == LLM42_SEQ_OK && n > 0)
+  if (n > 0)
     for (int b = len / LLM42_KV_BLOCK + lane % lanes; b <= (len + n - 1) / LLM42_KV_BLOCK; b += lanes) {
       const int id = r.block_table[(size_t)s * r.width + b];
       bad |= id < 0 || id >= r.num_blocks;
     }
   const uint64_t mine = (lanes == 64 ? ~0ull : ((1ull << lanes) - 1)) << (lane - lane % lanes);
-  if (__ballot(bad) & mine) status = LLM42_SEQ_BAD_BLOCK;
-  return status;
+  return (__ballot(bad) & mine) != 0;
 }
 
-// The launch's first workgroups take a (sequence, block, kv head) of K or of V per wave, the others a (row, head) of Q per HD / 8 lanes.
+// The launch's first workgroups take a (sequence, block, kv head) of K or of V per wave, the others a row and some heads of Q per HD / 8 lanes: its position's
+// cos and sin are read once for them.
 template <int HD, typename T>
-__global__ __launch_bounds__(256) void append_kernel(Append a, int slots, unsigned kv_groups) {
+__global__ __launch_bounds__(256) void append_kernel(Append a, Pairs pairs, int slots, unsigned kv_groups, int q_heads) {
   constexpr int LANES = HD / 8, UNITS = 64 / LANES, N = HD / 32, PAD = HD + 4;
   __shared__ float room[4][512];
   __shared__ __align__(16) uint16_t values[4][16 * PAD];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, c = lane % LANES, unit = lane / LANES;
   const Rows& r = a.rows;
+  float gain[8];
+  Turn turn;
   if (blockIdx.x >= kv_groups) {
-    const int64_t all = (int64_t)r.num_seqs * r.window * a.n_q_heads;
-    const int64_t at = ((int64_t)(blockIdx.x - kv_groups) * 4 + wave) * UNITS + unit;
-    const bool there = at < all;
-    const int64_t row = (there ? at : all - 1) / a.n_q_heads;
-    const int h = (int)((there ? at : all - 1) % a.n_q_heads), s = (int)(row / r.window), i = (int)(row % r.window);
-    float x[8];
-    load8(x, (const T*)a.q + row * a.q_stride + h * HD + c * 8);
+    const int per_row = (a.n_q_heads + q_heads - 1) / q_heads;
+    const int64_t all = (int64_t)r.num_seqs * r.window * per_row, mine = ((int64_t)(blockIdx.x - kv_groups) * 4 + wave) * UNITS + unit;
+    const int64_t row = min(mine, all - 1) / per_row;
+    const int h0 = (int)(min(mine, all - 1) % per_row) * q_heads, s = (int)(row / r.window), i = (int)(row % r.window);
+    const T* src = (const T*)a.q + row * a.q_stride + c * 8;
+    float x[8], next[8];
+    load8(next, src + h0 * HD);
+    if (a.q_norm) load8(gain, a.q_norm + c * 8);
     const int len = r.seq_len[s], n = r.seq_n ? r.seq_n[s] : r.window;
-    const bool live = sequence_status(r, s, len, n, lane, LANES) == LLM42_SEQ_OK && i < n && there;
-    norm_and_rotate<HD>(x, a.q_norm, a.eps, a.rope, live ? len + i : 0, a.rot_dim, a.layout, room[wave], lane);
-    if (live) *(u32x4*)(a.q_out + row * a.q_out_stride + h * HD + c * 8) = pack8(x);
+    bool live = mine < all && length_status(r, len, n) == LLM42_SEQ_OK && i < n;
+    load_turn(turn, pairs, a.rope, live ? len + i : 0, a.rot_dim, c);
+    if (bad_block(r, s, len, live ? n : 0, lane, LANES)) live = false;
+    for (int h = h0; h < h0 + q_heads; ++h) {                     // (heads behind the last one repeat it)
+#pragma unroll
+      for (int f = 0; f < 8; ++f) x[f] = next[f];
+      if (h + 1 < h0 + q_heads) load8(next, src + min(h + 1, a.n_q_heads - 1) * HD);
+      if (a.q_norm) norm<HD>(x, gain, a.eps);
+      rotate<HD>(x, turn, pairs, a.rot_dim, room[wave], lane);
+      if (live && h < a.n_q_heads) *(u32x4*)(a.q_out + row * a.q_out_stride + h * HD + c * 8) = pack8(x);
+    }
     return;
   }
   const int64_t item = (int64_t)blockIdx.x * 4 + wave;
@@ -136,7 +177,8 @@ __global__ __launch_bounds__(256) void append_kernel(Append a, int slots, unsign
   const int h = (int)(item / 2 % a.n_kv_heads), slot = (int)(item / 2 / a.n_kv_heads % slots), s = (int)(item / 2 / a.n_kv_heads / slots);
   if (s >= r.num_seqs) return;
   const int len = r.seq_len[s], n = r.seq_n ? r.seq_n[s] : r.window;
-  const int status = sequence_status(r, s, len, n, lane, 64);
+  int status = length_status(r, len, n);
+  if (bad_block(r, s, len, status == LLM42_SEQ_OK ? n : 0, lane, 64)) status = LLM42_SEQ_BAD_BLOCK;
   if (a.seq_status && slot == 0 && h == 0 && !is_v && lane == 0) a.seq_status[s] = status;
   if (status != LLM42_SEQ_OK || n == 0) return;
   const int block = len / LLM42_KV_BLOCK + slot, end = len + n;
@@ -180,14 +222,18 @@ __global__ __launch_bounds__(256) void append_kernel(Append a, int slots, unsign
   }
   uint16_t* tile = a.k_plane + at * 16 * HD;
   u32x4 key[N];
+  if (a.k_norm) load8(gain, a.k_norm + c * 8);
 #pragma unroll
   for (int j = 0; j < N; ++j) {
     const int t = j * UNITS + unit;
     if ((j + 1) * UNITS <= lo || j * UNITS >= hi) continue;       // (none of these tokens, for the whole wave)
     const bool live = t >= lo && t < hi;
+    const int from = min(max(t, lo), hi - 1);
     float x[8];
-    load8(x, (const T*)a.k + (row0 + min(max(t, lo), hi - 1)) * a.k_stride + h * HD + c * 8);
-    norm_and_rotate<HD>(x, a.k_norm, a.eps, a.rope, live ? block * 16 + t : len, a.rot_dim, a.layout, room[wave], lane);
+    load8(x, (const T*)a.k + (row0 + from) * a.k_stride + h * HD + c * 8);
+    load_turn(turn, pairs, a.rope, block * 16 + from, a.rot_dim, c);
+    if (a.k_norm) norm<HD>(x, gain, a.eps);
+    rotate<HD>(x, turn, pairs, a.rot_dim, room[wave], lane);
     key[j] = pack8(x);
     if (live) *(u32x4*)(tile + (c * 16 + t) * 8) = key[j];
   }
@@ -210,9 +256,12 @@ void launch_rope_table(const double* freq, double factor, int pairs, int max_pos
 void launch_kv_append(const Append& a, hipStream_t st) {
   const Rows& r = a.rows;
   const int slots = slots_of(r.window, r.width), units = 4 * (512 / a.head_dim);
-  const unsigned kv = (unsigned)(((int64_t)r.num_seqs * slots * a.n_kv_heads * 2 + 3) / 4);
-  const unsigned q = a.q ? (unsigned)(((int64_t)r.num_seqs * r.window * a.n_q_heads + units - 1) / units) : 0;
-  const auto go = [&](auto kernel) { kernel<<<kv + q, 256, 0, st>>>(a, slots, kv); };
+  const int64_t rows = (int64_t)r.num_seqs * r.window;
+  const Pairs pairs = !a.rope ? Pairs::NONE : a.layout == LLM42_ROPE_INTERLEAVED ? Pairs::NEAR : a.rot_dim == a.head_dim ? Pairs::HALVES : Pairs::PART;
+  const int q_heads = rows * a.n_q_heads <= 32768 ? 1 : Q_HEADS;
+  const unsigned kv = (unsigned)((rows / r.window * slots * a.n_kv_heads * 2 + 3) / 4);
+  const unsigned q = a.q ? (unsigned)((rows * ((a.n_q_heads + q_heads - 1) / q_heads) + units - 1) / units) : 0;
+  const auto go = [&](auto kernel) { kernel<<<kv + q, 256, 0, st>>>(a, pairs, slots, kv, q_heads); };
   if (a.head_dim == 128) a.type == LLM42_F32 ? go(append_kernel<128, float>) : go(append_kernel<128, uint16_t>);
   else a.type == LLM42_F32 ? go(append_kernel<64, float>) : go(append_kernel<64, uint16_t>);
 }

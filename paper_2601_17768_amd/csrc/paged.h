@@ -48,10 +48,10 @@ __device__ inline float power_of_two(int e) { return __uint_as_float((uint32_t)(
 __device__ inline float lo_bf16(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ inline float hi_bf16(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 
-// The value of another lane of the same 16: l ^ 1, l ^ 2, the mirrored one of its 8 or 16, l ^ 8.
+// The value of another lane of the same 16: l ^ 1, l ^ 2, the mirrored one of its 4, 8 or 16, l ^ 8.
 template <int CTRL>
 __device__ inline uint32_t other_lane(uint32_t x) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, true); }
-constexpr int kXor1 = 0xB1, kXor2 = 0x4E, kMirror8 = 0x141, kMirror16 = 0x140, kXor8 = 0x128;
+constexpr int kXor1 = 0xB1, kXor2 = 0x4E, kMirror4 = 0x1B, kMirror8 = 0x141, kMirror16 = 0x140, kXor8 = 0x128;
 // f over a value and the same lanes' of the other 16 of its 32, and of the other 32: for all of the wave's groups of 16 lanes alike.
 template <class F>
 __device__ inline float over_rows(float x, F f) {
