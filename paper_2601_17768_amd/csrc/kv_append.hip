@@ -22,23 +22,32 @@ __global__ __launch_bounds__(256) void rope_table_kernel(const double* __restric
   table[at] = make_float2((float)(c * factor), (float)(s * factor));
 }
 
+// Eight neighbouring features as they lie in memory, and as fp32.
 template <typename T>
-__device__ inline void load8(float (&x)[8], const T* p) {
-  if constexpr (std::is_same_v<T, float>) {
-    const f32x4 a = *(const f32x4*)p, b = *(const f32x4*)(p + 4);
+struct Eight {
+  u32x4 w[sizeof(T) / 2];
+  __device__ inline void load(const T* p) {
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) w[i] = ((const u32x4*)p)[i];
+  }
+  __device__ inline void get(float (&x)[8]) const {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      x[i] = a[i];
-      x[4 + i] = b[i];
-    }
-  } else {
-    const u32x4 w = *(const u32x4*)p;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[2 * i] = lo_bf16(w[i]);
-      x[2 * i + 1] = hi_bf16(w[i]);
+      if constexpr (sizeof(T) == 4) {
+        x[i] = __uint_as_float(w[0][i]);
+        x[4 + i] = __uint_as_float(w[1][i]);
+      } else {
+        x[2 * i] = lo_bf16(w[0][i]);
+        x[2 * i + 1] = hi_bf16(w[0][i]);
+      }
     }
   }
+};
+template <typename T>
+__device__ inline void load8(float (&x)[8], const T* p) {
+  Eight<T> d;
+  d.load(p);
+  d.get(x);
 }
 
 __device__ inline u32x4 pack8(const float (&x)[8]) {
@@ -59,6 +68,33 @@ __device__ inline void load_turn(Turn& d, Pairs pairs, const float2* rope, int p
   if (pairs == Pairs::NONE) return;
   const int half = rot_dim / 2;
   const float2* cs = rope + (size_t)pos * half;
+  if (pairs == Pairs::HALVES) {                                   // (half is 32 or 64: rows of the table are 16-byte aligned)
+    const bool first = c * 8 < half;
+    const f32x4* p = (const f32x4*)(cs + (first ? c * 8 : c * 8 - half));
+#pragma unroll
+    for (int f = 0; f < 8; f += 2) {
+      const f32x4 t = p[f / 2];
+      d.cos[f] = t[0];
+      d.sin[f] = first ? -t[1] : t[1];
+      d.cos[f + 1] = t[2];
+      d.sin[f + 1] = first ? -t[3] : t[3];
+    }
+    return;
+  }
+  if (pairs == Pairs::NEAR && half % 4 == 0) {
+    const f32x4* p = (const f32x4*)(cs + min(c * 4, half - 4));
+#pragma unroll
+    for (int f = 0; f < 8; f += 4) {
+      const f32x4 t = p[f / 4];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        d.cos[f + 2 * i] = d.cos[f + 2 * i + 1] = t[2 * i];
+        d.sin[f + 2 * i] = -t[2 * i + 1];
+        d.sin[f + 2 * i + 1] = t[2 * i + 1];
+      }
+    }
+    return;
+  }
 #pragma unroll
   for (int f = 0; f < 8; ++f) {
     const int at = c * 8 + f;
@@ -155,17 +191,17 @@ __global__ __launch_bounds__(256) void append_kernel(Append a, Pairs pairs, int 
     const int64_t row = min(mine, all - 1) / per_row;
     const int h0 = (int)(min(mine, all - 1) % per_row) * q_heads, s = (int)(row / r.window), i = (int)(row % r.window);
     const T* src = (const T*)a.q + row * a.q_stride + c * 8;
-    float x[8], next[8];
-    load8(next, src + h0 * HD);
+    Eight<T> next;
+    next.load(src + h0 * HD);
     if (a.q_norm) load8(gain, a.q_norm + c * 8);
     const int len = r.seq_len[s], n = r.seq_n ? r.seq_n[s] : r.window;
     bool live = mine < all && length_status(r, len, n) == LLM42_SEQ_OK && i < n;
     load_turn(turn, pairs, a.rope, live ? len + i : 0, a.rot_dim, c);
     if (bad_block(r, s, len, live ? n : 0, lane, LANES)) live = false;
     for (int h = h0; h < h0 + q_heads; ++h) {                     // (heads behind the last one repeat it)
-#pragma unroll
-      for (int f = 0; f < 8; ++f) x[f] = next[f];
-      if (h + 1 < h0 + q_heads) load8(next, src + min(h + 1, a.n_q_heads - 1) * HD);
+      float x[8];
+      next.get(x);
+      if (h + 1 < h0 + q_heads) next.load(src + min(h + 1, a.n_q_heads - 1) * HD);
       if (a.q_norm) norm<HD>(x, gain, a.eps);
       rotate<HD>(x, turn, pairs, a.rot_dim, room[wave], lane);
       if (live && h < a.n_q_heads) *(u32x4*)(a.q_out + row * a.q_out_stride + h * HD + c * 8) = pack8(x);
@@ -190,12 +226,15 @@ __global__ __launch_bounds__(256) void append_kernel(Append a, Pairs pairs, int 
   if (is_v) {
     uint16_t* tile = a.v_plane + at * 16 * HD;
     uint16_t* mine = values[wave];
+    Eight<T> in[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) in[j].load((const T*)a.v + (row0 + min(max(j * UNITS + unit, lo), hi - 1)) * a.v_stride + h * HD + c * 8);
 #pragma unroll
     for (int j = 0; j < N; ++j) {
       const int t = j * UNITS + unit;
       if (t < lo || t >= hi) continue;
       float x[8];
-      load8(x, (const T*)a.v + (row0 + t) * a.v_stride + h * HD + c * 8);
+      in[j].get(x);
       const u32x4 w = pack8(x);
       *(u32x2*)(mine + t * PAD + c * 8) = (u32x2){w[0], w[1]};
       *(u32x2*)(mine + t * PAD + c * 8 + 4) = (u32x2){w[2], w[3]};
@@ -222,6 +261,9 @@ __global__ __launch_bounds__(256) void append_kernel(Append a, Pairs pairs, int 
   }
   uint16_t* tile = a.k_plane + at * 16 * HD;
   u32x4 key[N];
+  Eight<T> in[N];
+#pragma unroll
+  for (int j = 0; j < N; ++j) in[j].load((const T*)a.k + (row0 + min(max(j * UNITS + unit, lo), hi - 1)) * a.k_stride + h * HD + c * 8);
   if (a.k_norm) load8(gain, a.k_norm + c * 8);
 #pragma unroll
   for (int j = 0; j < N; ++j) {
@@ -230,7 +272,7 @@ __global__ __launch_bounds__(256) void append_kernel(Append a, Pairs pairs, int 
     const bool live = t >= lo && t < hi;
     const int from = min(max(t, lo), hi - 1);
     float x[8];
-    load8(x, (const T*)a.k + (row0 + from) * a.k_stride + h * HD + c * 8);
+    in[j].get(x);
     load_turn(turn, pairs, a.rope, block * 16 + from, a.rot_dim, c);
     if (a.k_norm) norm<HD>(x, gain, a.eps);
     rotate<HD>(x, turn, pairs, a.rot_dim, room[wave], lane);
