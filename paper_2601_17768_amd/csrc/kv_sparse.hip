@@ -39,7 +39,7 @@ __global__ __launch_bounds__(64 * NW) void sparse_attention_kernel(SparseAttenti
   extern __shared__ int2 sh_list[];                               // [entry of the part, made even]: physical block (-1: none), keys that are seen of it
   __shared__ float sh_ml[NW][2][16];
   __shared__ f32x4 sh_acc[NW][64 * FB];
-  __shared__ int sh_any;
+  __shared__ int sh_used[NW];                                     // entries up to the last one that is a block, among those that a wave looks at
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, g = lane >> 4, l16 = lane & 15;
   const Rows& r = a.rows;
   const int part = blockIdx.x % a.parts, row = blockIdx.x / a.parts, kvh = blockIdx.y, s = row / r.window, i = row % r.window;
@@ -48,20 +48,20 @@ __global__ __launch_bounds__(64 * NW) void sparse_attention_kernel(SparseAttenti
   const int pos = len + i, own = pos / LLM42_KV_BLOCK;
   const int begin = part * a.per_part, count = min(a.width - begin, a.per_part);
   const size_t at = (size_t)row * a.n_kv_heads + kvh, slot = at * a.parts + part;
-  if (threadIdx.x == 0) sh_any = 0;
-  __syncthreads();
-  bool bad = false, any = false;
-  for (int e = threadIdx.x; e < ((count + 1) & ~1); e += 64 * NW) {
+  bool bad = false;
+  int used = 0;
+  for (int e0 = wave * 64; e0 < ((count + 1) & ~1); e0 += 64 * NW) {
+    const int e = e0 + lane, b = e < count ? a.selected[at * a.width + begin + e] : -1;
     int2 x = make_int2(-1, 0);
-    const int b = e < count ? a.selected[at * a.width + begin + e] : -1;
     if (b >= 0 && b <= own) {
       x = make_int2(r.block_table[(size_t)s * r.width + b], min(pos - b * LLM42_KV_BLOCK + 1, 16));
       bad |= x.x < 0 || x.x >= r.num_blocks;
-      any = true;
     }
-    sh_list[e] = x;
+    if (e < ((count + 1) & ~1)) sh_list[e] = x;
+    const uint64_t there = __ballot(x.y > 0);
+    if (there) used = e0 + 64 - __clzll((long long)there);
   }
-  if (any) sh_any = 1;
+  if (lane == 0) sh_used[wave] = used;
   bad = __syncthreads_or(bad);
   if (a.parts > 1 && threadIdx.x == 0) a.part_ok[slot] = !bad;
   if (bad) return;
@@ -81,11 +81,14 @@ __global__ __launch_bounds__(64 * NW) void sparse_attention_kernel(SparseAttenti
 #pragma unroll
   for (int f = 0; f < FB; ++f) acc[f] = (f32x4){0.f, 0.f, 0.f, 0.f};
   float m = -INFINITY, l = 0.f;
-  const int pairs = (count + 1) / 2;
+  used = 0;
+#pragma unroll
+  for (int v = 0; v < NW; ++v) used = max(used, sh_used[v]);
+  const int pairs = __builtin_amdgcn_readfirstlane((used + 1) / 2);
   const int64_t to_block = (int64_t)a.n_kv_heads * 16 * HD;
   const uint16_t *kp = a.k_plane + (int64_t)kvh * 16 * HD, *vp = a.v_plane + (int64_t)kvh * 16 * HD;
   for (int p = wave; p < pairs; p += NW) {
-    int2 x[2] = {sh_list[2 * p], sh_list[2 * p + 1]};
+    const int2 x[2] = {sh_list[2 * p], sh_list[2 * p + 1]};
     if (x[0].x < 0 && x[1].x < 0) continue;
     Pair<HD> d;
 #pragma unroll
@@ -170,8 +173,8 @@ __global__ __launch_bounds__(64 * NW) void sparse_attention_kernel(SparseAttenti
   if (l16 >= a.group) return;
   if (a.parts > 1 && wave == 0 && g == 0) {
     float* o = a.part_ml + (slot * a.group + l16) * 2;
-    o[0] = sh_any ? top : INFINITY;                               // (a part without keys: see the join)
-    o[1] = sh_any ? sum : -1.f;
+    o[0] = top;
+    o[1] = used ? sum : -1.f;                                 // (a part without keys: see the join)
   }
   for (int f = wave; f < FB; f += NW) {                           // features 16 f + 4 g .. + 3
     f32x4 x = {0.f, 0.f, 0.f, 0.f};
@@ -181,14 +184,14 @@ __global__ __launch_bounds__(64 * NW) void sparse_attention_kernel(SparseAttenti
       *(f32x4*)(a.part_acc + (slot * a.group + l16) * HD + f * 16 + g * 4) = x;
       continue;
     }
-    const u32x2 packed = sh_any ? (u32x2){pack2_bf16(x[0] / sum, x[1] / sum), pack2_bf16(x[2] / sum, x[3] / sum)} : (u32x2){0, 0};
+    const u32x2 packed = used ? (u32x2){pack2_bf16(x[0] / sum, x[1] / sum), pack2_bf16(x[2] / sum, x[3] / sum)} : (u32x2){0, 0};
     const int col = (kvh * a.group + l16) * HD + f * 16 + g * 4;
     if constexpr (TILES) *(u32x2*)(a.out + pk_off(s, col, a.n_kv_heads * a.group * HD)) = packed;
     else *(u32x2*)(a.out + (int64_t)row * a.out_stride + col) = packed;
   }
 }
 
-// One wave per (row, kv head, head): the parts of its list, first to last.
+// One wave per (row, kv head, head): the parts of its list, at most 64, a part's maximum and sum in a lane each.
 template <int HD, bool TILES>
 __global__ __launch_bounds__(256) void sparse_join_kernel(SparseAttention a) {
   const Rows& r = a.rows;
@@ -198,25 +201,24 @@ __global__ __launch_bounds__(256) void sparse_join_kernel(SparseAttention a) {
   const int s = row / r.window, i = row % r.window, len = r.seq_len[s], n = r.seq_n ? r.seq_n[s] : r.window;
   if (length_status(r, len, n) != LLM42_SEQ_OK || i >= n) return;
   const size_t slot0 = ((size_t)row * a.n_kv_heads + kvh) * a.parts;
-  float top = -INFINITY;
-  bool any = false;
-  for (int p = 0; p < a.parts; ++p) {
-    if (!a.part_ok[slot0 + p]) return;
-    const float* ml = a.part_ml + ((slot0 + p) * a.group + h) * 2;
-    if (ml[1] == -1.f) continue;
-    any = true;
-    top = fmaxf(top, ml[0]);
-  }
-  const float ref = top == -INFINITY ? 0.f : top;
+  const bool mine = lane < a.parts;
+  const size_t slot = slot0 + (mine ? lane : 0);
+  const int ok = a.part_ok[slot];
+  const float part_top = a.part_ml[(slot * a.group + h) * 2], part_sum = a.part_ml[(slot * a.group + h) * 2 + 1];
+  if (__any(!ok)) return;                                         // (the parts of such a list wrote nothing else)
+  const bool used = mine && part_sum != -1.f;
+  const float top = over_rows(over_lanes(used ? part_top : -INFINITY, [](float x, float y) { return fmaxf(x, y); }), [](float x, float y) { return fmaxf(x, y); });
+  const bool any = __any(used);
+  const float w = used ? __builtin_amdgcn_exp2f(part_top - (top == -INFINITY ? 0.f : top)) : 0.f;
   constexpr int E = HD / 64;
   float o[E] = {}, sum = 0.f;
   for (int p = 0; p < a.parts; ++p) {
-    const float* ml = a.part_ml + ((slot0 + p) * a.group + h) * 2;
-    if (ml[1] == -1.f) continue;
-    const float w = __builtin_amdgcn_exp2f(ml[0] - ref);
-    sum += w * ml[1];
+    if (!(__ballot(used) >> p & 1)) continue;
+    const float wp = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), p));
+    sum += wp * __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(part_sum), p));
+    const float* acc = a.part_acc + ((slot0 + p) * a.group + h) * HD + lane * E;
 #pragma unroll
-    for (int e = 0; e < E; ++e) o[e] += w * a.part_acc[((slot0 + p) * a.group + h) * HD + lane * E + e];
+    for (int e = 0; e < E; ++e) o[e] += wp * acc[e];
   }
   const int col = (kvh * a.group + h) * HD + lane * E;
   uint16_t* out = TILES ? a.out + pk_off(s, col, a.n_kv_heads * a.group * HD) : a.out + (int64_t)row * a.out_stride + col;
@@ -243,22 +245,32 @@ __global__ __launch_bounds__(256) void sparse_status_kernel(SparseAttention a) {
   if (threadIdx.x == 0) a.seq_status[s] = bad ? LLM42_SEQ_BAD_BLOCK : status;
 }
 
-constexpr int kWaves = 4;
+constexpr int kMostPart = 1024;   // entries of a part: 8 KiB of LDS
 
 template <int HD, bool TILES>
 void launch(const SparseAttention& a, hipStream_t st) {
   const int rows = a.rows.num_seqs * a.rows.window;
   const float scale_log2 = 1.4426950408889634f * (a.scale > 0.f ? a.scale : 1.0f / sqrtf((float)HD));
   if (a.seq_status) sparse_status_kernel<<<a.rows.num_seqs, 256, 0, st>>>(a);
-  sparse_attention_kernel<kWaves, HD, TILES><<<dim3(rows * a.parts, a.n_kv_heads), 64 * kWaves, sizeof(int2) * ((a.per_part + 1) & ~1), st>>>(a, scale_log2);
+  const dim3 grid(rows * a.parts, a.n_kv_heads);
+  const size_t lds = sizeof(int2) * ((a.per_part + 1) & ~1);
+  // (eight waves where a CU has no second workgroup: us by eight / four, sequences x 64 blocks, 1 9.6 / 10.4, 8 11.0 / 14.0, 16 14.1 / 15.3, 24 19.3 / 19.3)
+  if ((int64_t)grid.x * grid.y <= a.num_cus) sparse_attention_kernel<8, HD, TILES><<<grid, 512, lds, st>>>(a, scale_log2);
+  else sparse_attention_kernel<4, HD, TILES><<<grid, 256, lds, st>>>(a, scale_log2);
   if (a.parts > 1) sparse_join_kernel<HD, TILES><<<dim3((unsigned)(((int64_t)rows * a.group + 3) / 4), a.n_kv_heads), 256, 0, st>>>(a);
 }
 
 }  // namespace
 
 void plan_sparse_attention(int rows, int n_kv_heads, int head_dim, int width, int num_cus, int& parts, int& per_part) {
-  // (simplest: lists of up to 256 blocks whole)
-  per_part = std::min(width, 256);
+  // A list is cut where that spreads it over an idle device: a CU takes about 1.4 us for every 16 of its blocks, the join 3 (us whole / in parts of 32 / 64 blocks,
+  // sequences x blocks, 8 kv heads of 128, group 4: 1 x 64 9.6 / 9.9, 1 x 128 15.1 / 10.9, 1 x 256 25.8 / 12.4 / 14.1, 1 x 1024 in parts of 256 / 32 / 64
+  // 31 / 25 / 21, 4 x 256 27 / 18.9 / 17.9, 16 x 256 55 / 48.7 / 47.8; but 16 x 64 14.2 / 17.6, 32 x 256 99 / 108 / 105, 128 x 128 194 / 204 / 200).
+  const int64_t lists = (int64_t)rows * n_kv_heads, want = 4 * lists < num_cus ? num_cus / 2 : num_cus;
+  int parts_ = lists < num_cus && width >= 96 ? (int)((want + lists - 1) / lists) : 1;
+  parts_ = std::max(parts_, (width + kMostPart - 1) / kMostPart);
+  per_part = std::max(std::min(width, 32), (width + parts_ - 1) / parts_ + 1 & ~1);
+  per_part = std::max(per_part, (width + 63) / 64);              // (the join has a lane for every part)
   parts = (width + per_part - 1) / per_part;
 }
 

@@ -52,6 +52,14 @@ __device__ inline float hi_bf16(uint32_t w) { return __uint_as_float(w & 0xFFFF0
 template <int CTRL>
 __device__ inline uint32_t other_lane(uint32_t x) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, true); }
 constexpr int kXor1 = 0xB1, kXor2 = 0x4E, kMirror4 = 0x1B, kMirror8 = 0x141, kMirror16 = 0x140, kXor8 = 0x128;
+// f over the 16 lanes of a group.
+template <class F>
+__device__ inline float over_lanes(float x, F f) {
+  x = f(x, __uint_as_float(other_lane<kXor1>(__float_as_uint(x))));
+  x = f(x, __uint_as_float(other_lane<kXor2>(__float_as_uint(x))));
+  x = f(x, __uint_as_float(other_lane<kMirror8>(__float_as_uint(x))));
+  return f(x, __uint_as_float(other_lane<kMirror16>(__float_as_uint(x))));
+}
 // f over a value and the same lanes' of the other 16 of its 32, and of the other 32: for all of the wave's groups of 16 lanes alike.
 template <class F>
 __device__ inline float over_rows(float x, F f) {
@@ -162,7 +170,8 @@ struct SparseAttention {
   int n_kv_heads, group, head_dim;
   const int32_t* selected;
   int width;                   // entries of a list
-  int parts, per_part;         // launches' split of a list
+  int parts, per_part;         // workgroups of a list, and entries of each
+  int num_cus;
   float scale;
   float *part_acc, *part_ml;   // [row][kv head][part][head][head_dim], [..][2]
   int32_t* part_ok;            // [row][kv head][part]

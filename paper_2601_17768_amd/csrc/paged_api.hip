@@ -394,7 +394,8 @@ llm42_status llm42_kv_sparse_attention(const llm42_heads* heads, int32_t layer, 
   a.width = width;
   a.scale = scale;
   a.seq_status = seq_status;
-  plan_sparse_attention(num_seqs * window, a.n_kv_heads, a.head_dim, width, current_cus(), a.parts, a.per_part);
+  a.num_cus = current_cus();
+  plan_sparse_attention(num_seqs * window, a.n_kv_heads, a.head_dim, width, a.num_cus, a.parts, a.per_part);
   const SparseWorkspace ws = carve(heads, num_seqs * window, a.parts, (char*)workspace);
   if (llm42_status st = check_workspace(who, workspace, workspace_bytes, a.parts > 1 ? ws.bytes : 0)) return st;
   a.part_acc = ws.acc;
