@@ -214,6 +214,32 @@ llm42_status llm42_kv_sparse_attention(
     size_t                workspace_bytes,
     void*                 hip_stream);
 
+/* ---- the fast path ---------------------------------------------------------------------------------------- */
+
+/* llm42_decode_step_sampled with attention over selected blocks: the same arguments, effects, errors and status, and for each sequence, layer and kv
+ * head llm42_kv_select's choice of `budget` blocks (sequences of no more blocks read all of them) in kv_bounds, the bounds of kv_cache (its model's numbers as llm42_heads).
+ * Those of blocks that are whole below seq_lens[s] must have been stored; the step stores those of a block that its token makes whole.
+ * The verifier overwrites the window's entries of the cache; llm42_kv_bounds_store behind the commit follows it.
+ * workspace: llm42_decode_step_sparse_workspace_bytes for any call of 1 .. max_seqs sequences, contexts up to max_context and this budget;
+ * 256-byte aligned. */
+llm42_status llm42_decode_step_sparse_workspace_bytes(const llm42_model* model, int32_t max_seqs, int32_t max_context, int32_t budget,
+                                                      size_t* out_bytes);
+llm42_status llm42_decode_step_sparse(
+    const llm42_model*    model,
+    const llm42_kv_cache* kv_cache,
+    void*                 kv_bounds,       /* dev, 16-byte aligned                         */
+    int32_t               budget,          /* as in llm42_kv_select                        */
+    int32_t               sink,
+    int32_t               recent,
+    const int32_t*        seq_lens,        /* dev [num_seqs]                               */
+    const int32_t*        tokens,          /* dev [num_seqs]                               */
+    int32_t               num_seqs,
+    int32_t               max_context,     /* up to 2^30                                   */
+    int32_t*              out_tokens,      /* dev [num_seqs]                               */
+    int32_t*              seq_status,      /* dev [num_seqs] or NULL                       */
+    void* workspace, size_t workspace_bytes, void* hip_stream,
+    const llm42_sampling* sampling);       /* or NULL                                      */
+
 #ifdef __cplusplus
 }
 #endif

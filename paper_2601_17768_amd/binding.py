@@ -38,7 +38,7 @@ EXPORTS = ("llm42_model_create", "llm42_model_destroy", "llm42_kv_bytes", "llm42
            "llm42_mx4_model_create", "llm42_mx4_model_destroy", "llm42_decode_step_mx4_workspace_bytes", "llm42_decode_step_mx4",
            "llm42_heads_kv_bytes", "llm42_rope_create", "llm42_rope_destroy", "llm42_kv_append", "llm42_kv_bounds_bytes", "llm42_kv_bounds_store",
            "llm42_kv_bounds_read", "llm42_kv_select_workspace_bytes", "llm42_kv_select", "llm42_kv_sparse_attention_workspace_bytes",
-           "llm42_kv_sparse_attention")
+           "llm42_kv_sparse_attention", "llm42_decode_step_sparse_workspace_bytes", "llm42_decode_step_sparse")
 KERNEL_CLASSES = ("prepare", "embed", "rmsnorm", "qkv", "attention", "o_proj", "gate_up", "down", "lm_head",
                   "argmax", "commit")
 
@@ -164,6 +164,8 @@ def load_library(path: Optional[str] = None):
             "llm42_kv_select_workspace_bytes": [hp, i32, i32, i32, i32, size_p],
             "llm42_kv_select": [hp, i32, kvp, vp, vp, i64, vp, i32, vp, i32, i32, i32, i32, i32, vp, vp, vp, size, vp],
             "llm42_kv_sparse_attention_workspace_bytes": [hp, i32, i32, i32, size_p],
+            "llm42_decode_step_sparse_workspace_bytes": [vp, i32, i32, i32, size_p],
+            "llm42_decode_step_sparse": [vp, kvp, vp, i32, i32, i32, vp, vp, i32, i32, vp, vp, vp, size, vp, ctypes.POINTER(Sampling)],
             "llm42_kv_sparse_attention": [hp, i32, kvp, vp, i64, vp, i32, vp, i32, i32, vp, i32, f32, vp, i64, vp, vp, size, vp]}.items():
         getattr(lib, name).argtypes = args
         getattr(lib, name).restype = i32
@@ -690,6 +692,26 @@ def llm42_kv_sparse_attention(heads: Heads, layer: int, kv: torch.Tensor, num_bl
         ctypes.byref(heads), layer, ctypes.byref(view), qp, qs, _per_seq(seq_lens, num_seqs), window, _per_seq(n_valid, num_seqs), num_seqs,
         max_context, _lists(selected, num_seqs, window, heads.n_kv_heads), selected.shape[-1], scale, op, os_, _per_seq(seq_status, num_seqs),
         *_workspace(workspace), _stream_handle(stream)))
+
+
+def llm42_decode_step_sparse_workspace_bytes(model: int, max_seqs: int, max_context: int, budget: int) -> int:
+    return _asked(load_library().llm42_decode_step_sparse_workspace_bytes, model, max_seqs, max_context, budget)
+
+
+def llm42_decode_step_sparse(model: int, heads: Heads, kv_base: torch.Tensor, num_blocks: int, block_table: torch.Tensor, bounds: torch.Tensor,
+                             budget: int, sink: int, recent: int, seq_lens: torch.Tensor, tokens: torch.Tensor, max_context: int,
+                             out_tokens: torch.Tensor, workspace: torch.Tensor, seq_status: Optional[torch.Tensor] = None, stream=None,
+                             sampling: Optional[Sampling] = None) -> None:
+    """(`heads`: the model's, for the check of the bounds' size.)"""
+    num_seqs = seq_lens.numel()
+    _on_current_device(kv_base, block_table, bounds, seq_lens, tokens, out_tokens, workspace, seq_status)
+    kv = _kv_view(model, kv_base, num_blocks, block_table, num_seqs)
+    if llm42_heads_kv_bytes(heads, num_blocks) != llm42_kv_bytes(model, num_blocks):
+        raise ValueError("heads are not the model's")
+    _check(load_library().llm42_decode_step_sparse(
+        model, ctypes.byref(kv), _bounds(heads, bounds, num_blocks), budget, sink, recent, _per_seq(seq_lens, num_seqs),
+        _per_seq(tokens, num_seqs), num_seqs, max_context, _per_seq(out_tokens, num_seqs), _per_seq(seq_status, num_seqs), *_workspace(workspace),
+        _stream_handle(stream), ctypes.byref(sampling) if sampling is not None else None))
 
 
 def llm42_commit_rollback(candidates: torch.Tensor, out_tokens: torch.Tensor, n_valid: Optional[torch.Tensor],

@@ -12,6 +12,7 @@
 #include <new>
 
 #include "mx4.h"
+#include "paged.h"
 
 // Scratch area of llm42_verify_window_static: one copy per GPU that loads the library, held until the process ends.
 // In host code the array's name is only a handle for hipGetSymbolAddress; the device address it yields (one per
@@ -322,6 +323,74 @@ void attention4(const Fast4& f4, int layer, const llm42_kv_cache* kv, int num_se
   launch_kv4_attention(a, st);
 }
 
+// A decoding step with attention over selected blocks.
+struct FastSparse {
+  char* bounds;
+  int budget, sink, recent;
+  int32_t* selected;           // scratch: the lists, scores, partials
+  uint32_t* keys;
+  int parts, per_part;
+  paged::SparseWorkspace part;
+};
+
+// ... its scratch behind the workspace of a decoding step.
+size_t carve_fast_sparse(const llm42_model* m, int num_seqs, int max_context, FastSparse& f, char* base) {
+  const llm42_config& c = m->cfg;
+  const size_t lists = align_up(sizeof(int32_t) * (size_t)num_seqs * c.n_kv_heads * f.budget, 256);
+  const size_t keys = align_up(select_workspace(num_seqs, 1, c.n_kv_heads, m->group, max_context, f.budget, m->num_cus), 256);
+  plan_sparse_attention(num_seqs, c.n_kv_heads, c.head_dim, f.budget, m->num_cus, f.parts, f.per_part);
+  f.part = paged::carve_sparse(num_seqs, c.n_kv_heads, m->group, c.head_dim, f.parts, base ? base + lists + keys : nullptr);
+  f.selected = (int32_t*)base;
+  f.keys = base && keys ? (uint32_t*)(base + lists) : nullptr;
+  return lists + keys + f.part.bytes;
+}
+
+paged::Rows sparse_rows(const llm42_kv_cache* kv, int num_seqs, int max_context, const Workspace& ws) {
+  return {kv->block_table, kv->max_blocks_per_seq, kv->num_blocks, ws.seq_len, nullptr, num_seqs, 1, max_context};
+}
+
+void attention_sparse(const llm42_model* m, const FastSparse& f, int layer, const llm42_kv_cache* kv, int num_seqs, int max_context,
+                      const Workspace& ws, hipStream_t st) {
+  const llm42_config& c = m->cfg;
+  const int64_t plane = kv->num_blocks * c.n_kv_heads * 16 * c.head_dim;
+  paged::Select a;
+  memset(&a, 0, sizeof a);
+  a.rows = sparse_rows(kv, num_seqs, max_context, ws);
+  a.bounds = f.bounds + layer * kv->num_blocks * c.n_kv_heads * paged::bounds_record(c.head_dim);
+  a.q = ws.q;
+  a.tiles = true;
+  a.n_kv_heads = c.n_kv_heads;
+  a.group = m->group;
+  a.head_dim = c.head_dim;
+  a.budget = f.budget;
+  a.sink = f.sink;
+  a.recent = f.recent;
+  a.selected = f.selected;
+  a.keys = f.keys;
+  a.num_cus = m->num_cus;
+  launch_kv_select(a, st);
+  paged::SparseAttention b;
+  memset(&b, 0, sizeof b);
+  b.rows = a.rows;
+  b.k_plane = (const uint16_t*)kv->kv_base + 2 * layer * plane;
+  b.v_plane = b.k_plane + plane;
+  b.q = ws.q;
+  b.out = ws.attn;
+  b.tiles = true;
+  b.n_kv_heads = c.n_kv_heads;
+  b.group = m->group;
+  b.head_dim = c.head_dim;
+  b.selected = f.selected;
+  b.width = f.budget;
+  b.parts = f.parts;
+  b.per_part = f.per_part;
+  b.num_cus = m->num_cus;
+  b.part_acc = f.part.acc;
+  b.part_ml = f.part.ml;
+  b.part_ok = f.part.ok;
+  launch_sparse_attention(b, st);
+}
+
 // Layer l behind its attention, by the 4-bit weights; as run_mlp.
 bool run_mlp4(const Fast4& f4, int l, const Workspace& ws, hipStream_t st) {
   const llm42_model* m = f4.m4->model;
@@ -362,7 +431,8 @@ void run_head(const llm42_model* m, bool pending, int window, int num_seqs, int3
 llm42_status run_pass(const llm42_model* m, const llm42_kv_cache* kv, const int32_t* seq_lens, const int32_t* candidates,
                       int window, const int32_t* n_valid, int num_seqs, int max_context, int32_t* out_tokens,
                       int32_t* seq_status, float* out_logits, const int32_t* dump_seq_ids, int n_dump,
-                      Workspace& ws, hipStream_t st, const llm42_sampling* sampling, bool prefill_pass, const Fast4* f4 = nullptr) {
+                      Workspace& ws, hipStream_t st, const llm42_sampling* sampling, bool prefill_pass, const Fast4* f4 = nullptr,
+                      const FastSparse* fs = nullptr) {
   const llm42_config& c = m->cfg;
   const bool kv4 = f4 && f4->kv4;
   // Partly filled windows: the rows are packed, and what pads the end of the grid is skipped.  (Each workgroup of the prepare
@@ -379,7 +449,7 @@ llm42_status run_pass(const llm42_model* m, const llm42_kv_cache* kv, const int3
     // (a mirror with the bf16 cache's own table has been checked with it)
     if (f4->kv4->block_table != kv->block_table || f4->kv4->max_blocks_per_seq != kv->max_blocks_per_seq || f4->kv4->num_blocks < kv->num_blocks)
       TIMED(LLM42_K_PREPARE, launch_kv4_step_check(m, f4->kv4, num_seqs, seq_status, ws, st));
-  } else if (ws.attn_list) {
+  } else if (ws.attn_list && !fs) {
     TIMED(LLM42_K_PREPARE, launch_attention_plan(m, num_seqs, max_context, ws, st));
   }
   TIMED(LLM42_K_EMBED, launch_embed(m, candidates, window, ws, st));
@@ -390,6 +460,7 @@ llm42_status run_pass(const llm42_model* m, const llm42_kv_cache* kv, const int3
     if (f4) TIMED(LLM42_K_QKV, launch_mx4_qkv(f4->m4, l, kv, ws, st));
     else TIMED(LLM42_K_QKV, launch_gemm_qkv(m, l, kv, window, ws, st));
     if (kv4) TIMED(LLM42_K_ATTENTION, attention4(*f4, l, kv, num_seqs, max_context, ws, st));
+    else if (fs) TIMED(LLM42_K_ATTENTION, attention_sparse(m, *fs, l, kv, num_seqs, max_context, ws, st));
     else TIMED(LLM42_K_ATTENTION, launch_attention(m, l, kv, num_seqs, window, max_context, ws, st));
     if (f4) {
       pending = run_mlp4(*f4, l, ws, st);
@@ -399,6 +470,9 @@ llm42_status run_pass(const llm42_model* m, const llm42_kv_cache* kv, const int3
     pending = run_mlp(m, ly, ws, st);
   }
   run_head(m, pending, window, num_seqs, out_tokens, out_logits, sampling, ws, st, f4);
+  // (a block that the step's token makes whole is among the last ones of its row, which are read whatever their bounds: all layers at once here)
+  if (fs) launch_bounds_store(c.n_layers, c.n_kv_heads, c.head_dim, (const uint16_t*)kv->kv_base, 2 * kv->num_blocks * c.n_kv_heads * 16 * c.head_dim,
+                              fs->bounds, kv->block_table, kv->max_blocks_per_seq, kv->num_blocks, ws.seq_len, nullptr, num_seqs, 1, nullptr, st);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return fail(LLM42_EHIP, "verifier pass: launch failed: %s", hipGetErrorString(e));
   return LLM42_OK;
@@ -440,7 +514,7 @@ llm42_status verify_impl(const char* who, const llm42_model* m, const llm42_kv_c
                          const int32_t* candidates, int32_t window, const int32_t* n_valid, int32_t num_seqs,
                          int32_t max_context, int32_t* out_tokens, int32_t* seq_status, float* out_logits,
                          const int32_t* dump_seq_ids, int32_t n_dump, void* workspace, size_t workspace_bytes,
-                         void* hip_stream, const llm42_sampling* sampling, bool batch_chosen, Fast4* f4 = nullptr) {
+                         void* hip_stream, const llm42_sampling* sampling, bool batch_chosen, Fast4* f4 = nullptr, FastSparse* fs = nullptr) {
   if (sampling && !(sampling->temperature >= 0.f)) return fail(LLM42_EINVAL, "%s: negative temperature", who);
   if (!m || !kv || !seq_lens || !candidates || !out_tokens || !workspace)
     return fail(LLM42_EINVAL, "%s: null argument", who);
@@ -467,15 +541,25 @@ llm42_status verify_impl(const char* who, const llm42_model* m, const llm42_kv_c
       return fail(LLM42_ECAPACITY, "%s: max_context %d exceeds the 4-bit cache's block-table capacity %lld", who, max_context,
                   (long long)k.max_blocks_per_seq * LLM42_KV_BLOCK);
   }
-  Workspace ws = f4 && f4->kv4 ? carve(m, num_seqs, window, max_context, (char*)workspace, true, part_rows4(m, num_seqs, max_context, *f4))
+  if (fs) {
+    if (!fs->bounds || (uintptr_t)fs->bounds % 16) return fail(LLM42_EINVAL, "%s: kv_bounds must be 16-byte aligned", who);
+    if (kv->num_blocks > 0x7FFFFFFF || (uintptr_t)kv->kv_base % 16) return fail(LLM42_EINVAL, "%s: bad kv_cache view", who);
+    if (max_context > kMostContextPaged) return fail(LLM42_EINVAL, "%s: max_context must be 1..%d", who, kMostContextPaged);
+    if (fs->budget < 1 || fs->budget > LLM42_MAX_SELECTED) return fail(LLM42_EINVAL, "%s: a list has 1..%d blocks", who, LLM42_MAX_SELECTED);
+    if (fs->sink < 0 || fs->recent < 1 || (int64_t)fs->sink + fs->recent > fs->budget)
+      return fail(LLM42_EINVAL, "%s: sink and recent must be at least 0 and 1, and no more than the budget together", who);
+  }
+  Workspace ws = fs ? carve(m, num_seqs, window, max_context, (char*)workspace, true)
+                 : f4 && f4->kv4 ? carve(m, num_seqs, window, max_context, (char*)workspace, true, part_rows4(m, num_seqs, max_context, *f4))
                                : call_workspace(m, num_seqs, window, max_context, (char*)workspace,
                                                 f4 ? workspace_bytes - std::min(workspace_bytes, mx4_residual_bytes(num_seqs, padded_rows(num_seqs), m->cfg.d_model))
                                                    : workspace_bytes, batch_chosen);
-  const size_t parts4 = f4 ? mx4_residual_bytes(ws.m_rows, ws.m_pad, m->cfg.d_model) : 0, need = ws.bytes + parts4;
+  const size_t parts4 = f4 ? mx4_residual_bytes(ws.m_rows, ws.m_pad, m->cfg.d_model) : 0;
+  const size_t need = ws.bytes + parts4 + (fs ? carve_fast_sparse(m, num_seqs, max_context, *fs, (char*)workspace + ws.bytes) : 0);
   if (need > workspace_bytes) return fail(LLM42_EWORKSPACE, "%s: workspace %zu < %zu bytes", who, workspace_bytes, need);
   if (f4) f4->parts = (float*)((char*)workspace + ws.bytes);
   return run_pass(m, kv, seq_lens, candidates, window, n_valid, num_seqs, max_context, out_tokens, seq_status,
-                  n_dump > 0 ? out_logits : nullptr, dump_seq_ids, n_dump, ws, (hipStream_t)hip_stream, sampling, false, f4);
+                  n_dump > 0 ? out_logits : nullptr, dump_seq_ids, n_dump, ws, (hipStream_t)hip_stream, sampling, false, f4, fs);
 }
 
 }  // namespace
@@ -798,6 +882,36 @@ llm42_status llm42_decode_step_mx4(const llm42_mx4_model* m4, const llm42_kv_cac
   Fast4 f4{m4, kv4, 0, 0, nullptr};
   return verify_impl("decode_step_mx4", m4->model, kv, seq_lens, tokens, 1, nullptr, num_seqs, max_context, out_tokens, seq_status,
                      nullptr, nullptr, 0, workspace, workspace_bytes, hip_stream, sampling, true, &f4);
+}
+
+llm42_status llm42_decode_step_sparse_workspace_bytes(const llm42_model* m, int32_t max_seqs, int32_t max_context, int32_t budget,
+                                                      size_t* out_bytes) {
+  const char* who = "decode_step_sparse_workspace_bytes";
+  if (!m || !out_bytes) return fail(LLM42_EINVAL, "%s: null argument", who);
+  if (max_seqs < 1 || max_seqs > LLM42_MAX_ROWS || max_context < 1 || max_context > kMostContextPaged || budget < 1 || budget > LLM42_MAX_SELECTED)
+    return fail(LLM42_EINVAL, "%s: max_seqs/max_context/budget out of range", who);
+  FastSparse f;
+  memset(&f, 0, sizeof f);
+  f.budget = budget;
+  size_t most = 0;                                               // (the ways in which the work is split change with the number of sequences)
+  for (int n = 1; n <= max_seqs; ++n)
+    most = std::max(most, carve(m, n, 1, max_context, nullptr, true).bytes + carve_fast_sparse(m, n, max_context, f, nullptr));
+  *out_bytes = most;
+  return LLM42_OK;
+}
+
+llm42_status llm42_decode_step_sparse(const llm42_model* m, const llm42_kv_cache* kv, void* kv_bounds, int32_t budget, int32_t sink, int32_t recent,
+                                      const int32_t* seq_lens, const int32_t* tokens, int32_t num_seqs, int32_t max_context,
+                                      int32_t* out_tokens, int32_t* seq_status, void* workspace, size_t workspace_bytes, void* hip_stream,
+                                      const llm42_sampling* sampling) {
+  FastSparse f;
+  memset(&f, 0, sizeof f);
+  f.bounds = (char*)kv_bounds;
+  f.budget = budget;
+  f.sink = sink;
+  f.recent = recent;
+  return verify_impl("decode_step_sparse", m, kv, seq_lens, tokens, 1, nullptr, num_seqs, max_context, out_tokens, seq_status, nullptr, nullptr,
+                     0, workspace, workspace_bytes, hip_stream, sampling, true, nullptr, &f);
 }
 
 llm42_status llm42_prefill_workspace_bytes(const llm42_model* m, int32_t max_seqs, int32_t chunk, int32_t max_context,

@@ -21,7 +21,7 @@ __global__ __launch_bounds__(256) void bounds_store_kernel(const uint16_t* __res
   const int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   const int h = (int)(item % n_kv_heads), slot = (int)(item / n_kv_heads % slots), s = (int)(item / n_kv_heads / slots), layer = blockIdx.y * L;
   if (s >= num_seqs) return;
-  const int64_t first = first_[s], count = count_[s];
+  const int64_t first = first_[s], count = count_ ? count_[s] : max_count;
   int status = LLM42_SEQ_OK;
   const int begin = (int)(first / LLM42_KV_BLOCK), end = (int)min((first + count) / LLM42_KV_BLOCK, (int64_t)width);   // whole blocks end here
   if (first < 0 || count < 0 || count > max_count || first + count > (int64_t)width * LLM42_KV_BLOCK) {

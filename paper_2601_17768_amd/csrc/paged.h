@@ -160,6 +160,14 @@ struct Select {
   uint32_t* keys;              // workspace, or null: the scores stay in LDS
   int num_cus;
 };
+// Partials of a call whose lists are cut into parts.
+struct SparseWorkspace {
+  float *acc, *ml;
+  int32_t* ok;
+  size_t bytes;
+};
+SparseWorkspace carve_sparse(int rows, int n_kv_heads, int group, int head_dim, int parts, char* base);
+
 struct SparseAttention {
   Rows rows;
   const uint16_t *k_plane, *v_plane;
@@ -182,6 +190,7 @@ struct SparseAttention {
 
 void launch_rope_table(const double* freq, double factor, int pairs, int max_position, float2* table, hipStream_t st);
 void launch_kv_append(const paged::Append& a, hipStream_t st);
+// count null: max_count everywhere.
 void launch_bounds_store(int n_layers, int n_kv_heads, int head_dim, const uint16_t* k_plane, int64_t layer_stride, char* bounds,
                          const int32_t* block_table, int width, int64_t num_blocks, const int32_t* first, const int32_t* count, int num_seqs,
                          int max_count, int32_t* seq_status, hipStream_t st);

@@ -102,27 +102,6 @@ std::vector<double> frequencies(const llm42_rope_config& c) {
   return f;
 }
 
-struct SparseWorkspace {
-  float *acc, *ml;
-  int32_t* ok;
-  size_t bytes;
-};
-SparseWorkspace carve(const llm42_heads* h, int rows, int parts, char* base) {
-  SparseWorkspace w;
-  size_t off = 0;
-  auto take = [&](size_t bytes) {
-    char* p = base ? base + off : nullptr;
-    off = align_up(off + bytes, 256);
-    return p;
-  };
-  const size_t lists = parts > 1 ? (size_t)rows * h->n_kv_heads * parts : 0, slots = lists * (h->n_q_heads / h->n_kv_heads);
-  w.ok = (int32_t*)take(4 * lists);
-  w.acc = (float*)take(4 * slots * h->head_dim);
-  w.ml = (float*)take(8 * slots);
-  w.bytes = off;
-  return w;
-}
-
 llm42_status check_workspace(const char* who, const void* workspace, size_t bytes, size_t need) {
   if (need && (!workspace || (uintptr_t)workspace % 256)) return fail(LLM42_EWORKSPACE, "%s: the call needs a workspace, 256-byte aligned", who);
   if (bytes < need) return fail(LLM42_EWORKSPACE, "%s: workspace %zu < %zu bytes", who, bytes, need);
@@ -135,6 +114,22 @@ llm42_status check_budget(const char* who, int32_t budget) {
 }
 
 }  // namespace
+
+paged::SparseWorkspace paged::carve_sparse(int rows, int n_kv_heads, int group, int head_dim, int parts, char* base) {
+  SparseWorkspace w;
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    char* p = base ? base + off : nullptr;
+    off = align_up(off + bytes, 256);
+    return p;
+  };
+  const size_t lists = parts > 1 ? (size_t)rows * n_kv_heads * parts : 0, slots = lists * group;
+  w.ok = (int32_t*)take(4 * lists);
+  w.acc = (float*)take(4 * slots * head_dim);
+  w.ml = (float*)take(8 * slots);
+  w.bytes = off;
+  return w;
+}
 
 extern "C" {
 
@@ -360,7 +355,7 @@ llm42_status llm42_kv_sparse_attention_workspace_bytes(const llm42_heads* heads,
   if (llm42_status st = check_budget(who, width)) return st;
   int parts, per_part;
   plan_sparse_attention(num_seqs * window, heads->n_kv_heads, heads->head_dim, width, current_cus(), parts, per_part);
-  *out_bytes = carve(heads, num_seqs * window, parts, nullptr).bytes;
+  *out_bytes = carve_sparse(num_seqs * window, heads->n_kv_heads, heads->n_q_heads / heads->n_kv_heads, heads->head_dim, parts, nullptr).bytes;
   return LLM42_OK;
 }
 
@@ -396,7 +391,7 @@ llm42_status llm42_kv_sparse_attention(const llm42_heads* heads, int32_t layer, 
   a.seq_status = seq_status;
   a.num_cus = current_cus();
   plan_sparse_attention(num_seqs * window, a.n_kv_heads, a.head_dim, width, a.num_cus, a.parts, a.per_part);
-  const SparseWorkspace ws = carve(heads, num_seqs * window, a.parts, (char*)workspace);
+  const SparseWorkspace ws = carve_sparse(num_seqs * window, a.n_kv_heads, a.group, a.head_dim, a.parts, (char*)workspace);
   if (llm42_status st = check_workspace(who, workspace, workspace_bytes, a.parts > 1 ? ws.bytes : 0)) return st;
   a.part_acc = ws.acc;
   a.part_ml = ws.ml;

@@ -84,7 +84,7 @@ class PagedCache:
         self._select_need: Dict = {}
         self._attention_need: Dict = {}
 
-    def _kept_bounds(self) -> torch.Tensor:
+    def kept_bounds(self) -> torch.Tensor:
         if self.bounds is None:
             raise ValueError("the cache was made without bounds")
         return self.bounds
@@ -112,7 +112,7 @@ class PagedCache:
     def store_bounds(self, block_table: torch.Tensor, first: torch.Tensor, count: torch.Tensor, max_count: int, layer: int = -1,
                      seq_status: Optional[torch.Tensor] = None) -> None:
         """One llm42_kv_bounds_store call: behind a prefill, or a verifier pass and its commit."""
-        B.llm42_kv_bounds_store(self.heads, layer, self.kv, self.num_blocks, block_table, self._kept_bounds(), first, count, max_count, seq_status)
+        B.llm42_kv_bounds_store(self.heads, layer, self.kv, self.num_blocks, block_table, self.kept_bounds(), first, count, max_count, seq_status)
 
     def read_bounds(self, block_ids: torch.Tensor) -> Tuple[torch.Tensor, torch.Tensor]:
         """One llm42_kv_bounds_read call: (smallest, largest) of the physical blocks, bfloat16 [n_layers, len(block_ids), n_kv_heads, head_dim];
@@ -120,7 +120,7 @@ class PagedCache:
         h = self.heads
         lo, hi = (torch.empty((h.n_layers, block_ids.numel(), h.n_kv_heads, h.head_dim), dtype=torch.bfloat16, device=self.kv.device)
                   for _ in range(2))
-        B.llm42_kv_bounds_read(h, self._kept_bounds(), self.num_blocks, block_ids, lo, hi)
+        B.llm42_kv_bounds_read(h, self.kept_bounds(), self.num_blocks, block_ids, lo, hi)
         return lo, hi
 
     def select(self, layer: int, q: torch.Tensor, block_table: torch.Tensor, seq_lens: torch.Tensor, budget: int, sink: int = 1, recent: int = 2,
@@ -138,7 +138,7 @@ class PagedCache:
         if need is None:
             need = self._select_need[key] = B.llm42_kv_select_workspace_bytes(self.heads, *key)
         ws = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
-        B.llm42_kv_select(self.heads, layer, self.num_blocks, block_table, self._kept_bounds(), q, seq_lens, n_valid, max_context, sink, recent,
+        B.llm42_kv_select(self.heads, layer, self.num_blocks, block_table, self.kept_bounds(), q, seq_lens, n_valid, max_context, sink, recent,
                           selected, ws, seq_status)
         return selected
 

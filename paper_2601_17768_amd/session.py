@@ -31,7 +31,7 @@ class VerifierSession:
         self.model = B.llm42_model_create(self.cfg, dev_w)
         del dev_w
         self._mx4 = None
-        self._attention4_need, self._decode4_need = {}, {}
+        self._attention4_need, self._decode4_need, self._decode_sparse_need = {}, {}, {}
         self._ws = None
         self._ws_key = None
         self._ws_captured, self._ws_kept = False, []
@@ -170,6 +170,29 @@ class VerifierSession:
         table4 = None if kv4 is None else block_table if kv4_block_table is None else kv4_block_table
         B.llm42_decode_step_mx4(self.model, self.mx4, kv, kv.shape[2], block_table, kv4, 0 if kv4 is None else kv4.shape[1], table4, seq_lens,
                                 tokens, max_context, out_tokens, self._room(need), seq_status, sampling=sampling)
+        return out_tokens
+
+    # ---- the fast path over selected blocks ----
+    def paged(self, kv: torch.Tensor, bounds=True):
+        """The operators around the cache `kv` of this model (paged.PagedCache)."""
+        from .paged import PagedCache
+        return PagedCache(kv, self.shape.n_q_heads, self.shape.head_dim, bounds)
+
+    def decode_sparse(self, cache, block_table: torch.Tensor, seq_lens: torch.Tensor, tokens: torch.Tensor, budget: int, sink: int = 1,
+                      recent: int = 2, max_context: Optional[int] = None, out_tokens: Optional[torch.Tensor] = None,
+                      seq_status: Optional[torch.Tensor] = None, sampling=None) -> torch.Tensor:
+        """One llm42_decode_step_sparse call: the fast path with attention over `budget` blocks; cache: what `paged` made, with the bounds of
+        everything below seq_lens stored.  Returns out_tokens."""
+        if max_context is None:
+            max_context = block_table.shape[1] * B.LLM42_KV_BLOCK
+        key = (seq_lens.numel(), max_context, budget)
+        need = self._decode_sparse_need.get(key)
+        if need is None:
+            need = self._decode_sparse_need[key] = B.llm42_decode_step_sparse_workspace_bytes(self.model, *key)
+        if out_tokens is None:
+            out_tokens = torch.empty(seq_lens.numel(), dtype=torch.int32, device=self.device)
+        B.llm42_decode_step_sparse(self.model, cache.heads, cache.kv, cache.num_blocks, block_table, cache.kept_bounds(), budget, sink, recent,
+                                   seq_lens, tokens, max_context, out_tokens, self._room(need), seq_status, sampling=sampling)
         return out_tokens
 
     def commit(self, candidates: torch.Tensor, out_tokens: torch.Tensor, seq_lens: torch.Tensor,

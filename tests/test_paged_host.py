@@ -129,3 +129,9 @@ ATTEND = dict(heads=HEADS(), layer=0, kv=KV(), q=4096, qs=1024, lens=4096, windo
     (dict(width=4096), -3), (dict(width=4096, ws=4096, ws_bytes=256), -3), (dict(width=4096, ws=4100, ws_bytes=2 ** 40), -3)])
 def test_sparse_attention_refuses(bad, code):
     assert call("llm42_kv_sparse_attention", {**ATTEND, **bad}) == code
+
+
+def test_sparse_step_refuses_without_a_model():
+    lib, out = B.load_library(), SZ()
+    assert lib.llm42_decode_step_sparse_workspace_bytes(None, 1, 64, 8, ctypes.byref(out)) == B.LLM42_EINVAL
+    assert lib.llm42_decode_step_sparse(None, None, None, 8, 1, 2, None, None, 1, 64, None, None, None, 0, None, None) == B.LLM42_EINVAL
