@@ -543,6 +543,8 @@ def _head_rows(t: torch.Tensor, num_seqs: int, window: int, heads: int, head_dim
     kind = _TYPES.get(t.dtype)
     if kind is None:
         raise ValueError(f"expected bfloat16 or float32, got {t.dtype}")
+    if t.is_contiguous():
+        return t.data_ptr(), kind, heads * head_dim
     of_seq, of_row, of_head, near = t.stride()
     row = of_row if window > 1 else of_seq if num_seqs > 1 else heads * head_dim
     if near != 1 or (heads > 1 and of_head != head_dim) or (num_seqs > 1 and window > 1 and of_seq != window * row):
@@ -553,16 +555,19 @@ def _head_rows(t: torch.Tensor, num_seqs: int, window: int, heads: int, head_dim
 def _paged_view(heads: Heads, kv: Optional[torch.Tensor], num_blocks: int, block_table: torch.Tensor, num_seqs: int) -> KVCache:
     if block_table.dim() != 2 or block_table.shape[0] != num_seqs:
         raise ValueError("block_table must be [num_seqs, max_blocks_per_seq]")
-    if kv is not None and kv.numel() * kv.element_size() < llm42_heads_kv_bytes(heads, num_blocks):
-        raise ValueError(f"kv holds {kv.numel() * kv.element_size()} bytes, {num_blocks} blocks need {llm42_heads_kv_bytes(heads, num_blocks)}")
+    # (llm42_heads_kv_bytes and llm42_kv_bounds_bytes by hand: a call of the library each would cost as much as all the rest)
+    need = 64 * heads.n_layers * heads.n_kv_heads * heads.head_dim * num_blocks
+    if kv is not None and kv.numel() * kv.element_size() < need:
+        raise ValueError(f"kv holds {kv.numel() * kv.element_size()} bytes, {num_blocks} blocks need {need}")
     return KVCache(_ptr(kv), num_blocks, _ptr(block_table, torch.int32), block_table.shape[1])
 
 
 def _bounds(heads: Heads, bounds: torch.Tensor, num_blocks: int) -> int:
     if bounds.dtype != torch.uint8:
         raise ValueError(f"bounds are a uint8 tensor, got {bounds.dtype}")
-    if bounds.numel() < llm42_kv_bounds_bytes(heads, num_blocks):
-        raise ValueError(f"bounds hold {bounds.numel()} bytes, {num_blocks} blocks need {llm42_kv_bounds_bytes(heads, num_blocks)}")
+    need = heads.n_layers * heads.n_kv_heads * (2 * heads.head_dim + 16) * num_blocks
+    if bounds.numel() < need:
+        raise ValueError(f"bounds hold {bounds.numel()} bytes, {num_blocks} blocks need {need}")
     return _ptr(bounds)
 
 

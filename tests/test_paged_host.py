@@ -135,3 +135,18 @@ def test_sparse_step_refuses_without_a_model():
     lib, out = B.load_library(), SZ()
     assert lib.llm42_decode_step_sparse_workspace_bytes(None, 1, 64, 8, ctypes.byref(out)) == B.LLM42_EINVAL
     assert lib.llm42_decode_step_sparse(None, None, None, 8, 1, 2, None, None, 1, 64, None, None, None, 0, None, None) == B.LLM42_EINVAL
+
+
+@pytest.mark.parametrize("layers,kv_heads,hd", [(1, 1, 64), (3, 8, 128), (32, 5, 64)])
+def test_the_bindings_sizes_are_the_librarys(layers, kv_heads, hd):
+    """The binding checks buffers by its own arithmetic: one byte less than the library asks for is refused."""
+    heads, blocks = B.Heads(layers, 2 * kv_heads, kv_heads, hd), 7
+    table = torch.zeros((2, 3), dtype=torch.int32)
+    kv, bounds = (torch.zeros(n(heads, blocks) - 1, dtype=torch.uint8) for n in (B.llm42_heads_kv_bytes, B.llm42_kv_bounds_bytes))
+    for call in (lambda: B._paged_view(heads, kv, blocks, table, 2), lambda: B._bounds(heads, bounds, blocks)):
+        with pytest.raises(ValueError, match="blocks need"):
+            call()
+    for call in (lambda: B._paged_view(heads, torch.zeros(len(kv) + 1, dtype=torch.uint8), blocks, table, 2),
+                 lambda: B._bounds(heads, torch.zeros(len(bounds) + 1, dtype=torch.uint8), blocks)):
+        with pytest.raises(ValueError, match="device tensor"):
+            call()
