@@ -9,6 +9,7 @@ using namespace paged;
 namespace {
 
 constexpr int kWaves = 4, kThreads = 64 * kWaves;
+constexpr int kChunk = 256;    // blocks that a workgroup scores where scores go through the workspace; more where that is too many workgroups
 
 // Unsigned keys in the order of the scores; a block whose bounds are infinite comes before all.
 __device__ inline uint32_t key_of(float score) {
@@ -137,20 +138,38 @@ __device__ inline void reduce_bits(uint32_t& all, uint32_t& any) {
   all = a32.x & a32.y, any = o32.x | o32.y;
 }
 
+// Sum of a value over this lane and those before it.
+__device__ inline uint32_t sum_up_to(uint32_t x) {
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xF, 0xF, false);     // one lane down in its group of 16, two, four, eight
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x112, 0xF, 0xF, false);
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x114, 0xF, 0xF, false);
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x118, 0xF, 0xF, false);
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xA, 0xF, false);     // the last lane of the group before, to groups 1 and 3
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xC, 0xF, false);     // lane 31 to groups 2 and 3
+  return x;
+}
+
 // The `k` highest of keys[begin .. end - 1], the lowest index on ties, ascending to out; the whole workgroup of T threads together.  The k-th highest key is
 // found eight bits at a time, among those that differ, from counts of the keys that agree with it so far; then one pass in order.  R keys to a thread are held in
 // registers; R 0: any number of them, read again in every pass.
 template <int T, int R>
-__device__ inline void pick(const uint32_t* keys, int begin, int end, int k, int32_t* out, Scratch& sh) {
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-  uint32_t u[R ? R : 1], all = 0xFFFFFFFFu, any = 0;
-  if constexpr (R > 0) {
+struct Held {
+  uint32_t u[R ? R : 1];
+  __device__ inline void load(const uint32_t* keys, int begin, int end) {
+    if constexpr (R > 0) {
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      const int i = begin + r * T + tid;
-      u[r] = i < end ? keys[i] : 0;                               // (no key is 0: that is the pattern of a NaN)
+      for (int r = 0; r < R; ++r) {
+        const int i = begin + r * T + (int)threadIdx.x;
+        u[r] = i < end ? keys[i] : 0;                             // (no key is 0: that is the pattern of a NaN)
+      }
     }
   }
+};
+template <int T, int R>
+__device__ inline void pick(const Held<T, R>& held, const uint32_t* keys, int begin, int end, int k, int32_t* out, Scratch& sh) {
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  const auto& u = held.u;
+  uint32_t all = 0xFFFFFFFFu, any = 0;
   const auto each = [&](const auto& f) __attribute__((always_inline)) {
     if constexpr (R > 0) {
 #pragma unroll
@@ -187,13 +206,7 @@ __device__ inline void pick(const uint32_t* keys, int begin, int end, int k, int
       int c[4], sum = 0;
 #pragma unroll
       for (int j = 0; j < 4; ++j) sum += c[j] = sh.hist[255 - (lane * 4 + j)];
-      int before = sum;
-#pragma unroll
-      for (int d = 1; d < 64; d *= 2) {
-        const int x = __shfl_up(before, d);
-        if (lane >= d) before += x;
-      }
-      before -= sum;
+      int before = (int)sum_up_to((uint32_t)sum) - sum;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         if (before < need && before + c[j] >= need) {
@@ -233,12 +246,7 @@ __device__ inline void pick(const uint32_t* keys, int begin, int end, int k, int
       uint32_t c[C], sum = 0;
 #pragma unroll
       for (int j = 0; j < C; ++j) sum += c[j] = lane * C + j < E ? sh.counts[lane * C + j] : 0;
-      uint32_t before = sum;
-#pragma unroll
-      for (int d = 1; d < 64; d *= 2) {
-        const uint32_t x = (uint32_t)__shfl_up((int)before, d);
-        if (lane >= d) before += x;
-      }
+      uint32_t before = sum_up_to(sum);
       if (lane == 63) sh.any = before;
       before -= sum;
 #pragma unroll
@@ -343,11 +351,18 @@ __device__ inline void query_of(const uint16_t* (&src)[HD / 64][2], const Select
 __device__ inline int whole_status(const Rows& r, int s, int len, int n) {
   const int status = length_status(r, len, n);
   bool bad = false;
-  if (status == LLM42_SEQ_OK && n > 0)
-    for (int b = threadIdx.x; b <= (len + n - 1) / LLM42_KV_BLOCK; b += blockDim.x) {
-      const int id = r.block_table[(size_t)s * r.width + b];
-      bad |= id < 0 || id >= r.num_blocks;
+  if (status == LLM42_SEQ_OK && n > 0) {
+    constexpr int U = 8;
+    const int32_t* ids = r.block_table + (size_t)s * r.width;
+    const int last = (len + n - 1) / LLM42_KV_BLOCK;
+    for (int b = threadIdx.x; b <= last; b += U * blockDim.x) {
+      int id[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) id[u] = ids[min(b + u * (int)blockDim.x, last)];
+#pragma unroll
+      for (int u = 0; u < U; ++u) bad |= id[u] < 0 || id[u] >= r.num_blocks;
     }
+  }
   return __syncthreads_or(bad) ? LLM42_SEQ_BAD_BLOCK : status;
 }
 
@@ -432,7 +447,7 @@ __global__ __launch_bounds__(kThreads) void select_kernel(Select a, int tile_row
   for (int i = 0; i < rows; ++i) {
     const int own = (len + i0 + i) / LLM42_KV_BLOCK;
     const int k = select_plain<kThreads>(a, own, out_of(i), threadIdx.x);
-    if (k) pick<kThreads, 0>(sh_keys + i * stride, a.sink, own + 1 - a.recent, k, out_of(i) + a.sink, sh);
+    if (k) pick<kThreads, 0>(Held<kThreads, 0>(), sh_keys + i * stride, a.sink, own + 1 - a.recent, k, out_of(i) + a.sink, sh);
     __syncthreads();
   }
 }
@@ -448,37 +463,44 @@ __global__ __launch_bounds__(kThreads) void score_kernel(Select a, int tile_rows
   if (last + 1 <= a.budget || a.budget == a.sink + a.recent) return;
   const int begin = max(a.sink, (int)blockIdx.z * chunk), end = min(last + 1 - a.recent, ((int)blockIdx.z + 1) * chunk);
   if (begin >= end) return;
+  // (the ids wait in LDS where they are no more than that)
+  __shared__ int32_t sh_ids[kChunk];
+  const int32_t* ids = r.block_table + (size_t)s * r.width;
   bool bad = false;
   for (int b = begin + threadIdx.x; b < end; b += kThreads) {
-    const int id = r.block_table[(size_t)s * r.width + b];
+    const int id = ids[b];
     bad |= id < 0 || id >= r.num_blocks;
+    if (chunk == kChunk) sh_ids[b - (int)blockIdx.z * kChunk] = id;
   }
+  const Query<HD> q = query<HD, COLS>(a, s, kvh, i0, rows);
   if (__syncthreads_or(bad)) return;                              // (the second launch sees it too)
-  const int32_t* ids = r.block_table + (size_t)s * r.width;
-  score_blocks<HD, COLS>(a, query<HD, COLS>(a, s, kvh, i0, rows), kvh, rows, begin, end, a.keys + (((size_t)s * r.window + i0) * a.n_kv_heads + kvh) * stride,
-                   a.n_kv_heads * stride, [&](int b) { return ids[b]; });
+  uint32_t* keys = a.keys + (((size_t)s * r.window + i0) * a.n_kv_heads + kvh) * stride;
+  if (chunk == kChunk)
+    score_blocks<HD, COLS>(a, q, kvh, rows, begin, end, keys, a.n_kv_heads * stride, [&](int b) { return sh_ids[b - (int)blockIdx.z * kChunk]; });
+  else
+    score_blocks<HD, COLS>(a, q, kvh, rows, begin, end, keys, a.n_kv_heads * stride, [&](int b) { return ids[b]; });
 }
 
-// ... and second: a workgroup per row, blockIdx.y: kv head.
+// ... and second: a workgroup per row, blockIdx.y: kv head.  R: keys that a thread holds, 0 any number.  They are asked for together with the table that says whether the sequence is in
+// order (what the workspace holds where it is not is of no use and does no harm).
 constexpr int kPickThreads = 1024;
+template <int R>
 __global__ __launch_bounds__(kPickThreads) void pick_kernel(Select a, int64_t stride) {
   __shared__ Scratch sh;
   const Rows& r = a.rows;
   const int s = blockIdx.x / r.window, i = blockIdx.x % r.window, kvh = blockIdx.y;
   const int len = r.seq_len[s], n = r.seq_n ? r.seq_n[s] : r.window;
+  const size_t at = ((size_t)s * r.window + i) * a.n_kv_heads + kvh;
+  const uint32_t* keys = a.keys + at * stride;
+  const int own = (len + i) / LLM42_KV_BLOCK, end = own + 1 - a.recent;
+  Held<kPickThreads, R> held;
+  if (length_status(r, len, n) == LLM42_SEQ_OK && i < n) held.load(keys, a.sink, end);   // (a row that is not there may lie behind max_context)
   const int status = whole_status(r, s, len, n);
   if (a.seq_status && i == 0 && kvh == 0 && threadIdx.x == 0) a.seq_status[s] = status;
   if (status != LLM42_SEQ_OK || i >= n) return;
-  const size_t at = ((size_t)s * r.window + i) * a.n_kv_heads + kvh;
-  const int own = (len + i) / LLM42_KV_BLOCK;
   int32_t* out = a.selected + at * a.budget;
   const int k = select_plain<kPickThreads>(a, own, out, threadIdx.x);
-  if (k == 0) return;
-  const uint32_t* keys = a.keys + at * stride;
-  const int end = own + 1 - a.recent, most = end - a.sink;
-  if (most <= 2 * kPickThreads) pick<kPickThreads, 2>(keys, a.sink, end, k, out + a.sink, sh);
-  else if (most <= 8 * kPickThreads) pick<kPickThreads, 8>(keys, a.sink, end, k, out + a.sink, sh);
-  else pick<kPickThreads, 0>(keys, a.sink, end, k, out + a.sink, sh);
+  if (k) pick<kPickThreads, R>(held, keys, a.sink, end, k, out + a.sink, sh);
 }
 
 // Keys of a tile row, one for each block that max_context positions can have, a multiple of 16.
@@ -513,9 +535,14 @@ void launch_kv_select(const Select& a, hipStream_t st) {
       select_kernel<HD, COLS><<<dim3(r.num_seqs * tiles, a.n_kv_heads), kThreads, lds, st>>>(a, tile_rows, tiles, (int)keys);
       return;
     }
-    const int chunk = (int)std::max<int64_t>(256, (keys + 65535) / 65536 * 16);
+    const int chunk = (int)std::max<int64_t>(kChunk, (keys + 65535) / 65536 * 16);
     score_kernel<HD, COLS><<<dim3(r.num_seqs * tiles, a.n_kv_heads, (unsigned)((keys + chunk - 1) / chunk)), kThreads, 0, st>>>(a, tile_rows, tiles, keys, chunk);
-    pick_kernel<<<dim3(r.num_seqs * r.window, a.n_kv_heads), kPickThreads, 0, st>>>(a, keys);
+    const auto pick = [&](auto held) {
+      pick_kernel<decltype(held)::value><<<dim3(r.num_seqs * r.window, a.n_kv_heads), kPickThreads, 0, st>>>(a, keys);
+    };
+    if (keys <= 2 * kPickThreads) pick(std::integral_constant<int, 2>{});
+    else if (keys <= 8 * kPickThreads) pick(std::integral_constant<int, 8>{});
+    else pick(std::integral_constant<int, 0>{});
   };
   const auto by_cols = [&](auto hd) {
     switch (cols_of(a.group)) {
