@@ -64,7 +64,10 @@ __global__ __launch_bounds__(64 * NW) void sparse_attention_kernel(SparseAttenti
   if (lane == 0) sh_used[wave] = used;
   bad = __syncthreads_or(bad);
   if (a.parts > 1 && threadIdx.x == 0) a.part_ok[slot] = !bad;
-  if (bad) return;
+  if (bad) {
+    if (a.seq_status && threadIdx.x == 0) atomicOr(a.seq_status + s, LLM42_SEQ_BAD_BLOCK);
+    return;
+  }
 
   bf16x8 q[KT];
   {
@@ -226,23 +229,11 @@ __global__ __launch_bounds__(256) void sparse_join_kernel(SparseAttention a) {
   else *out = any ? (uint16_t)pack2_bf16(o[0] / sum, 0.f) : 0;
 }
 
-// Status of every sequence, from the lengths and the entries that the lists need: a workgroup per sequence.
+// Status of every sequence by its lengths; the attention adds what it finds in the table.
 __global__ __launch_bounds__(256) void sparse_status_kernel(SparseAttention a) {
   const Rows& r = a.rows;
-  const int s = blockIdx.x, len = r.seq_len[s], n = r.seq_n ? r.seq_n[s] : r.window;
-  const int status = length_status(r, len, n);
-  bool bad = false;
-  if (status == LLM42_SEQ_OK) {
-    const int64_t per_row = (int64_t)a.n_kv_heads * a.width;
-    for (int64_t e = threadIdx.x; e < n * per_row; e += 256) {
-      const int b = a.selected[(int64_t)s * r.window * per_row + e];
-      if (b < 0 || b > (len + (int)(e / per_row)) / LLM42_KV_BLOCK) continue;
-      const int id = r.block_table[(size_t)s * r.width + b];
-      bad |= id < 0 || id >= r.num_blocks;
-    }
-  }
-  bad = __syncthreads_or(bad);
-  if (threadIdx.x == 0) a.seq_status[s] = bad ? LLM42_SEQ_BAD_BLOCK : status;
+  const int s = blockIdx.x * 256 + threadIdx.x;
+  if (s < r.num_seqs) a.seq_status[s] = length_status(r, r.seq_len[s], r.seq_n ? r.seq_n[s] : r.window);
 }
 
 constexpr int kMostPart = 1024;   // entries of a part: 8 KiB of LDS
@@ -251,7 +242,7 @@ template <int HD, bool TILES>
 void launch(const SparseAttention& a, hipStream_t st) {
   const int rows = a.rows.num_seqs * a.rows.window;
   const float scale_log2 = 1.4426950408889634f * (a.scale > 0.f ? a.scale : 1.0f / sqrtf((float)HD));
-  if (a.seq_status) sparse_status_kernel<<<a.rows.num_seqs, 256, 0, st>>>(a);
+  if (a.seq_status) sparse_status_kernel<<<(a.rows.num_seqs + 255) / 256, 256, 0, st>>>(a);
   const dim3 grid(rows * a.parts, a.n_kv_heads);
   const size_t lds = sizeof(int2) * ((a.per_part + 1) & ~1);
   // (eight waves where a CU has no second workgroup: us by eight / four, sequences x 64 blocks, 1 9.6 / 10.4, 8 11.0 / 14.0, 16 14.1 / 15.3, 24 19.3 / 19.3)

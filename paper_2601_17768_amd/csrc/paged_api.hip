@@ -1,8 +1,6 @@
 // C ABI of the operators around the paged bf16 cache (declared in include/llm42_paged.h): host-side validation.
 #include <cmath>
-#include <cstring>
 #include <new>
-#include <vector>
 
 #include "paged.h"
 
@@ -76,9 +74,8 @@ const uint16_t* k_plane_of(const llm42_heads* h, const llm42_kv_cache* kv, int32
 int64_t bounds_of(const llm42_heads* h, int64_t num_blocks) { return num_blocks * h->n_kv_heads * bounds_record(h->head_dim); }
 
 // Frequencies of the pairs, scaled.
-std::vector<double> frequencies(const llm42_rope_config& c) {
+void frequencies(const llm42_rope_config& c, double* f) {
   const int half = c.rot_dim / 2;
-  std::vector<double> f(half);
   const double two_pi = 6.283185307179586476925286766559, n = c.original_max_position;
   double lo = 0, hi = 0;
   if (c.scaling == LLM42_ROPE_YARN) {
@@ -99,7 +96,6 @@ std::vector<double> frequencies(const llm42_rope_config& c) {
       f[j] = x * (1 - ramp) + x / c.factor * ramp;
     } else f[j] = x;
   }
-  return f;
 }
 
 llm42_status check_workspace(const char* who, const void* workspace, size_t bytes, size_t need) {
@@ -161,10 +157,7 @@ llm42_status llm42_rope_create(const llm42_rope_config* cfg, llm42_rope** out) {
   const double factor = c.attention_factor > 0 ? c.attention_factor : c.scaling == LLM42_ROPE_YARN ? 0.1 * std::log(c.factor) + 1.0 : 1.0;
   const int half = c.rot_dim / 2;
   double freq[64];
-  {
-    const std::vector<double> f = frequencies(c);
-    std::memcpy(freq, f.data(), sizeof(double) * half);
-  }
+  frequencies(c, freq);
   llm42_rope* r = new (std::nothrow) llm42_rope();
   if (!r) return fail(LLM42_EHIP, "%s: out of host memory", who);
   r->rot_dim = c.rot_dim;

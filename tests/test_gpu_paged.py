@@ -229,6 +229,25 @@ def test_bounds_are_exact(hd, kv_heads):
     assert status.tolist() == [0, 0, 1, 0] and bool((w.cache.bounds == 99).all())
 
 
+@pytest.mark.parametrize("hd", [64, 128])
+def test_bounds_of_the_smallest_and_largest_keys(hd):
+    """bf16 numbers below the normal ones still count, outward, as one unit of 2^-40; every border between two powers of two."""
+    w = World([16 * 40], 1, 1, hd, layers=1)
+    k = w.k[0]
+    k[:] = 0
+    k[0, 0:16, :, 0], k[0, 5, :, 1] = 2.0 ** -133, -(2.0 ** -130)
+    for b in range(1, 40):
+        e = 2 * b - 41
+        k[0, 16 * b + 3, 0, b] = 127 * 2.0 ** e if b % 2 else 127.5 * 2.0 ** e
+        k[0, 16 * b + 9, 0, b + 1] = -(2.0 ** (e - 3))
+    kv_layout.write_tokens(w.cache.kv, w.bt[0], k.to(DEV), w.v[0].to(DEV))
+    w.cache.store_bounds(w.bt, i32([0]), i32([640]), 640)
+    lo, hi = w.cache.read_bounds(w.bt[0].contiguous())
+    l, u = w.bounds(0, 0)
+    assert torch.equal(lo[0].cpu().double(), l) and torch.equal(hi[0].cpu().double(), u)
+    assert float(hi[0, 0, 0, 0]) == 2.0 ** -40 and float(lo[0, 0, 0, 1]) == -(2.0 ** -40)
+
+
 def expected_lists(w, layer, q, lens, valid, budget, sink, recent):
     n, window = q.shape[:2]
     out = torch.full((n, window, w.kv_heads, budget), -77, dtype=torch.int32)
@@ -310,6 +329,20 @@ def test_select_skips_sequences_that_are_not_in_order(room):
     assert bool((out[1:4] == -77).all()) and bool((out[[0, 4]] != -77).all())
     w.cache.select(0, w.queries(2).to(DEV), bt, i32([398] * 5), 8, n_valid=i32([3, 0, -1, 0, 2]), selected=out.fill_(-77), seq_status=status)
     assert status.tolist() == [1, 0, 1, 0, 2] and bool((out == -77).all())
+
+
+def test_select_of_rows_that_are_not_there():
+    """A window at the end of the room: its rows behind n_valid would see blocks that no array has."""
+    w = World([16 * 800] * 2, kv_heads=1, group=1, hd=64, layers=1)
+    w.cache.store_bounds(w.bt, i32([0] * 2), i32(w.lens), 12800)
+    q, lens = w.queries(512), [12799, 12500]
+    got = w.cache.select(0, q.to(DEV), w.bt, i32(lens), 6, n_valid=i32([1, 300]))
+    few = [0, 1, 2, 17, 299]
+    for s, rows in ((0, [0]), (1, few)):
+        lo, hi = w.bounds(0, s)
+        for i in rows:
+            assert got[s, i, 0].tolist() == ref.select(q[s, i], lo[:, 0], hi[:, 0], (lens[s] + i) // 16, 6, 1, 2), (s, i)
+    assert bool((got[0, 1:] == -1).all()) and bool((got[1, 300:] == -1).all())
 
 
 def lists_of(w, lens, window, width, kind):
