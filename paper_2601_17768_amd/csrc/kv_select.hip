@@ -70,36 +70,54 @@ __device__ inline void quantize(Query<HD>& d, const uint16_t* const (&src)[HD / 
     }
 }
 
-// What lane (g, l16) holds of the bounds of block l16.
+// The bounds of 16 blocks.  As operands of the products, lane (g, l16) needs 16 bytes here and there of record l16; asked for like that, every lane of a load looks up a cache line of
+// its own, and a CU gets 20 bytes a ns.  So a wave reads whole records, 16 neighbouring lanes (head_dim 64: 8) each, and turns them through LDS: piece p of
+// record r lies at place p ^ r of the record, so that neither way has lanes in one bank.
 template <int HD>
 struct Record {
-  i32x4 up[HD / 64], down[HD / 64];
+  static constexpr int P = HD / 8, J = P / 4;                     // pieces of a record, loads of 64 lanes for 16 of them
+  u32x4 w[J];
   int e;
-  __device__ inline void load(const char* rec, int g) {
+  // rec_of(r): record r of the 16
+  template <class Rec>
+  __device__ inline void load(Rec rec_of, int lane) {
 #pragma unroll
-    for (int c = 0; c < HD / 64; ++c) {
-      up[c] = *(const i32x4*)(rec + c * 64 + g * 16);
-      down[c] = *(const i32x4*)(rec + HD + c * 64 + g * 16);
+    for (int j = 0; j < J; ++j) {
+      const int r = j * (64 / P) + lane / P;
+      w[j] = *(const u32x4*)(rec_of(r) + ((lane % P) ^ (r % P)) * 16);
     }
-    e = *(const uint8_t*)(rec + 2 * HD);
+    e = *(const uint8_t*)(rec_of(lane & 15) + 2 * HD);
   }
 };
 
 // Keys of U times 16 blocks, of which lane l16 of every group of 16 has the records: lane (g, column) gets those of blocks 4 g .. 4 g + 3 for its column's tile row (the
 // largest over the columns of the same tile row).
 template <int HD, int COLS, int U>
-__device__ inline void score16(u32x4 (&key)[U], const Record<HD> (&d)[U], const Query<HD>& q, int lane) {
-  constexpr int C = HD / 64;
-  const int g = lane >> 4;
-  i32x4 acc[U];
+__device__ inline void score16(u32x4 (&key)[U], const Record<HD> (&d)[U], const Query<HD>& q, u32x4* stage, int lane) {
+  constexpr int C = HD / 64, P = Record<HD>::P;
+  const int g = lane >> 4, l16 = lane & 15;
+  i32x4 acc[U], up[U][C], down[U][C];
+  // (a wave's LDS accesses are in order: the next 16 records may follow as soon as these have been asked for)
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+#pragma unroll
+    for (int j = 0; j < Record<HD>::J; ++j) stage[j * 64 + lane] = d[u].w[j];
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      up[u][c] = __builtin_bit_cast(i32x4, stage[l16 * P + ((c * 4 + g) ^ (l16 % P))]);
+      down[u][c] = __builtin_bit_cast(i32x4, stage[l16 * P + ((P / 2 + c * 4 + g) ^ (l16 % P))]);
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
 #pragma unroll
   for (int u = 0; u < U; ++u) acc[u] = (i32x4){0, 0, 0, 0};
 #pragma unroll
   for (int c = 0; c < C; ++c) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) acc[u] = __builtin_amdgcn_mfma_i32_16x16x64_i8(d[u].up[c], q.pos[c], acc[u], 0, 0, 0);
+    for (int u = 0; u < U; ++u) acc[u] = __builtin_amdgcn_mfma_i32_16x16x64_i8(up[u][c], q.pos[c], acc[u], 0, 0, 0);
 #pragma unroll
-    for (int u = 0; u < U; ++u) acc[u] = __builtin_amdgcn_mfma_i32_16x16x64_i8(d[u].down[c], q.neg[c], acc[u], 0, 0, 0);
+    for (int u = 0; u < U; ++u) acc[u] = __builtin_amdgcn_mfma_i32_16x16x64_i8(down[u][c], q.neg[c], acc[u], 0, 0, 0);
   }
   int e[U][4];
 #pragma unroll
@@ -369,20 +387,24 @@ __device__ inline int whole_status(const Rows& r, int s, int len, int n) {
 // Keys of blocks begin .. end - 1 (of the sequence) for a tile of rows, by the waves of a workgroup in turn, four times 16 blocks at once; keys of tile row r at
 // keys + r * stride, a multiple of 16 (those around begin and end - 1 may be anything).  id_of(b): the physical block.
 template <int HD, int COLS, class Ids>
-__device__ inline void score_blocks(const Select& a, const Query<HD>& q, int kvh, int rows, int begin, int end, uint32_t* keys, int64_t stride, Ids id_of) {
+__device__ inline void score_blocks(const Select& a, const Query<HD>& q, int kvh, int rows, int begin, int end, uint32_t* keys, int64_t stride,
+                                    u32x4 (&stage)[kWaves][16 * Record<HD>::P], Ids id_of) {
   constexpr int U = 4;
-  const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6, lane = threadIdx.x & 63, g = lane >> 4, l16 = lane & 15;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, g = lane >> 4, l16 = lane & 15;
   const int end_tile = (end + 15) / 16;
-  for (int t0 = begin / 16 + wave * U; t0 < end_tile; t0 += waves * U) {
+  for (int t0 = begin / 16 + wave * U; t0 < end_tile; t0 += kWaves * U) {
     Record<HD> d[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int b = min(max((t0 + u) * 16 + l16, begin), end - 1);
-      d[u].load(a.bounds + ((size_t)id_of(b) * a.n_kv_heads + kvh) * bounds_record(HD), g);
+      const auto rec_of = [&](int r) __attribute__((always_inline)) {
+        const int b = min(max((t0 + u) * 16 + r, begin), end - 1);
+        return a.bounds + ((size_t)id_of(b) * a.n_kv_heads + kvh) * bounds_record(HD);
+      };
+      d[u].load(rec_of, lane);
     }
     __builtin_amdgcn_sched_barrier(0);                            // (all of them asked for before the first is waited for)
     u32x4 key[U];
-    score16<HD, COLS, U>(key, d, q, lane);
+    score16<HD, COLS, U>(key, d, q, stage[wave], lane);
     if (l16 % COLS == 0 && l16 / COLS < rows) {
 #pragma unroll
       for (int u = 0; u < U; ++u)
@@ -405,6 +427,7 @@ __device__ inline Query<HD> query(const Select& a, int s, int kvh, int i0, int r
 template <int HD, int COLS>
 __global__ __launch_bounds__(kThreads) void select_kernel(Select a, int tile_rows, int tiles, int stride) {
   extern __shared__ __align__(16) uint32_t sh_keys[];
+  __shared__ u32x4 stage[kWaves][16 * Record<HD>::P];
   __shared__ Scratch sh;
   const Rows& r = a.rows;
   const int s = blockIdx.x / tiles, i0 = blockIdx.x % tiles * tile_rows, kvh = blockIdx.y;
@@ -425,7 +448,7 @@ __global__ __launch_bounds__(kThreads) void select_kernel(Select a, int tile_row
   if (a.seq_status && i0 == 0 && kvh == 0 && threadIdx.x == 0) a.seq_status[s] = status;
   if (status != LLM42_SEQ_OK || rows <= 0) return;
   if (scores) {
-    score_blocks<HD, COLS>(a, q, kvh, rows, a.sink, scored, sh_keys, stride, [&](int b) { return sh_keys[b]; });
+    score_blocks<HD, COLS>(a, q, kvh, rows, a.sink, scored, sh_keys, stride, stage, [&](int b) { return sh_keys[b]; });
     __syncthreads();
   }
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
@@ -465,6 +488,7 @@ __global__ __launch_bounds__(kThreads) void score_kernel(Select a, int tile_rows
   if (begin >= end) return;
   // (the ids wait in LDS where they are no more than that)
   __shared__ int32_t sh_ids[kChunk];
+  __shared__ u32x4 stage[kWaves][16 * Record<HD>::P];
   const int32_t* ids = r.block_table + (size_t)s * r.width;
   bool bad = false;
   for (int b = begin + threadIdx.x; b < end; b += kThreads) {
@@ -476,9 +500,9 @@ __global__ __launch_bounds__(kThreads) void score_kernel(Select a, int tile_rows
   if (__syncthreads_or(bad)) return;                              // (the second launch sees it too)
   uint32_t* keys = a.keys + (((size_t)s * r.window + i0) * a.n_kv_heads + kvh) * stride;
   if (chunk == kChunk)
-    score_blocks<HD, COLS>(a, q, kvh, rows, begin, end, keys, a.n_kv_heads * stride, [&](int b) { return sh_ids[b - (int)blockIdx.z * kChunk]; });
+    score_blocks<HD, COLS>(a, q, kvh, rows, begin, end, keys, a.n_kv_heads * stride, stage, [&](int b) { return sh_ids[b - (int)blockIdx.z * kChunk]; });
   else
-    score_blocks<HD, COLS>(a, q, kvh, rows, begin, end, keys, a.n_kv_heads * stride, [&](int b) { return ids[b]; });
+    score_blocks<HD, COLS>(a, q, kvh, rows, begin, end, keys, a.n_kv_heads * stride, stage, [&](int b) { return ids[b]; });
 }
 
 // ... and second: a workgroup per row, blockIdx.y: kv head.  R: keys that a thread holds, 0 any number.  They are asked for together with the table that says whether the sequence is in
