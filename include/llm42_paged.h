@@ -188,7 +188,7 @@ llm42_status llm42_kv_select(
 /* Attention of row (s, i) over the blocks selected[s][i][kv head][0 .. width - 1], in any order (llm42_kv_select's lists or others): out = softmax(scale * q . k) v over
  * the positions of those blocks up to seq_lens[s] + i, all of which must have been stored; head h uses kv head h / (n_q_heads / n_kv_heads).
  * An entry < 0 or beyond the row's own block counts for nothing, one that is listed twice counts twice; a row that lists nothing gets zeros.
- * Sums are fp32; weights enter the products with V as a sum of two bf16 (2^-17 of a weight).
+ * Sums are fp32; weights enter the products with V as a sum of two bf16 (off by 2^-16 of a weight).
  * scale 0 stands for 1 / sqrt(head_dim).  Block-table entries are needed for the listed blocks only: where one of a (row, kv head)'s is out of range, the heads of that kv head
  * are left as they were and the sequence's status is LLM42_SEQ_BAD_BLOCK; the other rows are written. */
 llm42_status llm42_kv_sparse_attention_workspace_bytes(const llm42_heads* heads, int32_t num_seqs, int32_t window, int32_t width,

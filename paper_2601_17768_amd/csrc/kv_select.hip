@@ -71,8 +71,8 @@ __device__ inline void quantize(Query<HD>& d, const uint16_t* const (&src)[HD / 
 }
 
 // The bounds of 16 blocks.  As operands of the products, lane (g, l16) needs 16 bytes here and there of record l16; asked for like that, every lane of a load looks up a cache line of
-// its own, and a CU gets 20 bytes a ns.  So a wave reads whole records, 16 neighbouring lanes (head_dim 64: 8) each, and turns them through LDS: piece p of
-// record r lies at place p ^ r of the record, so that neither way has lanes in one bank.
+// its own.  So a wave reads whole records, 16 neighbouring lanes (head_dim 64: 8) each, and turns them through LDS: piece p of record r lies at place p ^ r of the record,
+// so that neither way has lanes in one bank (128 sequences of 1024 - 8192 positions 27.6 -> 23.3 us, 3.2 TB/s; single workgroups gain nothing).
 template <int HD>
 struct Record {
   static constexpr int P = HD / 8, J = P / 4;                     // pieces of a record, loads of 64 lanes for 16 of them
@@ -540,10 +540,11 @@ size_t select_workspace(int num_seqs, int window, int n_kv_heads, int group, int
   const int tile_rows = tile_rows_of(group, window);
   const int64_t wgs = (int64_t)num_seqs * ((window + tile_rows - 1) / tile_rows) * n_kv_heads;
   if (keys <= budget) return 0;
-  // A workgroup gets about 20 bytes a ns from memory, whatever it has in flight, so few of them with long contexts leave the device idle: their scores go through the
-  // workspace, 256 blocks to a workgroup, and a second launch picks (us so / in LDS, sequences x positions, 8 kv heads of 128, group 4: 1 x 8192
-  // 13.6 / 13.7, 1 x 16384 14.4 / 21, 8 x 16384 14.7 / 21, 16 x 32768 26 / 34, 1 x 131072 25 / 106, 1 window of 64 x 30000 33 / 58; but 32 x 32768
-  // 39 / 36, 128 x 8192 56 / 34, 4 windows of 32 x 8000 36 / 17).  Those of a tile of rows that LDS does not hold go there too.
+  // A workgroup gets about 20 bytes a ns from memory, whatever it has in flight (most records lie in pages of their own), so few of them with long contexts leave the
+  // device idle: their scores go through the workspace, 256 blocks to a workgroup, and a second launch picks (us so / in LDS, sequences x positions, 8 kv heads
+  // of 128, group 4: 1 x 4096 12.0 / 8.8, 1 x 8192 12.3 / 12.5, 1 x 16384 13.0 / 19.6, 8 x 16384 13.6 / 20.6, 16 x 32768 25.7 / 34.7, 1 x 131072
+  // 27 / 109, 1 window of 64 x 30000 22.7 / 59; 32 x 32768 36.7 / 38.8; but 64 x 32768 75 / 62, 128 x 8192 42 / 32, 4 windows of 32 x 8000 25 / 16.5).  Those of a tile of rows that LDS does not
+  // hold go there too.
   if (tile_rows * keys <= kMostLdsKeys && (2 * wgs > num_cus || keys <= 512)) return 0;
   return 4ull * num_seqs * window * n_kv_heads * keys;
 }

@@ -31,7 +31,7 @@ struct Pair {
 // its own, and are joined through LDS.  The heads of the kv head are the columns of the products:
 //   scores: D[key][head] = K Q, a tile of K being an operand as it lies in memory;
 //   weights: p = exp2((s - ref) scale log2 e) in fp32; ref moves when a pair's maximum exceeds it by more than 8.  They enter the product with V as
-//   the sum of two bf16, so that what is lost is 2^-17 of a weight: the launch waits for memory, not for the matrix cores;
+//   the sum of two bf16, so that what is lost is 2^-16 of a weight: the launch waits for memory, not for the matrix cores;
 //   output: D[feature][head] = V P, a tile of V being four tokens of a feature for each lane, as D's rows of the scores are.
 template <int NW, int HD, bool TILES>
 __global__ __launch_bounds__(64 * NW) void sparse_attention_kernel(SparseAttention a, float scale_log2) {
@@ -142,11 +142,13 @@ __global__ __launch_bounds__(64 * NW) void sparse_attention_kernel(SparseAttenti
       sum += w[k];
     }
     l += sum;
+    // (cut off, not rounded: the second part is never below zero, nor zero where the weight is not - an infinite V stays what it is)
     u32x4 hi, lo;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      hi[k] = pack2_bf16(w[2 * k], w[2 * k + 1]);
-      lo[k] = pack2_bf16(w[2 * k] - lo_bf16(hi[k]), w[2 * k + 1] - hi_bf16(hi[k]));
+      const float a = w[2 * k], b = w[2 * k + 1];
+      hi[k] = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+      lo[k] = pack2_bf16(fmaxf(a - lo_bf16(hi[k]), fminf(a, 0x1p-126f)), fmaxf(b - hi_bf16(hi[k]), fminf(b, 0x1p-126f)));
     }
 #pragma unroll
     for (int f = 0; f < FB; ++f) {

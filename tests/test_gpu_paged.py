@@ -439,6 +439,22 @@ def test_infinities_and_nan_are_those_of_the_softmax():
     assert bool(((out[2, 0].double() - o).abs() <= o.abs() * 2.0 ** -8 + 2.0 ** -12 * mag).all())
 
 
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("pos", [0, 5, 40])
+def test_infinite_values_stay_infinite(hd, pos):
+    """Whatever their weights are, 1 among them (the only key, or one of equal keys)."""
+    w = World([64], kv_heads=2, group=4, hd=hd, layers=1, bounds=False)
+    w.k[0][:] = 0
+    w.v[0][0, 0, :, 1], w.v[0][0, 0, :, 2] = math.inf, -math.inf
+    kv_layout.write_tokens(w.cache.kv, w.bt[0], w.k[0].to(DEV), w.v[0].to(DEV))
+    lists = torch.tensor([0, 1, 2], dtype=torch.int32, device=DEV).expand(1, 1, 2, 3).contiguous()
+    out = w.cache.attention(0, w.queries(1).to(DEV), w.bt, i32([pos]), lists).cpu()
+    assert bool((out[..., 1] == math.inf).all()) and bool((out[..., 2] == -math.inf).all())
+    want = w.v[0][0, :pos + 1].double().mean(0).repeat_interleave(4, 0)
+    fine = torch.tensor([f for f in range(hd) if f not in (1, 2)])
+    assert bool(((out[0, 0][:, fine].double() - want[:, fine]).abs() <= want[:, fine].abs() * 2.0 ** -8 + 2.0 ** -12 * w.v[0][0, :pos + 1].double().abs().mean(0).repeat_interleave(4, 0)[:, fine]).all())
+
+
 def test_offsets_beyond_32_bits():
     """Blocks whose keys, values and bounds lie 2^32 bytes and 2^31 elements behind their arrays' beginnings."""
     h, hd, blocks = 8, 128, 2_100_000                             # K plane: 34.4e9 elements; bounds: 4.57e9 bytes
