@@ -536,49 +536,76 @@ def llm42_decode_step_mx4(model: int, mx4: int, kv_base: torch.Tensor, num_block
                                                 ctypes.byref(sampling) if sampling is not None else None))
 
 
-def _head_rows(t: torch.Tensor, num_seqs: int, window: int, heads: int, head_dim: int):
-    """(pointer, type, stride) of rows [num_seqs, window, heads, head_dim] at one distance from each other, their heads side by side."""
-    if t.shape != (num_seqs, window, heads, head_dim):
-        raise ValueError(f"expected [{num_seqs}, {window}, {heads}, {head_dim}], got {list(t.shape)}")
-    kind = _TYPES.get(t.dtype)
-    if kind is None:
-        raise ValueError(f"expected bfloat16 or float32, got {t.dtype}")
+def _all_here(*tensors: Optional[torch.Tensor]) -> None:
+    """_on_current_device, at half the time."""
+    here = torch._C._cuda_getDevice()
+    for t in tensors:
+        if t is not None and t.get_device() != here:
+            raise ValueError("expected tensors on the current device")
+
+
+def _dense(t: Optional[torch.Tensor], dtype: torch.dtype) -> Optional[int]:
+    """Pointer of a tensor that has been found on the device."""
+    if t is None:
+        return None
+    if t.dtype is not dtype:
+        raise ValueError(f"expected dtype {dtype}, got {t.dtype}")
+    if not t.is_contiguous():
+        raise ValueError("expected a contiguous device tensor")
+    return t.data_ptr()
+
+
+def _for_seqs(t: Optional[torch.Tensor], num_seqs: int) -> Optional[int]:
+    if t is None:
+        return None
+    if t.numel() != num_seqs:
+        raise ValueError("expected one entry per sequence")
+    return _dense(t, torch.int32)
+
+
+def _head_rows(t: torch.Tensor, shape):
+    """(pointer, stride) of rows [num_seqs, window, heads, head_dim] at one distance from each other, their heads side by side."""
+    if t.shape != shape:
+        raise ValueError(f"expected {list(shape)}, got {list(t.shape)}")
+    num_seqs, window, heads, head_dim = shape
     if t.is_contiguous():
-        return t.data_ptr(), kind, heads * head_dim
+        return t.data_ptr(), heads * head_dim
     of_seq, of_row, of_head, near = t.stride()
     row = of_row if window > 1 else of_seq if num_seqs > 1 else heads * head_dim
     if near != 1 or (heads > 1 and of_head != head_dim) or (num_seqs > 1 and window > 1 and of_seq != window * row):
         raise ValueError("rows (sequence, token) must lie at one distance from each other, their heads side by side")
-    return t.data_ptr(), kind, row
+    return t.data_ptr(), row
 
 
+# (llm42_heads_kv_bytes and llm42_kv_bounds_bytes are reckoned by hand in what follows: a call of the library each would cost as much as all the rest)
 def _paged_view(heads: Heads, kv: Optional[torch.Tensor], num_blocks: int, block_table: torch.Tensor, num_seqs: int) -> KVCache:
-    if block_table.dim() != 2 or block_table.shape[0] != num_seqs:
+    shape = block_table.shape
+    if len(shape) != 2 or shape[0] != num_seqs:
         raise ValueError("block_table must be [num_seqs, max_blocks_per_seq]")
-    # (llm42_heads_kv_bytes and llm42_kv_bounds_bytes by hand: a call of the library each would cost as much as all the rest)
-    need = 64 * heads.n_layers * heads.n_kv_heads * heads.head_dim * num_blocks
-    if kv is not None and kv.numel() * kv.element_size() < need:
-        raise ValueError(f"kv holds {kv.numel() * kv.element_size()} bytes, {num_blocks} blocks need {need}")
-    return KVCache(_ptr(kv), num_blocks, _ptr(block_table, torch.int32), block_table.shape[1])
+    base = None
+    if kv is not None:
+        need = 64 * heads.n_layers * heads.n_kv_heads * heads.head_dim * num_blocks
+        if kv.nbytes < need:
+            raise ValueError(f"kv holds {kv.nbytes} bytes, {num_blocks} blocks need {need}")
+        base = _dense(kv, kv.dtype)
+    return KVCache(base, num_blocks, _dense(block_table, torch.int32), shape[1])
 
 
 def _bounds(heads: Heads, bounds: torch.Tensor, num_blocks: int) -> int:
-    if bounds.dtype != torch.uint8:
-        raise ValueError(f"bounds are a uint8 tensor, got {bounds.dtype}")
     need = heads.n_layers * heads.n_kv_heads * (2 * heads.head_dim + 16) * num_blocks
     if bounds.numel() < need:
         raise ValueError(f"bounds hold {bounds.numel()} bytes, {num_blocks} blocks need {need}")
-    return _ptr(bounds)
+    return _dense(bounds, torch.uint8)
 
 
 def _workspace(t: Optional[torch.Tensor]):
-    return _ptr(t), 0 if t is None else t.numel() * t.element_size()
+    return (None, 0) if t is None else (_dense(t, t.dtype), t.nbytes)
 
 
 def _lists(t: torch.Tensor, num_seqs: int, window: int, kv_heads: int) -> int:
-    if t.dim() != 4 or tuple(t.shape[:3]) != (num_seqs, window, kv_heads):
+    if t.dim() != 4 or t.shape[:3] != (num_seqs, window, kv_heads):
         raise ValueError(f"lists of blocks must be [{num_seqs}, {window}, {kv_heads}, entries], got {list(t.shape)}")
-    return _ptr(t, torch.int32)
+    return _dense(t, torch.int32)
 
 
 def _asked(call, *args) -> int:
@@ -612,46 +639,48 @@ def llm42_kv_append(heads: Heads, layer: int, kv: torch.Tensor, num_blocks: int,
     """k, v [num_seqs, window, n_kv_heads, head_dim] and q [num_seqs, window, n_q_heads, head_dim]: bfloat16 or float32, all the same; q_out bfloat16.
     rope: a handle of llm42_rope_create."""
     num_seqs = seq_lens.numel()
-    _on_current_device(kv, block_table, bounds, q, k, v, q_norm, k_norm, seq_lens, n_valid, q_out, seq_status)
+    _all_here(kv, block_table, bounds, q, k, v, q_norm, k_norm, seq_lens, n_valid, q_out, seq_status)
     if k.dim() != 4:
         raise ValueError("k must be [num_seqs, window, n_kv_heads, head_dim]")
-    window, hd = k.shape[1], heads.head_dim
-    kp, kind, ks = _head_rows(k, num_seqs, window, heads.n_kv_heads, hd)
-    vp, v_kind, vs = _head_rows(v, num_seqs, window, heads.n_kv_heads, hd)
-    qp, q_kind, qs = (None, kind, 0) if q is None else _head_rows(q, num_seqs, window, heads.n_q_heads, hd)
-    op, o_kind, os_ = (None, LLM42_BF16, 0) if q_out is None else _head_rows(q_out, num_seqs, window, heads.n_q_heads, hd)
-    if kind != v_kind or kind != q_kind or o_kind != LLM42_BF16:
-        raise ValueError("q, k and v must be of one type, q_out bfloat16")
+    window, hd, dtype = k.shape[1], heads.head_dim, k.dtype
+    kind = _TYPES.get(dtype)
+    if kind is None or v.dtype is not dtype or (q is not None and q.dtype is not dtype) or (q_out is not None and q_out.dtype is not torch.bfloat16):
+        raise ValueError("q, k and v must be of one type, bfloat16 or float32, q_out bfloat16")
+    of_kv, of_q = (num_seqs, window, heads.n_kv_heads, hd), (num_seqs, window, heads.n_q_heads, hd)
+    kp, ks = _head_rows(k, of_kv)
+    vp, vs = _head_rows(v, of_kv)
+    qp, qs = (None, 0) if q is None else _head_rows(q, of_q)
+    op, os_ = (None, 0) if q_out is None else _head_rows(q_out, of_q)
     for t in (q_norm, k_norm):
         if t is not None and t.numel() != hd:
             raise ValueError(f"gains hold {hd} values")
     view = _paged_view(heads, kv, num_blocks, block_table, num_seqs)
     _check(load_library().llm42_kv_append(
         ctypes.byref(heads), layer, ctypes.byref(view), None if bounds is None else _bounds(heads, bounds, num_blocks), qp, qs, kp, ks, vp, vs, kind,
-        _ptr(q_norm, torch.bfloat16), _ptr(k_norm, torch.bfloat16), norm_eps, rope, _per_seq(seq_lens, num_seqs), window,
-        _per_seq(n_valid, num_seqs), num_seqs, max_context, op, os_, _per_seq(seq_status, num_seqs), _stream_handle(stream)))
+        _dense(q_norm, torch.bfloat16), _dense(k_norm, torch.bfloat16), norm_eps, rope, _for_seqs(seq_lens, num_seqs), window,
+        _for_seqs(n_valid, num_seqs), num_seqs, max_context, op, os_, _for_seqs(seq_status, num_seqs), _stream_handle(stream)))
 
 
 def llm42_kv_bounds_store(heads: Heads, layer: int, kv: torch.Tensor, num_blocks: int, block_table: torch.Tensor, bounds: torch.Tensor,
                           first: torch.Tensor, count: torch.Tensor, max_count: int, seq_status: Optional[torch.Tensor] = None, stream=None) -> None:
     """layer -1: all."""
     num_seqs = first.numel()
-    _on_current_device(kv, block_table, bounds, first, count, seq_status)
+    _all_here(kv, block_table, bounds, first, count, seq_status)
     view = _paged_view(heads, kv, num_blocks, block_table, num_seqs)
     _check(load_library().llm42_kv_bounds_store(ctypes.byref(heads), layer, ctypes.byref(view), _bounds(heads, bounds, num_blocks),
-                                                _per_seq(first, num_seqs), _per_seq(count, num_seqs), num_seqs, max_count,
-                                                _per_seq(seq_status, num_seqs), _stream_handle(stream)))
+                                                _for_seqs(first, num_seqs), _for_seqs(count, num_seqs), num_seqs, max_count,
+                                                _for_seqs(seq_status, num_seqs), _stream_handle(stream)))
 
 
 def llm42_kv_bounds_read(heads: Heads, bounds: torch.Tensor, num_blocks: int, block_ids: torch.Tensor, out_lo: torch.Tensor,
                          out_hi: torch.Tensor, stream=None) -> None:
     """out_lo, out_hi: bfloat16 [n_layers, len(block_ids), n_kv_heads, head_dim]."""
-    _on_current_device(bounds, block_ids, out_lo, out_hi)
+    _all_here(bounds, block_ids, out_lo, out_hi)
     shape = (heads.n_layers, block_ids.numel(), heads.n_kv_heads, heads.head_dim)
     if out_lo.shape != shape or out_hi.shape != shape:
         raise ValueError(f"out_lo and out_hi must be {list(shape)}")
-    _check(load_library().llm42_kv_bounds_read(ctypes.byref(heads), _bounds(heads, bounds, num_blocks), num_blocks, _ptr(block_ids, torch.int32),
-                                               block_ids.numel(), _ptr(out_lo, torch.bfloat16), _ptr(out_hi, torch.bfloat16),
+    _check(load_library().llm42_kv_bounds_read(ctypes.byref(heads), _bounds(heads, bounds, num_blocks), num_blocks, _dense(block_ids, torch.int32),
+                                               block_ids.numel(), _dense(out_lo, torch.bfloat16), _dense(out_hi, torch.bfloat16),
                                                _stream_handle(stream)))
 
 
@@ -664,16 +693,17 @@ def llm42_kv_select(heads: Heads, layer: int, num_blocks: int, block_table: torc
                     workspace: Optional[torch.Tensor], seq_status: Optional[torch.Tensor] = None, stream=None) -> None:
     """selected: int32 [num_seqs, window, n_kv_heads, budget]."""
     num_seqs = seq_lens.numel()
-    _on_current_device(block_table, bounds, q, seq_lens, n_valid, selected, workspace, seq_status)
+    _all_here(block_table, bounds, q, seq_lens, n_valid, selected, workspace, seq_status)
     if q.dim() != 4 or q.dtype != torch.bfloat16:
         raise ValueError("q must be bfloat16 [num_seqs, window, n_q_heads, head_dim]")
     window = q.shape[1]
-    qp, _, qs = _head_rows(q, num_seqs, window, heads.n_q_heads, heads.head_dim)
+    shape = (num_seqs, window, heads.n_q_heads, heads.head_dim)
+    qp, qs = _head_rows(q, shape)
     view = _paged_view(heads, None, num_blocks, block_table, num_seqs)
     _check(load_library().llm42_kv_select(
-        ctypes.byref(heads), layer, ctypes.byref(view), _bounds(heads, bounds, num_blocks), qp, qs, _per_seq(seq_lens, num_seqs), window,
-        _per_seq(n_valid, num_seqs), num_seqs, max_context, selected.shape[-1], sink, recent,
-        _lists(selected, num_seqs, window, heads.n_kv_heads), _per_seq(seq_status, num_seqs), *_workspace(workspace), _stream_handle(stream)))
+        ctypes.byref(heads), layer, ctypes.byref(view), _bounds(heads, bounds, num_blocks), qp, qs, _for_seqs(seq_lens, num_seqs), window,
+        _for_seqs(n_valid, num_seqs), num_seqs, max_context, selected.shape[-1], sink, recent,
+        _lists(selected, num_seqs, window, heads.n_kv_heads), _for_seqs(seq_status, num_seqs), *_workspace(workspace), _stream_handle(stream)))
 
 
 def llm42_kv_sparse_attention_workspace_bytes(heads: Heads, num_seqs: int, window: int, width: int) -> int:
@@ -686,16 +716,17 @@ def llm42_kv_sparse_attention(heads: Heads, layer: int, kv: torch.Tensor, num_bl
                               stream=None) -> None:
     """q, out: bfloat16 [num_seqs, window, n_q_heads, head_dim]; selected: int32 [num_seqs, window, n_kv_heads, width]; scale 0: 1 / sqrt(head_dim)."""
     num_seqs = seq_lens.numel()
-    _on_current_device(kv, block_table, q, seq_lens, n_valid, selected, out, workspace, seq_status)
+    _all_here(kv, block_table, q, seq_lens, n_valid, selected, out, workspace, seq_status)
     if q.dim() != 4 or q.dtype != torch.bfloat16 or out.dtype != torch.bfloat16:
         raise ValueError("q and out must be bfloat16 [num_seqs, window, n_q_heads, head_dim]")
     window = q.shape[1]
-    qp, _, qs = _head_rows(q, num_seqs, window, heads.n_q_heads, heads.head_dim)
-    op, _, os_ = _head_rows(out, num_seqs, window, heads.n_q_heads, heads.head_dim)
+    shape = (num_seqs, window, heads.n_q_heads, heads.head_dim)
+    qp, qs = _head_rows(q, shape)
+    op, os_ = _head_rows(out, shape)
     view = _paged_view(heads, kv, num_blocks, block_table, num_seqs)
     _check(load_library().llm42_kv_sparse_attention(
-        ctypes.byref(heads), layer, ctypes.byref(view), qp, qs, _per_seq(seq_lens, num_seqs), window, _per_seq(n_valid, num_seqs), num_seqs,
-        max_context, _lists(selected, num_seqs, window, heads.n_kv_heads), selected.shape[-1], scale, op, os_, _per_seq(seq_status, num_seqs),
+        ctypes.byref(heads), layer, ctypes.byref(view), qp, qs, _for_seqs(seq_lens, num_seqs), window, _for_seqs(n_valid, num_seqs), num_seqs,
+        max_context, _lists(selected, num_seqs, window, heads.n_kv_heads), selected.shape[-1], scale, op, os_, _for_seqs(seq_status, num_seqs),
         *_workspace(workspace), _stream_handle(stream)))
 
 
@@ -709,13 +740,13 @@ def llm42_decode_step_sparse(model: int, heads: Heads, kv_base: torch.Tensor, nu
                              sampling: Optional[Sampling] = None) -> None:
     """(`heads`: the model's, for the check of the bounds' size.)"""
     num_seqs = seq_lens.numel()
-    _on_current_device(kv_base, block_table, bounds, seq_lens, tokens, out_tokens, workspace, seq_status)
+    _all_here(kv_base, block_table, bounds, seq_lens, tokens, out_tokens, workspace, seq_status)
     kv = _kv_view(model, kv_base, num_blocks, block_table, num_seqs)
     if llm42_heads_kv_bytes(heads, num_blocks) != llm42_kv_bytes(model, num_blocks):
         raise ValueError("heads are not the model's")
     _check(load_library().llm42_decode_step_sparse(
-        model, ctypes.byref(kv), _bounds(heads, bounds, num_blocks), budget, sink, recent, _per_seq(seq_lens, num_seqs),
-        _per_seq(tokens, num_seqs), num_seqs, max_context, _per_seq(out_tokens, num_seqs), _per_seq(seq_status, num_seqs), *_workspace(workspace),
+        model, ctypes.byref(kv), _bounds(heads, bounds, num_blocks), budget, sink, recent, _for_seqs(seq_lens, num_seqs),
+        _for_seqs(tokens, num_seqs), num_seqs, max_context, _for_seqs(out_tokens, num_seqs), _for_seqs(seq_status, num_seqs), *_workspace(workspace),
         _stream_handle(stream), ctypes.byref(sampling) if sampling is not None else None))
 
 

@@ -540,7 +540,7 @@ size_t select_workspace(int num_seqs, int window, int n_kv_heads, int group, int
   const int tile_rows = tile_rows_of(group, window);
   const int64_t wgs = (int64_t)num_seqs * ((window + tile_rows - 1) / tile_rows) * n_kv_heads;
   if (keys <= budget) return 0;
-  // A workgroup gets about 20 bytes a ns from memory, whatever it has in flight (most records lie in pages of their own), so few of them with long contexts leave the
+  // A workgroup gets about 20 bytes a ns from memory, so few of them with long contexts leave the
   // device idle: their scores go through the workspace, 256 blocks to a workgroup, and a second launch picks (us so / in LDS, sequences x positions, 8 kv heads
   // of 128, group 4: 1 x 4096 12.0 / 8.8, 1 x 8192 12.3 / 12.5, 1 x 16384 13.0 / 19.6, 8 x 16384 13.6 / 20.6, 16 x 32768 25.7 / 34.7, 1 x 131072
   // 27 / 109, 1 window of 64 x 30000 22.7 / 59; 32 x 32768 36.7 / 38.8; but 64 x 32768 75 / 62, 128 x 8192 42 / 32, 4 windows of 32 x 8000 25 / 16.5).  Those of a tile of rows that LDS does not
