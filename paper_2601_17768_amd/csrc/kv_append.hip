@@ -8,10 +8,6 @@ using namespace paged;
 
 namespace {
 
-#ifndef Q_HEADS
-#define Q_HEADS 8
-#endif
-
 // One thread per (position, pair): the angle and its functions in 64 bits.
 __global__ __launch_bounds__(256) void rope_table_kernel(const double* __restrict__ freq, double factor, int pairs, int64_t all,
                                                          float2* __restrict__ table) {
@@ -175,7 +171,8 @@ __device__ inline bool bad_block(const Rows& r, int s, int len, int n, int lane,
 }
 
 // The launch's first workgroups take a (sequence, block, kv head) of K or of V per wave, the others a row and some heads of Q per HD / 8 lanes: its position's
-// cos and sin are read once for them.
+// cos and sin are read once for them.  Bound by memory where rows are many: 8 x 512 rows of 32 + 2 x 8 heads of 128 with norms, 103 MB, take 29 us, 3.5 TB/s (a head at a
+// time 47, four 33, sixteen 37); by launch and two trips where they are few: one row 3.8, 128 4.8.
 template <int HD, typename T>
 __global__ __launch_bounds__(256) void append_kernel(Append a, Pairs pairs, int slots, unsigned kv_groups, int q_heads) {
   constexpr int LANES = HD / 8, UNITS = 64 / LANES, N = HD / 32, PAD = HD + 4;
@@ -300,7 +297,8 @@ void launch_kv_append(const Append& a, hipStream_t st) {
   const int slots = slots_of(r.window, r.width), units = 4 * (512 / a.head_dim);
   const int64_t rows = (int64_t)r.num_seqs * r.window;
   const Pairs pairs = !a.rope ? Pairs::NONE : a.layout == LLM42_ROPE_INTERLEAVED ? Pairs::NEAR : a.rot_dim == a.head_dim ? Pairs::HALVES : Pairs::PART;
-  const int q_heads = rows * a.n_q_heads <= 32768 ? 1 : Q_HEADS;
+  // (a head at a time while heads are no more than lanes enough to fill the device)
+  const int q_heads = rows * a.n_q_heads <= 32768 ? 1 : 8;
   const unsigned kv = (unsigned)((rows / r.window * slots * a.n_kv_heads * 2 + 3) / 4);
   const unsigned q = a.q ? (unsigned)((rows * ((a.n_q_heads + q_heads - 1) / q_heads) + units - 1) / units) : 0;
   const auto go = [&](auto kernel) { kernel<<<kv + q, 256, 0, st>>>(a, pairs, slots, kv, q_heads); };
