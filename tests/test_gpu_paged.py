@@ -293,6 +293,25 @@ def test_select_is_exact(case, room):
     assert torch.equal(out.cpu(), want)
 
 
+@pytest.mark.parametrize("blocks,window,group", [(1800, 3, 4), (5000, 1, 3), (9500, 2, 1), (1_100_000, 1, 2)])
+def test_select_of_long_contexts(blocks, window, group):
+    """Rows whose scores are held two or eight to a thread, or read again and again; more blocks than a launch has workgroups for 256 of them each."""
+    hd, n = 64, blocks * 16
+    g = torch.Generator(device=DEV).manual_seed(blocks)
+    kv = torch.empty(1, 2, blocks, 1, 16 * hd, dtype=torch.bfloat16, device=DEV)
+    kv[:, 0].normal_(generator=g)                                # (in whatever order: random is random)
+    kv[0, 0, ::7] *= 1.5
+    cache, table = PagedCache(kv, group, hd), torch.randperm(blocks, generator=g, device=DEV).int()[None]
+    cache.store_bounds(table, i32([0]), i32([n]), n)
+    lo, hi = (x[0, :, 0].cpu().double() for x in cache.read_bounds(table[0].contiguous()))
+    q = torch.randn(1, window, group, hd, generator=g, device=DEV).to(torch.bfloat16)
+    for budget, sink, recent in ((7, 1, 2), (130, 4, 8), (4096, 0, 1)):
+        if budget < blocks:
+            got = cache.select(0, q, table, i32([n - window]), budget, sink, recent)
+            for i in range(window):
+                assert got[0, i, 0].tolist() == ref.select(q[0, i].cpu(), lo, hi, (n - window + i) // 16, budget, sink, recent)
+
+
 @pytest.mark.parametrize("room", ["own", "longer"])
 def test_select_ties_and_values_without_an_order(room):
     w = World([1000] * 6, kv_heads=1, group=2, hd=64, layers=1)
@@ -476,6 +495,48 @@ def test_offsets_beyond_32_bits():
     for a, b in zip(*got):
         assert torch.equal(a, b)
     del kv, cache
+
+
+def test_the_most_rows_of_a_call():
+    """65536 sequences of a token each: append, bounds, selection and attention, looked at in some of them and by their sums in all."""
+    n, hd, blocks = 65536, 64, 3
+    g = torch.Generator(device=DEV).manual_seed(5)
+    table = torch.randperm(n * blocks, generator=g, device=DEV).int().view(n, blocks)
+    k, v = (torch.randn(n, blocks * 16, 1, hd, generator=g, device=DEV).to(torch.bfloat16) for _ in range(2))
+    kv = torch.zeros(1, 2, n * blocks, 1, 16 * hd, dtype=torch.bfloat16, device=DEV)
+    at = table.flatten().long()
+    kv[0, 0, at] = kv_layout._tokens_to_tiles_k(k.view(1, -1, 1, hd), hd)[0]
+    kv[0, 1, at] = kv_layout._tokens_to_tiles_v(v.view(1, -1, 1, hd), hd)[0]
+    cache, lens = PagedCache(kv, 2, hd), torch.randint(0, 47, (n,), generator=g, device=DEV).int()
+    lens[:3] = torch.tensor([0, 15, 46])
+    start = kv.clone()
+    cache.store_bounds(table, torch.zeros_like(lens), lens, 48)
+    q, nk, nv = (torch.randn(n, 1, h, hd, generator=g, device=DEV).to(torch.bfloat16) for h in (2, 1, 1))
+    rope, status = Rope(hd, 1e4, 64), torch.full((n,), 9, dtype=torch.int32, device=DEV)
+    turned = cache.append(0, nk, nv, table, lens, q=q, rope=rope, seq_status=status)
+    assert int(status.abs().sum()) == 0
+    lists = cache.select(0, turned, table, lens, 2, 0, 1, seq_status=status.fill_(9))
+    assert int(status.abs().sum()) == 0
+    out = cache.attention(0, turned, table, lens, lists, seq_status=status.fill_(9))
+    assert int(status.abs().sum()) == 0
+    own = (lens // 16)[:, None, None]
+    assert bool((lists[..., 0] <= own).all()) and bool((torch.where(own > 0, lists[..., 1], lists[..., 0]) == own).all())
+    # one position of every sequence has changed, in K and in V
+    read = lambda c: (kv_layout._tiles_to_tokens_k(c[:, 0, at], hd)[0].view(n, 48, hd), kv_layout._tiles_to_tokens_v(c[:, 1, at], hd)[0].view(n, 48, hd))
+    (k0, v0), (k1, v1) = read(start), read(kv)
+    here = torch.arange(48, device=DEV) == lens[:, None]
+    assert torch.equal(v1, torch.where(here[..., None], nv.view(n, 1, hd), v0)) and torch.equal(k1[~here], k0[~here])
+    for s in [0, 1, 2, 3, 1000, 32767, 32768, 65535] + [int(x) for x in torch.randint(0, n, (60,), generator=g, device=DEV)]:
+        pos = int(lens[s])
+        ks, vs = k1[s].cpu(), v1[s].cpu()
+        for got, plain in ((turned[s, 0], q[s, 0]), (ks[pos:pos + 1], nk[s, 0])):
+            want = ref.turned(plain.cpu(), pos, None, 0, (hd, 1e4, "half", dict(kind="none")))
+            assert bool(((got.cpu().double() - want).abs() <= want.abs() * 2.0 ** -8 + 2.0 ** -18 * want.abs().max()).all())
+        pairs = [ref.bounds(ks[16 * b:16 * b + 16]) for b in range(pos // 16 + 1)]
+        lo, hi = (torch.stack([x[i] for x in pairs]) for i in range(2))
+        assert lists[s, 0, 0].tolist() == ref.select(turned[s, 0].cpu(), lo, hi, pos // 16, 2, 0, 1)
+        o, mag = ref.attention(turned[s, 0].cpu(), ks, vs, lists[s, 0, 0].tolist(), pos, 0.125)
+        assert bool(((out[s, 0].cpu().double() - o).abs() <= o.abs() * 2.0 ** -8 + 2.0 ** -12 * mag).all())
 
 
 @pytest.mark.parametrize("hd,group", [(64, 2), (128, 4)])
