@@ -1,4 +1,4 @@
-"""The operators around the paged bf16 cache on the GPU against their definitions in float64: appending bit by bit, bounds and selections exactly,
+"""The operators around the paged bf16 cache on the GPU against their definitions in float64: appending to the last position, bounds and selections exactly,
 attention over lists of every kind, and all of them together.
 
 Tolerances.  A bf16 result is off by half a step, 2^-8 of it, and by the fp32 arithmetic before.  append: the norm's sum of up to 128 squares, its root,
