@@ -536,12 +536,13 @@ def llm42_decode_step_mx4(model: int, mx4: int, kv_base: torch.Tensor, num_block
                                                 ctypes.byref(sampling) if sampling is not None else None))
 
 
-def _all_here(*tensors: Optional[torch.Tensor]) -> None:
-    """_on_current_device, at half the time."""
+def _all_here(stream, *tensors: Optional[torch.Tensor]) -> Optional[int]:
+    """_on_current_device and _stream_handle, at half the time."""
     here = torch._C._cuda_getDevice()
     for t in tensors:
         if t is not None and t.get_device() != here:
             raise ValueError("expected tensors on the current device")
+    return (torch._C._cuda_getCurrentRawStream(here) if stream is None else stream.cuda_stream) or None
 
 
 def _dense(t: Optional[torch.Tensor], dtype: torch.dtype) -> Optional[int]:
@@ -639,7 +640,7 @@ def llm42_kv_append(heads: Heads, layer: int, kv: torch.Tensor, num_blocks: int,
     """k, v [num_seqs, window, n_kv_heads, head_dim] and q [num_seqs, window, n_q_heads, head_dim]: bfloat16 or float32, all the same; q_out bfloat16.
     rope: a handle of llm42_rope_create."""
     num_seqs = seq_lens.numel()
-    _all_here(kv, block_table, bounds, q, k, v, q_norm, k_norm, seq_lens, n_valid, q_out, seq_status)
+    handle = _all_here(stream, kv, block_table, bounds, q, k, v, q_norm, k_norm, seq_lens, n_valid, q_out, seq_status)
     if k.dim() != 4:
         raise ValueError("k must be [num_seqs, window, n_kv_heads, head_dim]")
     window, hd, dtype = k.shape[1], heads.head_dim, k.dtype
@@ -658,30 +659,30 @@ def llm42_kv_append(heads: Heads, layer: int, kv: torch.Tensor, num_blocks: int,
     _check(load_library().llm42_kv_append(
         ctypes.byref(heads), layer, ctypes.byref(view), None if bounds is None else _bounds(heads, bounds, num_blocks), qp, qs, kp, ks, vp, vs, kind,
         _dense(q_norm, torch.bfloat16), _dense(k_norm, torch.bfloat16), norm_eps, rope, _for_seqs(seq_lens, num_seqs), window,
-        _for_seqs(n_valid, num_seqs), num_seqs, max_context, op, os_, _for_seqs(seq_status, num_seqs), _stream_handle(stream)))
+        _for_seqs(n_valid, num_seqs), num_seqs, max_context, op, os_, _for_seqs(seq_status, num_seqs), handle))
 
 
 def llm42_kv_bounds_store(heads: Heads, layer: int, kv: torch.Tensor, num_blocks: int, block_table: torch.Tensor, bounds: torch.Tensor,
                           first: torch.Tensor, count: torch.Tensor, max_count: int, seq_status: Optional[torch.Tensor] = None, stream=None) -> None:
     """layer -1: all."""
     num_seqs = first.numel()
-    _all_here(kv, block_table, bounds, first, count, seq_status)
+    handle = _all_here(stream, kv, block_table, bounds, first, count, seq_status)
     view = _paged_view(heads, kv, num_blocks, block_table, num_seqs)
     _check(load_library().llm42_kv_bounds_store(ctypes.byref(heads), layer, ctypes.byref(view), _bounds(heads, bounds, num_blocks),
                                                 _for_seqs(first, num_seqs), _for_seqs(count, num_seqs), num_seqs, max_count,
-                                                _for_seqs(seq_status, num_seqs), _stream_handle(stream)))
+                                                _for_seqs(seq_status, num_seqs), handle))
 
 
 def llm42_kv_bounds_read(heads: Heads, bounds: torch.Tensor, num_blocks: int, block_ids: torch.Tensor, out_lo: torch.Tensor,
                          out_hi: torch.Tensor, stream=None) -> None:
     """out_lo, out_hi: bfloat16 [n_layers, len(block_ids), n_kv_heads, head_dim]."""
-    _all_here(bounds, block_ids, out_lo, out_hi)
+    handle = _all_here(stream, bounds, block_ids, out_lo, out_hi)
     shape = (heads.n_layers, block_ids.numel(), heads.n_kv_heads, heads.head_dim)
     if out_lo.shape != shape or out_hi.shape != shape:
         raise ValueError(f"out_lo and out_hi must be {list(shape)}")
     _check(load_library().llm42_kv_bounds_read(ctypes.byref(heads), _bounds(heads, bounds, num_blocks), num_blocks, _dense(block_ids, torch.int32),
                                                block_ids.numel(), _dense(out_lo, torch.bfloat16), _dense(out_hi, torch.bfloat16),
-                                               _stream_handle(stream)))
+                                               handle))
 
 
 def llm42_kv_select_workspace_bytes(heads: Heads, num_seqs: int, window: int, max_context: int, budget: int) -> int:
@@ -693,7 +694,7 @@ def llm42_kv_select(heads: Heads, layer: int, num_blocks: int, block_table: torc
                     workspace: Optional[torch.Tensor], seq_status: Optional[torch.Tensor] = None, stream=None) -> None:
     """selected: int32 [num_seqs, window, n_kv_heads, budget]."""
     num_seqs = seq_lens.numel()
-    _all_here(block_table, bounds, q, seq_lens, n_valid, selected, workspace, seq_status)
+    handle = _all_here(stream, block_table, bounds, q, seq_lens, n_valid, selected, workspace, seq_status)
     if q.dim() != 4 or q.dtype != torch.bfloat16:
         raise ValueError("q must be bfloat16 [num_seqs, window, n_q_heads, head_dim]")
     window = q.shape[1]
@@ -703,7 +704,7 @@ def llm42_kv_select(heads: Heads, layer: int, num_blocks: int, block_table: torc
     _check(load_library().llm42_kv_select(
         ctypes.byref(heads), layer, ctypes.byref(view), _bounds(heads, bounds, num_blocks), qp, qs, _for_seqs(seq_lens, num_seqs), window,
         _for_seqs(n_valid, num_seqs), num_seqs, max_context, selected.shape[-1], sink, recent,
-        _lists(selected, num_seqs, window, heads.n_kv_heads), _for_seqs(seq_status, num_seqs), *_workspace(workspace), _stream_handle(stream)))
+        _lists(selected, num_seqs, window, heads.n_kv_heads), _for_seqs(seq_status, num_seqs), *_workspace(workspace), handle))
 
 
 def llm42_kv_sparse_attention_workspace_bytes(heads: Heads, num_seqs: int, window: int, width: int) -> int:
@@ -716,7 +717,7 @@ def llm42_kv_sparse_attention(heads: Heads, layer: int, kv: torch.Tensor, num_bl
                               stream=None) -> None:
     """q, out: bfloat16 [num_seqs, window, n_q_heads, head_dim]; selected: int32 [num_seqs, window, n_kv_heads, width]; scale 0: 1 / sqrt(head_dim)."""
     num_seqs = seq_lens.numel()
-    _all_here(kv, block_table, q, seq_lens, n_valid, selected, out, workspace, seq_status)
+    handle = _all_here(stream, kv, block_table, q, seq_lens, n_valid, selected, out, workspace, seq_status)
     if q.dim() != 4 or q.dtype != torch.bfloat16 or out.dtype != torch.bfloat16:
         raise ValueError("q and out must be bfloat16 [num_seqs, window, n_q_heads, head_dim]")
     window = q.shape[1]
@@ -727,7 +728,7 @@ def llm42_kv_sparse_attention(heads: Heads, layer: int, kv: torch.Tensor, num_bl
     _check(load_library().llm42_kv_sparse_attention(
         ctypes.byref(heads), layer, ctypes.byref(view), qp, qs, _for_seqs(seq_lens, num_seqs), window, _for_seqs(n_valid, num_seqs), num_seqs,
         max_context, _lists(selected, num_seqs, window, heads.n_kv_heads), selected.shape[-1], scale, op, os_, _for_seqs(seq_status, num_seqs),
-        *_workspace(workspace), _stream_handle(stream)))
+        *_workspace(workspace), handle))
 
 
 def llm42_decode_step_sparse_workspace_bytes(model: int, max_seqs: int, max_context: int, budget: int) -> int:
@@ -740,14 +741,14 @@ def llm42_decode_step_sparse(model: int, heads: Heads, kv_base: torch.Tensor, nu
                              sampling: Optional[Sampling] = None) -> None:
     """(`heads`: the model's, for the check of the bounds' size.)"""
     num_seqs = seq_lens.numel()
-    _all_here(kv_base, block_table, bounds, seq_lens, tokens, out_tokens, workspace, seq_status)
+    handle = _all_here(stream, kv_base, block_table, bounds, seq_lens, tokens, out_tokens, workspace, seq_status)
     kv = _kv_view(model, kv_base, num_blocks, block_table, num_seqs)
     if llm42_heads_kv_bytes(heads, num_blocks) != llm42_kv_bytes(model, num_blocks):
         raise ValueError("heads are not the model's")
     _check(load_library().llm42_decode_step_sparse(
         model, ctypes.byref(kv), _bounds(heads, bounds, num_blocks), budget, sink, recent, _for_seqs(seq_lens, num_seqs),
         _for_seqs(tokens, num_seqs), num_seqs, max_context, _for_seqs(out_tokens, num_seqs), _for_seqs(seq_status, num_seqs), *_workspace(workspace),
-        _stream_handle(stream), ctypes.byref(sampling) if sampling is not None else None))
+        handle, ctypes.byref(sampling) if sampling is not None else None))
 
 
 def llm42_commit_rollback(candidates: torch.Tensor, out_tokens: torch.Tensor, n_valid: Optional[torch.Tensor],
