@@ -15,7 +15,7 @@
  * 1 <= window <= LLM42_MAX_WINDOW, at most LLM42_MAX_ROWS; n_valid[s] may be 0, and NULL stands for window everywhere.
  * A plain array of rows holds row (s, i) at (s * window + i) * stride elements, its heads side by side; it is 16-byte aligned
  * and so are its rows.  Rows that take no part (i >= n_valid[s]; a sequence whose status is not LLM42_SEQ_OK) are left
- * as they were in every output.  max_context (host, 1 .. 2^30) bounds seq_lens[s] + n_valid[s]: LLM42_ECAPACITY if it exceeds what
+ * as they were in every output (llm42_kv_sparse_attention looks at a row and kv head at a time, see there).  max_context (host, 1 .. 2^30) bounds seq_lens[s] + n_valid[s]: LLM42_ECAPACITY if it exceeds what
  * the block table or the rotary table holds.
  * Status of a sequence, where asked for: LLM42_SEQ_BAD_LENGTH if seq_lens[s] < 0, n_valid[s] is outside 0 .. window or their sum
  * exceeds max_context; LLM42_SEQ_BAD_BLOCK if a block-table entry that the call needs is < 0 or >= num_blocks.
