@@ -321,7 +321,11 @@ __device__ inline void pick_by_wave(const uint32_t* keys, int begin, int end, in
     }
   }
   if (exact) --least;
-  else need = k - at_least(least + 1);
+  else {                                                          // (counted by what is above it: the key of infinite bounds has no successor)
+    need = k;
+#pragma unroll
+    for (int r = 0; r < R; ++r) need -= __popcll(__ballot(u[r] > least));
+  }
   int ng = 0, ne = 0;
   const uint64_t below = (1ull << lane) - 1;
 #pragma unroll

@@ -1,0 +1,66 @@
+"""The decoding step with attention over selected blocks: calls whose result may depend on nothing but their inputs."""
+import numpy as np
+import pytest
+import torch
+
+import paged_reference as ref
+from helpers import wl
+from paper_2601_17768_amd import kv_layout
+from paper_2601_17768_amd.session import VerifierSession
+from test_gpu_kv4_step import VOCAB, cached_kv, factor, mirror_model
+from test_gpu_sparse_step import EPS
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+i32 = lambda x: torch.as_tensor(np.asarray(x, dtype=np.int32), device=DEV)
+
+
+@pytest.mark.parametrize("hd,kv_heads,group,longest", [(128, 2, 4, 2000), (64, 2, 2, 6000)])
+def test_blocks_with_infinite_bounds_and_a_workspace_that_holds_anything(hd, kv_heads, group, longest):
+    """Every block's bounds say -infinity .. infinity: the lowest blocks are read, whatever the workspace held.  (Rows picked by waves; the bounds are
+    written by hand, so that the attention itself stays one of ordinary numbers.)  Tolerance: as in test_gpu_sparse_step."""
+    shape, w = mirror_model(kv_heads, group, hd)
+    max_context = longest + 16
+    sess = VerifierSession(shape, w, max_position=max_context, device=DEV)
+    g, rng = torch.Generator().manual_seed(hd), wl.rng_for(hd, 4)
+    lens = [longest - 1, longest // 2, 700]
+    table, blocks = wl.make_block_table(rng, [n + 1 for n in lens], 16, spare_blocks=2, max_blocks_per_seq=-(-max_context // 16))
+    bt, kv, cached = torch.as_tensor(table, device=DEV), sess.kv_cache(blocks), []
+    for s, n in enumerate(lens):
+        k, v = cached_kv(shape, n, g)
+        cached.append((k, v))
+        kv_layout.write_tokens(kv, bt[s], *(torch.cat((t[None], torch.zeros(group, *t.shape, dtype=t.dtype))) for t in (k, v)))
+    cache, seq, tok = sess.paged(kv), i32(lens), i32(rng.integers(0, VOCAB, len(lens)))
+    rec = cache.bounds.view(-1, 2 * hd + 16)
+    rec.zero_()
+    rec[:, 2 * hd] = 255
+    budget, sink, recent = 9, 2, 1
+    start, seen = kv.clone(), []
+    for fill in (0, 1, 255, 3):
+        sess.decode_sparse(cache, bt, seq, tok, budget, sink, recent, max_context=max_context)
+        kv.copy_(start)
+        rec.zero_()
+        rec[:, 2 * hd] = 255
+        sess._ws.fill_(fill)
+        out = sess.decode_sparse(cache, bt, seq, tok, budget, sink, recent, max_context=max_context)
+        seen.append((out.clone(), kv.clone()))
+    for out, after in seen[1:]:
+        assert torch.equal(out, seen[0][0]) and torch.equal(after, seen[0][1])
+    for s, n in enumerate(lens):
+        k, v = (x[:, n].cpu() for x in kv_layout.read_tokens(seen[0][1], bt[s], n + 1, hd))
+        keys, values = torch.cat((cached[s][0], k[:1])), torch.cat((cached[s][1], v[:1]))
+        listed = list(range(budget - recent)) + [n // 16]
+        outs, mags = [], []
+        for h in range(kv_heads):
+            q = torch.stack([(keys[-1, h].double() * factor(h * group + j, group)).to(torch.bfloat16) for j in range(group)])
+            a, mag = ref.attention(q, keys[:, h], values[:, h], listed, n, hd ** -0.5)
+            outs.append(a)
+            mags.append(mag)
+        a, mag = torch.cat(outs).flatten(), torch.cat(mags).flatten()
+        t = 2.0 ** -8 * a.abs() + 2.0 ** -12 * mag
+        x = w["embed"][int(tok[s])].double() + a
+        rms, r = torch.sqrt((x * x).mean() + EPS), t.norm() / x.norm()
+        want = x / rms
+        tol = (t + x.abs() * r) / (rms * (1 - r)) * (1 + 2.0 ** -8) + 2.0 ** -8 * want.abs() + 1e-6
+        assert bool(((v[1:].flatten().double() - want).abs() <= tol).all()), (s, n)
+    sess.close()
