@@ -39,6 +39,9 @@ typedef struct {
 /* Bytes of a bf16 cache of num_blocks blocks (all layers, K and V). */
 llm42_status llm42_heads_kv_bytes(const llm42_heads* heads, int64_t num_blocks, size_t* out_bytes);
 
+/* A model's numbers as llm42_heads: those of the operators on its cache.  (Other numbers can give the same bytes of cache, in another layout.) */
+llm42_status llm42_model_heads(const llm42_model* model, llm42_heads* out);
+
 /* ---- rotary positions ----------------------------------------------------------------------------------- */
 
 #define LLM42_ROPE_HALF        0   /* pairs (j, j + rot_dim / 2)                                           */

@@ -36,7 +36,7 @@ EXPORTS = ("llm42_model_create", "llm42_model_destroy", "llm42_kv_bytes", "llm42
            "llm42_mx4_bytes", "llm42_mx4_quantize", "llm42_mx4_dequantize", "llm42_mx4_matmul_workspace_bytes", "llm42_mx4_matmul",
            "llm42_kv4_bytes", "llm42_kv4_store", "llm42_kv4_read", "llm42_kv4_attention_workspace_bytes", "llm42_kv4_attention",
            "llm42_mx4_model_create", "llm42_mx4_model_destroy", "llm42_decode_step_mx4_workspace_bytes", "llm42_decode_step_mx4",
-           "llm42_heads_kv_bytes", "llm42_rope_create", "llm42_rope_destroy", "llm42_kv_append", "llm42_kv_bounds_bytes", "llm42_kv_bounds_store",
+           "llm42_heads_kv_bytes", "llm42_model_heads", "llm42_rope_create", "llm42_rope_destroy", "llm42_kv_append", "llm42_kv_bounds_bytes", "llm42_kv_bounds_store",
            "llm42_kv_bounds_read", "llm42_kv_select_workspace_bytes", "llm42_kv_select", "llm42_kv_sparse_attention_workspace_bytes",
            "llm42_kv_sparse_attention", "llm42_decode_step_sparse_workspace_bytes", "llm42_decode_step_sparse")
 KERNEL_CLASSES = ("prepare", "embed", "rmsnorm", "qkv", "attention", "o_proj", "gate_up", "down", "lm_head",
@@ -156,6 +156,7 @@ def load_library(path: Optional[str] = None):
     hp, f32 = ctypes.POINTER(Heads), ctypes.c_float
     for name, args in {
             "llm42_heads_kv_bytes": [hp, i64, size_p],
+            "llm42_model_heads": [vp, hp],
             "llm42_rope_create": [ctypes.POINTER(RopeConfig), ctypes.POINTER(vp)],
             "llm42_kv_append": [hp, i32, kvp, vp, vp, i64, vp, i64, vp, i64, i32, vp, vp, f32, vp, vp, i32, vp, i32, i32, vp, i64, vp, vp],
             "llm42_kv_bounds_bytes": [hp, i64, size_p],
@@ -623,6 +624,12 @@ def llm42_kv_bounds_bytes(heads: Heads, num_blocks: int) -> int:
     return _asked(load_library().llm42_kv_bounds_bytes, ctypes.byref(heads), num_blocks)
 
 
+def llm42_model_heads(model: int) -> Heads:
+    heads = Heads()
+    _check(load_library().llm42_model_heads(model, ctypes.byref(heads)))
+    return heads
+
+
 def llm42_rope_create(cfg: RopeConfig) -> int:
     handle = ctypes.c_void_p()
     _check(load_library().llm42_rope_create(ctypes.byref(cfg), ctypes.byref(handle)))
@@ -739,11 +746,11 @@ def llm42_decode_step_sparse(model: int, heads: Heads, kv_base: torch.Tensor, nu
                              budget: int, sink: int, recent: int, seq_lens: torch.Tensor, tokens: torch.Tensor, max_context: int,
                              out_tokens: torch.Tensor, workspace: torch.Tensor, seq_status: Optional[torch.Tensor] = None, stream=None,
                              sampling: Optional[Sampling] = None) -> None:
-    """(`heads`: the model's, for the check of the bounds' size.)"""
+    """(`heads`: what the bounds were made with, which has to be the model's.)"""
     num_seqs = seq_lens.numel()
     handle = _all_here(stream, kv_base, block_table, bounds, seq_lens, tokens, out_tokens, workspace, seq_status)
     kv = _kv_view(model, kv_base, num_blocks, block_table, num_seqs)
-    if llm42_heads_kv_bytes(heads, num_blocks) != llm42_kv_bytes(model, num_blocks):
+    if bytes(llm42_model_heads(model)) != bytes(heads):
         raise ValueError("heads are not the model's")
     _check(load_library().llm42_decode_step_sparse(
         model, ctypes.byref(kv), _bounds(heads, bounds, num_blocks), budget, sink, recent, _for_seqs(seq_lens, num_seqs),

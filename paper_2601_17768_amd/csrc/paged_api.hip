@@ -137,6 +137,12 @@ llm42_status llm42_heads_kv_bytes(const llm42_heads* h, int64_t num_blocks, size
   return LLM42_OK;
 }
 
+llm42_status llm42_model_heads(const llm42_model* m, llm42_heads* out) {
+  if (!m || !out) return fail(LLM42_EINVAL, "model_heads: null argument");
+  *out = {m->cfg.n_layers, m->cfg.n_q_heads, m->cfg.n_kv_heads, m->cfg.head_dim};
+  return LLM42_OK;
+}
+
 llm42_status llm42_rope_create(const llm42_rope_config* cfg, llm42_rope** out) {
   const char* who = "rope_create";
   if (!cfg || !out) return fail(LLM42_EINVAL, "%s: null argument", who);

@@ -5,7 +5,9 @@ import torch
 
 import paged_reference as ref
 from helpers import wl
+from paper_2601_17768_amd import binding as B
 from paper_2601_17768_amd import kv_layout
+from paper_2601_17768_amd.paged import PagedCache
 from paper_2601_17768_amd.session import VerifierSession
 from test_gpu_kv4_step import VOCAB, cached_kv, factor, mirror_model
 from test_gpu_sparse_step import EPS
@@ -63,4 +65,21 @@ def test_blocks_with_infinite_bounds_and_a_workspace_that_holds_anything(hd, kv_
         want = x / rms
         tol = (t + x.abs() * r) / (rms * (1 - r)) * (1 + 2.0 ** -8) + 2.0 ** -8 * want.abs() + 1e-6
         assert bool(((v[1:].flatten().double() - want).abs() <= tol).all()), (s, n)
+    sess.close()
+
+
+def test_heads_that_are_not_the_models_are_refused():
+    """A cache of the same bytes in another layout: a kv head of 128 features for two of 64, whose records of bounds take less room; and of other query heads."""
+    shape = wl.TINY.replace(n_q_heads=4, n_kv_heads=2, head_dim=64)
+    sess = VerifierSession(shape, wl.make_weights(shape, seed=3), max_position=128, device=DEV)
+    assert bytes(B.llm42_model_heads(sess.model)) == bytes(B.Heads(shape.n_layers, 4, 2, 64))
+    kv = sess.kv_cache(4)
+    other = kv.view(shape.n_layers, 2, 4, 1, 16 * 128)
+    bt, zero = i32([[0, 1, 2, 3]]), i32([0])
+    for cache in (PagedCache(other, 2, 128), PagedCache(kv, 8, 64), PagedCache(kv[:1], 4, 64)):
+        before = cache.bounds.fill_(3).clone()
+        with pytest.raises(ValueError):
+            sess.decode_sparse(cache, bt, zero, zero, 2, 0, 1)
+        assert torch.equal(cache.bounds, before)
+    sess.decode_sparse(sess.paged(kv), bt, zero, zero, 2, 0, 1)
     sess.close()

@@ -1,0 +1,30 @@
+"""Calls around the paged cache that are refused, or do nothing, without a GPU."""
+import ctypes
+
+import pytest
+import torch
+
+from paper_2601_17768_amd import binding as B
+
+
+def test_model_heads_refuses():
+    lib, heads = B.load_library(), B.Heads()
+    assert lib.llm42_model_heads(None, ctypes.byref(heads)) == B.LLM42_EINVAL
+
+
+def test_the_sparse_step_compares_heads_by_their_numbers(monkeypatch):
+    """One kv head of 128 features and two of 64 take the same bytes of cache, but not of bounds."""
+    model, given, done = B.Heads(2, 4, 2, 64), B.Heads(2, 4, 1, 128), []
+    blocks, table = 4, torch.zeros((1, 4), dtype=torch.int32)
+    kv = torch.zeros(B.llm42_heads_kv_bytes(model, blocks), dtype=torch.uint8)
+    assert B.llm42_heads_kv_bytes(given, blocks) == kv.numel() and B.llm42_kv_bounds_bytes(given, blocks) < B.llm42_kv_bounds_bytes(model, blocks)
+    monkeypatch.setattr(B, "_all_here", lambda *a: None)
+    monkeypatch.setattr(B, "_kv_view", lambda m, base, n, bt, s: B.KVCache(None, n, None, bt.shape[1]))
+    monkeypatch.setattr(B, "llm42_kv_bytes", lambda m, n: kv.numel())
+    monkeypatch.setattr(B, "llm42_model_heads", lambda m: model, raising=False)
+    monkeypatch.setattr(B, "load_library", lambda: pytest.fail("the step was called") if done else B._lib)
+    bounds, one = torch.zeros(B.llm42_kv_bounds_bytes(given, blocks), dtype=torch.uint8), torch.zeros(1, dtype=torch.int32)
+    done.append(1)
+    monkeypatch.setattr(B, "_asked", lambda call, *a: kv.numel())
+    with pytest.raises(ValueError, match="not the model's"):
+        B.llm42_decode_step_sparse(1, given, kv, blocks, table, bounds, 2, 0, 1, one, one, 16, one, torch.zeros(256, dtype=torch.uint8))
