@@ -183,9 +183,9 @@ int padded_rows(int rows) {
 
 ResidLayout resid_layout(int m_pad, int d) { return m_pad <= 512 ? ResidLayout{d, 4} : ResidLayout{4, 64}; }
 
-// Carve the workspace.  Called with base == nullptr to size it.
+// Carve the workspace.  Called with base == nullptr to size it.  whole_context: with scratch for attention over all of it.
 Workspace carve(const llm42_model* m, int num_seqs, int window, int max_context, char* base, bool batch_chosen = false,
-                size_t min_part_rows = 0, size_t min_items = 0, WaveUse waves = WaveUse::NO) {
+                size_t min_part_rows = 0, size_t min_items = 0, WaveUse waves = WaveUse::NO, bool whole_context = true) {
   const llm42_config& c = m->cfg;
   Workspace ws;
   memset(&ws, 0, sizeof ws);
@@ -205,6 +205,7 @@ Workspace carve(const llm42_model* m, int num_seqs, int window, int max_context,
     ws.part_rows = m->group * window;          // (a slot's padding rows are never written)
     ws.attn_units = attention_units(false, max_context);
   }
+  if (!whole_context) ws.attn_units = 0, ws.attn_list = false;
   size_t off = 0;
   auto take = [&](size_t bytes) {
     char* p = base ? base + off : nullptr;
@@ -333,7 +334,11 @@ struct FastSparse {
   paged::SparseWorkspace part;
 };
 
-// ... its scratch behind the workspace of a decoding step.
+// ... its workspace: that of a decoding step without scratch for attention over the whole context, whose size would rise and fall with max_context,
+// so that what it holds grows with max_context alone; and its own scratch behind that.
+Workspace carve_sparse_step(const llm42_model* m, int num_seqs, int max_context, char* base) {
+  return carve(m, num_seqs, 1, max_context, base, true, 0, 0, WaveUse::NO, false);
+}
 size_t carve_fast_sparse(const llm42_model* m, int num_seqs, int max_context, FastSparse& f, char* base) {
   const llm42_config& c = m->cfg;
   const size_t lists = align_up(sizeof(int32_t) * (size_t)num_seqs * c.n_kv_heads * f.budget, 256);
@@ -449,7 +454,7 @@ llm42_status run_pass(const llm42_model* m, const llm42_kv_cache* kv, const int3
     // (a mirror with the bf16 cache's own table has been checked with it)
     if (f4->kv4->block_table != kv->block_table || f4->kv4->max_blocks_per_seq != kv->max_blocks_per_seq || f4->kv4->num_blocks < kv->num_blocks)
       TIMED(LLM42_K_PREPARE, launch_kv4_step_check(m, f4->kv4, num_seqs, seq_status, ws, st));
-  } else if (ws.attn_list && !fs) {
+  } else if (ws.attn_list) {
     TIMED(LLM42_K_PREPARE, launch_attention_plan(m, num_seqs, max_context, ws, st));
   }
   TIMED(LLM42_K_EMBED, launch_embed(m, candidates, window, ws, st));
@@ -549,7 +554,7 @@ llm42_status verify_impl(const char* who, const llm42_model* m, const llm42_kv_c
     if (fs->sink < 0 || fs->recent < 1 || (int64_t)fs->sink + fs->recent > fs->budget)
       return fail(LLM42_EINVAL, "%s: sink and recent must be at least 0 and 1, and no more than the budget together", who);
   }
-  Workspace ws = fs ? carve(m, num_seqs, window, max_context, (char*)workspace, true)
+  Workspace ws = fs ? carve_sparse_step(m, num_seqs, max_context, (char*)workspace)
                  : f4 && f4->kv4 ? carve(m, num_seqs, window, max_context, (char*)workspace, true, part_rows4(m, num_seqs, max_context, *f4))
                                : call_workspace(m, num_seqs, window, max_context, (char*)workspace,
                                                 f4 ? workspace_bytes - std::min(workspace_bytes, mx4_residual_bytes(num_seqs, padded_rows(num_seqs), m->cfg.d_model))
@@ -895,7 +900,7 @@ llm42_status llm42_decode_step_sparse_workspace_bytes(const llm42_model* m, int3
   f.budget = budget;
   size_t most = 0;                                               // (the ways in which the work is split change with the number of sequences)
   for (int n = 1; n <= max_seqs; ++n)
-    most = std::max(most, carve(m, n, 1, max_context, nullptr, true).bytes + carve_fast_sparse(m, n, max_context, f, nullptr));
+    most = std::max(most, carve_sparse_step(m, n, max_context, nullptr).bytes + carve_fast_sparse(m, n, max_context, f, nullptr));
   *out_bytes = most;
   return LLM42_OK;
 }

@@ -83,3 +83,38 @@ def test_heads_that_are_not_the_models_are_refused():
         assert torch.equal(cache.bounds, before)
     sess.decode_sparse(sess.paged(kv), bt, zero, zero, 2, 0, 1)
     sess.close()
+
+
+def test_one_workspace_serves_fewer_sequences_and_shorter_contexts():
+    """Across the context lengths at which attention over the whole context would change the way in which it is split (8 kv heads, one sequence: 47104)."""
+    shape = wl.TINY.replace(d_model=512, n_q_heads=8, n_kv_heads=8, head_dim=128)
+    sess = VerifierSession(shape, wl.make_weights(shape, seed=4), max_position=60000, device=DEV)
+    contexts = [1, 16, 17, 255, 257, 2048, 2049, 8000, 8192, 8208, 16000, 40960, 45056, 47104, 47105, 49152, 59999, 60000]
+    need = lambda n, c, b: B.llm42_decode_step_sparse_workspace_bytes(sess.model, n, c, b)
+    for budget in (4, 64, 2000):
+        for n in (1, 2, 5, 24, 130):
+            sizes = [need(n, c, budget) for c in contexts]
+            assert sizes == sorted(sizes)
+            assert sizes[-1] <= need(n + 1, contexts[-1], budget)
+    bt, one = i32(np.arange(3750)[None]), i32([40])
+    kv = sess.kv_cache(3750)
+    kv.normal_(generator=torch.Generator(device=DEV).manual_seed(2))
+    cache = sess.paged(kv)
+    cache.store_bounds(bt, i32([0]), one, 40)
+    ws, out, seen = torch.empty(need(1, 49152, 64), dtype=torch.uint8, device=DEV), i32([-7]), []
+    for c in (49152, 47104, 41):
+        start = kv.clone()
+        B.llm42_decode_step_sparse(sess.model, cache.heads, kv, 3750, bt, cache.bounds, 64, 1, 2, one, i32([5]), c, out, ws)
+        seen.append((int(out), kv.clone()))
+        kv.copy_(start)
+    assert all(t == seen[0][0] and torch.equal(after, seen[0][1]) for t, after in seen)
+    sess.close()
+
+
+def test_the_workspace_holds_no_partials_of_the_whole_context():
+    """128 sequences of 131072 positions: the scores of 8192 blocks for each kv head, the lists, and what a step takes at a context of one block."""
+    shape = wl.TINY.replace(d_model=512, n_q_heads=8, n_kv_heads=8, head_dim=128)
+    sess = VerifierSession(shape, wl.make_weights(shape, seed=4), max_position=131072, device=DEV)
+    need = lambda c: B.llm42_decode_step_sparse_workspace_bytes(sess.model, 128, c, 64)
+    assert need(131072) - need(16) <= 4 * 128 * 8 * 8192 + 4096
+    sess.close()
