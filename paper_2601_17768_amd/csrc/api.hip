@@ -92,11 +92,18 @@ llm42_status check_config(const llm42_config& c) {
   return LLM42_OK;
 }
 
+// Workgroups of an attention launch that take one unit of keys each: (sequence, kv head, up to 8 blocks of 16 query rows).
+long long attention_pairs(const llm42_model* m, int num_seqs, int r_pad) {
+  const int col_blocks = r_pad / 16, at_once = col_blocks >= 8 ? 8 : 4;
+  return (long long)num_seqs * m->cfg.n_kv_heads * ((col_blocks + at_once - 1) / at_once);
+}
+constexpr int kSuperWorkgroups = 192, kSuperKeys = 2048;   // pairs x supers of keys from which a call runs per super (see attention_mode)
+
 // How the attention work of a call is split (work distribution only; the bits do not depend on it).
 void attention_mode(const llm42_model* m, int num_seqs, int max_context, Workspace& ws) {
   const llm42_config& c = m->cfg;
   // attention work split: per chunk while the grid would otherwise be small, per super beyond that
-  const int col_blocks = ws.r_pad / 16, cb_groups = (col_blocks + (col_blocks >= 8 ? 8 : 4) - 1) / (col_blocks >= 8 ? 8 : 4);
+  const int col_blocks = ws.r_pad / 16;
   // One workgroup per 2048-key super (chunks folded in registers) once that gives enough workgroups - measured at
   // 8 .. 32 sequences and contexts 512 .. 6000: from about 192 (pairs x supers) on it beats one workgroup per chunk
   // plus the merge of 8 x as many partials.  Contexts that all fit one super need no merge pass at all (the
@@ -106,11 +113,11 @@ void attention_mode(const llm42_model* m, int num_seqs, int max_context, Workspa
   // order and writes the output (the store instructions that end a work item interrupt the workgroup's fetch stream,
   // and a super's fp32 partial takes nine per wave where a whole sequence's bf16 rows take four).  Whether the
   // sequences of the call deal out evenly enough for that is decided on the device, by the plan kernel.
-  const long long pairs = (long long)num_seqs * c.n_kv_heads * cb_groups;
+  const long long pairs = attention_pairs(m, num_seqs, ws.r_pad);
   const int supers = attention_units(true, max_context);
   ws.attn_seq = col_blocks >= 8 && supers > 1 && pairs >= 2LL * ws.num_cus;
   ws.attn_direct = supers == 1 && pairs >= 128;
-  ws.attn_super = ws.attn_direct || pairs * supers >= 192;
+  ws.attn_super = ws.attn_direct || pairs * supers >= kSuperWorkgroups;
   // Contexts within one super and few blocks of query rows: one workgroup per block of 16 rows, a wave per chunk, output
   // written by the same launch (attention_split_kernel).  It wins while the launch is latency - every row block fetches the
   // K and V for itself - and loses once those fetches fill the device.  us per layer, before -> with it, head_dim 128:
@@ -250,7 +257,9 @@ Workspace carve(const llm42_model* m, int num_seqs, int window, int max_context,
 // Bytes that serve every call of 1 .. max_seqs sequences: everything but the attention partials grows with the
 // number of sequences; the partials depend on the work split as well (a few sequences run per 256-key chunk where many
 // run per 2048-key super), so their slots are counted for every n, and those of a wave per chunk with them: which kernel a call
-// runs is then the same for every workspace of this size or more, whatever else it was sized for.
+// runs is then the same for every workspace of this size or more, whatever else it was sized for.  Shorter contexts can have more
+// slots than the longest: up to where a call runs per super, its chunks have one each; and a wave per chunk within one super is a matter of
+// where the context lies between 1152, 1280 and 2048 (see wave_use).
 size_t sized_for_up_to(const llm42_model* m, int max_seqs, int window, int max_context) {
   Workspace w;
   memset(&w, 0, sizeof w);
@@ -261,10 +270,21 @@ size_t sized_for_up_to(const llm42_model* m, int max_seqs, int window, int max_c
     part_rows = std::max(part_rows, (size_t)n * m->cfg.n_kv_heads * units * rows);
     items = std::max(items, (size_t)n * units);
   };
+  const auto count_waves = [&](int n, int context) {
+    if (wave_use(m, n, window, context) != WaveUse::NO) count(n, attention_units(false, context), m->group * window);
+  };
   for (int n = 1; n <= max_seqs; ++n) {
     attention_mode(m, n, max_context, w);
     count(n, w.attn_units, w.r_pad);
-    if (wave_use(m, n, window, max_context) != WaveUse::NO) count(n, attention_units(false, max_context), m->group * window);
+    count_waves(n, max_context);
+    const long long chunk_keys = (kSuperWorkgroups - 1) / attention_pairs(m, n, w.r_pad) * kSuperKeys;     // the longest context per chunk
+    if (w.attn_super && chunk_keys > 0) {
+      attention_mode(m, n, (int)std::min<long long>(chunk_keys, max_context), w);
+      count(n, w.attn_units, w.r_pad);
+    }
+    if (m->group * window <= 16)
+      for (const int context : {1152, 1280, 2048})
+        if (context < max_context) count_waves(n, context);
   }
   return carve(m, max_seqs, window, max_context, nullptr, false, part_rows, items).bytes;
 }
