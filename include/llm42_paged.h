@@ -125,8 +125,8 @@ llm42_status llm42_kv_bounds_bytes(const llm42_heads* heads, int64_t num_blocks,
  * first[s] + count[s], and have been stored), of one layer or (layer -1) all.  Behind a verifier pass and its commit: first = the length before, count = the
  * committed tokens; behind a prefill: 0 and the length.  Two sequences may share blocks.  first[s] < 0, positions beyond the table's
  * capacity, count[s] outside 0 .. max_count: LLM42_SEQ_BAD_LENGTH; an entry of the table for one of those blocks out of
- * range: LLM42_SEQ_BAD_BLOCK; nothing of such a sequence is written.  LLM42_EINVAL where num_seqs times the blocks that max_count positions can touch, times
- * n_kv_heads, exceeds 2^26. */
+ * range: LLM42_SEQ_BAD_BLOCK; nothing of such a sequence is written.  LLM42_EINVAL where num_seqs times the blocks that max_count positions can touch,
+ * (max_count + 14) / 16 + 1, times n_kv_heads is 2^26 or more. */
 llm42_status llm42_kv_bounds_store(
     const llm42_heads*    heads,
     int32_t               layer,           /* or -1: all                                   */

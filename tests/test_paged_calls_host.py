@@ -28,3 +28,11 @@ def test_the_sparse_step_compares_heads_by_their_numbers(monkeypatch):
     monkeypatch.setattr(B, "_asked", lambda call, *a: kv.numel())
     with pytest.raises(ValueError, match="not the model's"):
         B.llm42_decode_step_sparse(1, given, kv, blocks, table, bounds, 2, 0, 1, one, one, 16, one, torch.zeros(256, dtype=torch.uint8))
+
+
+@pytest.mark.parametrize("seqs,most", [(2 ** 25, 1), (2 ** 24, 17), (1, 16 * (2 ** 25 - 1) - 14)])
+def test_bounds_store_refuses_what_is_more_threads_than_a_launch_takes(seqs, most):
+    """2 kv heads: 2^26 waves, in workgroups of four, are 2^32 threads."""
+    heads, kv = B.Heads(2, 8, 2, 128), B.KVCache(4096, 4, 4096, 4)
+    assert seqs * ((most + 14) // 16 + 1) * 2 == 2 ** 26
+    assert B.load_library().llm42_kv_bounds_store(ctypes.byref(heads), -1, ctypes.byref(kv), 4096, 4096, 4096, seqs, most, None, None) == B.LLM42_EINVAL
