@@ -103,6 +103,8 @@ class PagedCache:
                k_norm: Optional[torch.Tensor] = None, eps: float = 1e-6, seq_status: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
         """One llm42_kv_append call; the bounds of blocks that become whole are kept up if the cache has bounds.  Returns q_out (zeros where a row takes no part,
         unless it is given)."""
+        if rope is not None and not rope.handle:
+            raise ValueError("the rotary table is closed")
         if q is not None and q_out is None:
             q_out = torch.zeros(q.shape, dtype=torch.bfloat16, device=q.device)
         B.llm42_kv_append(self.heads, layer, self.kv, self.num_blocks, block_table, self.bounds, q, k, v, q_norm, k_norm, eps,

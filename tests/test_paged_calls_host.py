@@ -5,6 +5,7 @@ import pytest
 import torch
 
 from paper_2601_17768_amd import binding as B
+from paper_2601_17768_amd.paged import PagedCache, Rope
 
 
 def test_model_heads_refuses():
@@ -36,3 +37,21 @@ def test_bounds_store_refuses_what_is_more_threads_than_a_launch_takes(seqs, mos
     heads, kv = B.Heads(2, 8, 2, 128), B.KVCache(4096, 4, 4096, 4)
     assert seqs * ((most + 14) // 16 + 1) * 2 == 2 ** 26
     assert B.load_library().llm42_kv_bounds_store(ctypes.byref(heads), -1, ctypes.byref(kv), 4096, 4096, 4096, seqs, most, None, None) == B.LLM42_EINVAL
+
+
+def unmade_rope(handle):
+    rope = Rope.__new__(Rope)
+    rope.rot_dim, rope.max_position, rope.handle, rope.device = 64, 128, handle, 0
+    return rope
+
+
+def test_append_refuses_a_closed_rope(monkeypatch):
+    """(The library takes a null handle for "no rotation".)"""
+    cache, called = PagedCache(torch.zeros(1, 2, 2, 1, 16 * 64, dtype=torch.bfloat16), 1, 64, bounds=False), []
+    monkeypatch.setattr(B, "llm42_kv_append", lambda *a: called.append(a))
+    k, lens, table = torch.zeros(1, 1, 1, 64, dtype=torch.bfloat16), torch.zeros(1, dtype=torch.int32), torch.zeros(1, 2, dtype=torch.int32)
+    with pytest.raises(ValueError, match="closed"):
+        cache.append(0, k, k, table, lens, rope=unmade_rope(None))
+    assert not called
+    cache.append(0, k, k, table, lens)
+    assert len(called) == 1
