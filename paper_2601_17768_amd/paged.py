@@ -24,13 +24,23 @@ _SCALINGS = {"none": (B.LLM42_ROPE_NONE, ()),
              "linear": (B.LLM42_ROPE_LINEAR, ("factor",)),
              "llama3": (B.LLM42_ROPE_LLAMA3, ("factor", "low_freq_factor", "high_freq_factor", "original_max_position")),
              "yarn": (B.LLM42_ROPE_YARN, ("factor", "beta_fast", "beta_slow", "original_max_position"))}
-_outlived = []          # handles whose owner went away during a capture, which no allocation may be freed in
+_dropped = []           # (device, handle) of tables whose owner went away without closing them
+
+
+def _give_back_dropped():
+    while _dropped:
+        device, handle = _dropped.pop()
+        torch.cuda.synchronize(device)
+        B.llm42_rope_destroy(handle)
 
 
 class Rope:
     """Rotary positions on the current device: the first rot_dim features of a head, in pairs by `layout` ("half": j and j + rot_dim / 2, "interleaved":
     2 j and 2 j + 1), frequencies theta^(-2 j / rot_dim) scaled by `scaling`: a dict with "kind" ("none", "linear", "llama3", "yarn"), the kind's
-    parameters by their names in llm42_rope_config, and if it is not the kind's own, attention_factor."""
+    parameters by their names in llm42_rope_config, and if it is not the kind's own, attention_factor.
+
+    A table holds 4 * rot_dim bytes a position until close(), which waits for its device, as making one does: neither belongs in a capture, on whatever stream.
+    One that is dropped instead is given back where the next is made or closed: a finalizer runs at any time, and frees and waits for nothing."""
 
     def __init__(self, rot_dim: int, theta: float, max_position: int, layout: str = "half", scaling: Optional[Dict] = None):
         self.handle = None
@@ -45,26 +55,23 @@ class Rope:
             raise ValueError(f"scaling {kind!r} takes {', '.join(names) or 'nothing'} (and attention_factor), got {', '.join(given) or 'nothing'}")
         if torch.cuda.is_current_stream_capturing():
             raise RuntimeError("a rotary table must be made before a capture")
-        while _outlived:
-            B.llm42_rope_destroy(_outlived.pop())
-        self.rot_dim, self.max_position = rot_dim, max_position
+        _give_back_dropped()
+        self.rot_dim, self.max_position, self.device = rot_dim, max_position, torch.cuda.current_device()
         self.handle = B.llm42_rope_create(B.RopeConfig(rot_dim=rot_dim, layout=_LAYOUTS[layout], scaling=number, max_position=max_position,
                                                        theta=theta, **given))
 
     def close(self):
         if self.handle:
-            torch.cuda.synchronize()
-            B.llm42_rope_destroy(self.handle)
+            if torch.cuda.is_current_stream_capturing():
+                raise RuntimeError("a rotary table must be closed outside of a capture")
+            _dropped.append((self.device, self.handle))
             self.handle = None
+            _give_back_dropped()
 
     def __del__(self):
-        try:
-            if self.handle and torch.cuda.is_current_stream_capturing():
-                _outlived.append(self.handle)
-            else:
-                self.close()
-        except Exception:
-            pass
+        if getattr(self, "handle", None) and _dropped is not None:      # (None while the interpreter ends)
+            _dropped.append((self.device, self.handle))
+            self.handle = None
 
 
 class PagedCache:

@@ -1,5 +1,6 @@
 """Calls around the paged cache that are refused, or do nothing, without a GPU."""
 import ctypes
+import gc
 
 import pytest
 import torch
@@ -55,3 +56,29 @@ def test_append_refuses_a_closed_rope(monkeypatch):
     assert not called
     cache.append(0, k, k, table, lens)
     assert len(called) == 1
+
+
+def test_a_dropped_rope_neither_waits_nor_frees(monkeypatch):
+    """A finalizer runs whenever its object is collected, while another stream captures as well; the table is given back with the next one that is closed, on its own
+    device."""
+    calls = []
+    monkeypatch.setattr(torch.cuda, "synchronize", lambda device=None: calls.append(("wait", device)))
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+    monkeypatch.setattr(B, "llm42_rope_destroy", lambda handle: calls.append(("free", handle)))
+    first, second = unmade_rope(11), unmade_rope(12)
+    first.device = 3
+    del first
+    gc.collect()
+    assert not calls
+    second.close()
+    assert sorted(calls[i:i + 2] for i in (0, 2)) == [[("wait", 0), ("free", 12)], [("wait", 3), ("free", 11)]]
+    second.close()
+    del second
+    gc.collect()
+    assert len(calls) == 4
+    captured = unmade_rope(13)
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: True)
+    with pytest.raises(RuntimeError, match="capture"):
+        captured.close()
+    assert len(calls) == 4 and captured.handle == 13
+    captured.handle = None
