@@ -164,7 +164,8 @@ llm42_status llm42_kv_bounds_read(
  * depend on an order of summation.  A block whose bounds are infinite comes first.
  * The bounds of blocks sink .. own - recent must have been stored; other blocks' are not read.  Block-table entries are needed for
  * all positions of the sequence.
- * selected[s][i][kv head][0 .. budget - 1]: the blocks, ascending, -1 behind them. */
+ * selected[s][i][kv head][0 .. budget - 1]: the blocks, ascending, -1 behind them.
+ * The workspace holds scores: at most 256 MiB, or what one sequence takes, 4 bytes for each row of the window, kv head and block of max_context, where that is more. */
 llm42_status llm42_kv_select_workspace_bytes(const llm42_heads* heads, int32_t num_seqs, int32_t window, int32_t max_context,
                                              int32_t budget, size_t* out_bytes);
 llm42_status llm42_kv_select(

@@ -537,6 +537,9 @@ int64_t keys_of(int max_context) { return ((int64_t)max_context + 255) / 256 * 1
 int cols_of(int group) { return group > 8 ? 16 : group > 4 ? 8 : group > 2 ? 4 : group; }
 int tile_rows_of(int group, int window) { return std::min(16 / cols_of(group), window); }
 constexpr int64_t kMostLdsKeys = 12288;      // 48 KiB
+// Scores that wait in the workspace at once, unless one sequence alone has more: a call of more goes through it some sequences at a time.
+constexpr size_t kMostScores = 256u << 20;
+size_t scores_of(int window, int n_kv_heads, int max_context) { return 4ull * window * n_kv_heads * keys_of(max_context); }   // (of a sequence)
 
 }  // namespace
 
@@ -551,7 +554,21 @@ size_t select_workspace(int num_seqs, int window, int n_kv_heads, int group, int
   // 27 / 109, 1 window of 64 x 30000 22.7 / 59; 32 x 32768 36.7 / 38.8; but 64 x 32768 75 / 62, 128 x 8192 42 / 32, 4 windows of 32 x 8000 25 / 16.5).  Those of a tile of rows that LDS does not
   // hold go there too.
   if (tile_rows * keys <= kMostLdsKeys && (2 * wgs > num_cus || keys <= 512)) return 0;
-  return 4ull * num_seqs * window * n_kv_heads * keys;
+  const size_t one = scores_of(window, n_kv_heads, max_context);
+  return std::min(num_seqs * one, std::max(one, kMostScores));
+}
+
+// The call's sequences from .. from + n - 1 as a call of their own.
+static Select sequences_from(Select a, int from, int n) {
+  Rows& r = a.rows;
+  r.num_seqs = n;
+  r.block_table += (size_t)from * r.width;
+  r.seq_len += from;
+  if (r.seq_n) r.seq_n += from;
+  a.q += a.tiles ? (int64_t)from * a.n_kv_heads * 16 * a.head_dim : (int64_t)from * r.window * a.q_stride;
+  a.selected += (size_t)from * r.window * a.n_kv_heads * a.budget;
+  if (a.seq_status) a.seq_status += from;
+  return a;
 }
 
 void launch_kv_select(const Select& a, hipStream_t st) {
@@ -566,13 +583,16 @@ void launch_kv_select(const Select& a, hipStream_t st) {
       return;
     }
     const int chunk = (int)std::max<int64_t>(kChunk, (keys + 65535) / 65536 * 16);
-    score_kernel<HD, COLS><<<dim3(r.num_seqs * tiles, a.n_kv_heads, (unsigned)((keys + chunk - 1) / chunk)), kThreads, 0, st>>>(a, tile_rows, tiles, keys, chunk);
-    const auto pick = [&](auto held) {
-      pick_kernel<decltype(held)::value><<<dim3(r.num_seqs * r.window, a.n_kv_heads), kPickThreads, 0, st>>>(a, keys);
-    };
-    if (keys <= 2 * kPickThreads) pick(std::integral_constant<int, 2>{});
-    else if (keys <= 8 * kPickThreads) pick(std::integral_constant<int, 8>{});
-    else pick(std::integral_constant<int, 0>{});
+    const int at_once = (int)std::min<size_t>(r.num_seqs, std::max<size_t>(1, kMostScores / scores_of(r.window, a.n_kv_heads, r.max_context)));
+    for (int from = 0; from < r.num_seqs; from += at_once) {
+      const Select b = sequences_from(a, from, std::min(at_once, r.num_seqs - from));
+      const int rows = b.rows.num_seqs * r.window;
+      score_kernel<HD, COLS><<<dim3(b.rows.num_seqs * tiles, a.n_kv_heads, (unsigned)((keys + chunk - 1) / chunk)), kThreads, 0, st>>>(b, tile_rows, tiles, keys, chunk);
+      const auto pick = [&](auto held) { pick_kernel<decltype(held)::value><<<dim3(rows, a.n_kv_heads), kPickThreads, 0, st>>>(b, keys); };
+      if (keys <= 2 * kPickThreads) pick(std::integral_constant<int, 2>{});
+      else if (keys <= 8 * kPickThreads) pick(std::integral_constant<int, 8>{});
+      else pick(std::integral_constant<int, 0>{});
+    }
   };
   const auto by_cols = [&](auto hd) {
     switch (cols_of(a.group)) {

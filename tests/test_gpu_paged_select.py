@@ -9,6 +9,7 @@ import pytest
 import torch
 
 import paged_reference as ref
+from paper_2601_17768_amd import binding as B
 from paper_2601_17768_amd.paged import PagedCache
 
 pytestmark = pytest.mark.gpu
@@ -79,3 +80,27 @@ def test_equal_keys_in_every_way():
         w.cache.kv[0, 0] = w.cache.kv[0, 0, :1].clone()
         w.stored()
         w.check(1, 9, 2, 3, 8, most)
+
+
+def test_scores_of_more_than_the_workspace_holds_go_through_it_in_turn():
+    """20 windows of 64 rows over 131072 positions, 8 kv heads: 16 of them fit at once.  Every sequence gets what it gets alone, status and rows that take no part among it."""
+    w = Shared(20, 8192, 8, 1, 64)
+    w.stored()
+    assert B.llm42_kv_select_workspace_bytes(w.cache.heads, 20, 64, 131072, 7) == 256 << 20
+    w.check(64, 7, 1, 2, 14)
+    q = torch.randn(20, 64, 8, 64, generator=w.g, device=DEV).to(torch.bfloat16)
+    lens = torch.randint(0, 131000, (20,), generator=w.g, device=DEV, dtype=torch.int32)
+    valid = torch.randint(0, 65, (20,), generator=w.g, device=DEV, dtype=torch.int32)
+    lens[[3, 18]] = torch.tensor([-1, 131009], dtype=torch.int32, device=DEV)
+    valid[18] = 64
+    table = w.table.clone()
+    table[17, 0], lens[17], valid[17] = -1, 500, 3
+    status = torch.full((20,), 9, dtype=torch.int32, device=DEV)
+    out = torch.full((20, 64, 8, 7), -77, dtype=torch.int32, device=DEV)
+    w.cache.select(0, q, table, lens, 7, n_valid=valid, selected=out, seq_status=status)
+    alone, one = torch.full_like(out, -77), torch.full_like(status, 9)
+    for s in range(20):
+        w.cache.select(0, q[s:s + 1], table[s:s + 1], lens[s:s + 1], 7, n_valid=valid[s:s + 1], selected=alone[s:s + 1], seq_status=one[s:s + 1])
+    assert torch.equal(out, alone) and torch.equal(status, one)
+    assert status.tolist() == [1 if s in (3, 18) else 2 if s == 17 else 0 for s in range(20)]
+    assert bool((out[[3, 17, 18]] == -77).all())

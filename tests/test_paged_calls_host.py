@@ -82,3 +82,15 @@ def test_a_dropped_rope_neither_waits_nor_frees(monkeypatch):
         captured.close()
     assert len(calls) == 4 and captured.handle == 13
     captured.handle = None
+
+
+def test_the_selections_workspace_has_a_ceiling():
+    """256 MiB, or what a sequence alone takes; it grows with the context, and never falls."""
+    need = lambda heads, *a: B.llm42_kv_select_workspace_bytes(heads, *a)
+    small, large = B.Heads(1, 32, 8, 128), B.Heads(1, 1024, 1024, 64)
+    assert need(small, 8, 512, 131072, 64) == need(small, 32768, 2, 131072, 64) == 256 << 20
+    assert need(small, 2, 1, 131072, 64) == 2 * 4 * 8 * 8192
+    assert need(large, 1, 512, 2 ** 20, 64) == need(large, 128, 512, 2 ** 20, 64) == 4 * 512 * 1024 * 2 ** 16
+    for seqs, window in ((1, 1), (3, 64), (128, 1), (128, 512)):
+        sizes = [need(small, seqs, window, 1000 * 2 ** i + j, 64) for i in range(20) for j in (0, 1, 300)]
+        assert sizes == sorted(sizes)
