@@ -210,7 +210,7 @@ llm42_status llm42_kv_sparse_attention(
     int32_t               max_context,
     const int32_t*        selected,        /* dev [num_seqs][window][n_kv_heads][width]    */
     int32_t               width,           /* 1 .. LLM42_MAX_SELECTED                      */
-    float                 scale,           /* >= 0, finite                                 */
+    float                 scale,           /* 0 .. 2^126                                   */
     void*                 out,             /* dev bf16 rows of n_q_heads * head_dim        */
     int64_t               out_stride,
     int32_t*              seq_status,

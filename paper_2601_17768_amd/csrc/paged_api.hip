@@ -372,7 +372,8 @@ llm42_status llm42_kv_sparse_attention(const llm42_heads* heads, int32_t layer, 
   if (llm42_status st = check_plain(who, "out", out, out_stride, heads->n_q_heads, heads->head_dim, 2)) return st;
   if (llm42_status st = check_budget(who, width)) return st;
   if (!selected) return fail(LLM42_EINVAL, "%s: null argument", who);
-  if (!(scale >= 0.f) || !std::isfinite(scale)) return fail(LLM42_EINVAL, "%s: scale must be finite and not negative", who);
+  // (it is multiplied by log2 e, which must stay finite: a score of 0 counts whatever the scale)
+  if (!(scale >= 0.f) || scale > 0x1p126f) return fail(LLM42_EINVAL, "%s: scale must be 0..2^126", who);
   SparseAttention a;
   a.rows = rows_of(kv, seq_lens, window, n_valid, num_seqs, max_context);
   a.k_plane = k_plane_of(heads, kv, layer);

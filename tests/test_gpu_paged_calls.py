@@ -35,3 +35,15 @@ def test_a_rope_is_dropped_while_another_stream_captures():
     with pytest.raises(ValueError):
         step()
     rope.close()
+
+
+def test_attention_by_the_largest_scale():
+    """Scores of 0 are equal at any scale."""
+    g = torch.Generator(device=DEV).manual_seed(2)
+    kv = torch.zeros(1, 2, 2, 1, 16 * 64, dtype=torch.bfloat16, device=DEV)
+    kv[0, 1] = 3.0
+    cache = PagedCache(kv, 2, 64, bounds=False)
+    q = torch.randn(1, 1, 2, 64, generator=g, device=DEV).bfloat16()
+    table, lens = torch.tensor([[1, 0]], dtype=torch.int32, device=DEV), torch.tensor([20], dtype=torch.int32, device=DEV)
+    lists = torch.tensor([0, 1], dtype=torch.int32, device=DEV).view(1, 1, 1, 2)
+    assert bool((cache.attention(0, q, table, lens, lists, scale=2.0 ** 126) == 3).all())

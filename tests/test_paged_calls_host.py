@@ -94,3 +94,10 @@ def test_the_selections_workspace_has_a_ceiling():
     for seqs, window in ((1, 1), (3, 64), (128, 1), (128, 512)):
         sizes = [need(small, seqs, window, 1000 * 2 ** i + j, 64) for i in range(20) for j in (0, 1, 300)]
         assert sizes == sorted(sizes)
+
+
+@pytest.mark.parametrize("scale", [2.0 ** 126 * 1.01, 3.4e38])
+def test_sparse_attention_refuses_a_scale_that_overflows_in_base_2(scale):
+    heads, kv = B.Heads(2, 8, 2, 128), B.KVCache(4096, 4, 4096, 4)
+    assert B.load_library().llm42_kv_sparse_attention(ctypes.byref(heads), 0, ctypes.byref(kv), 4096, 1024, 4096, 2, None, 3, 64, 4096, 8, scale, 8192, 1024,
+                                                      None, None, 0, None) == B.LLM42_EINVAL
