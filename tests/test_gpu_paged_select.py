@@ -104,3 +104,15 @@ def test_scores_of_more_than_the_workspace_holds_go_through_it_in_turn():
     assert torch.equal(out, alone) and torch.equal(status, one)
     assert status.tolist() == [1 if s in (3, 18) else 2 if s == 17 else 0 for s in range(20)]
     assert bool((out[[3, 17, 18]] == -77).all())
+
+
+@pytest.mark.parametrize("hd,kv_heads,group,window,blocks", [(128, 4, 3, 1, 12288), (64, 4, 1, 1, 12279), (128, 4, 4, 4, 3072), (64, 3, 1, 17, 768), (128, 2, 2, 9, 1536)])
+def test_the_most_scores_that_lds_holds(hd, kv_heads, group, window, blocks):
+    """48 KiB of them, for one row or up to 16, beside the records that are turned there; rows picked by waves and by the workgroup, one after the other."""
+    seqs = 129 // kv_heads + 1
+    w = Shared(seqs, blocks, kv_heads, group, hd, seed=window)
+    w.infinite(torch.randperm(blocks, generator=w.g, device=DEV)[:5])
+    w.stored()
+    assert B.llm42_kv_select_workspace_bytes(w.cache.heads, seqs, window, 16 * blocks, 50) == 0
+    w.check(window, 50, 1, 2, 24)
+    w.check(window, 3, 0, 1, 12)

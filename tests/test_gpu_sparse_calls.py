@@ -118,3 +118,32 @@ def test_the_workspace_holds_no_partials_of_the_whole_context():
     need = lambda c: B.llm42_decode_step_sparse_workspace_bytes(sess.model, 128, c, 64)
     assert need(131072) - need(16) <= 4 * 128 * 8 * 8192 + 4096
     sess.close()
+
+
+def test_sequences_that_are_not_in_order_store_no_bounds():
+    """Whose token would have made a block whole: each with one thing wrong, in a block before that one."""
+    shape = wl.TINY
+    sess = VerifierSession(shape, wl.make_weights(shape, seed=5), max_position=512, device=DEV)
+    rng = wl.rng_for(6, 2)
+    lens = [303, 303, 47, 47, 47]
+    table, blocks = wl.make_block_table(rng, [n + 1 for n in lens], 16, spare_blocks=1)
+    bt, kv = torch.as_tensor(table, device=DEV), sess.kv_cache(blocks)
+    tok = sess.prefill(kv, bt, [wl.random_tokens(rng, n, shape.vocab) for n in lens], window=32)
+    cache, seq = sess.paged(kv), i32(lens)
+    cache.bounds.fill_(77)
+    cache.store_bounds(bt, torch.zeros_like(seq), seq, 303)
+    before, start = cache.bounds.clone().view(shape.n_layers, blocks, -1), kv.clone()
+    whole = [int(table[s][lens[s] // 16]) for s in range(5)]
+    assert bool((before[:, whole] == 77).all())
+    bad_bt, bad_tok = bt.clone(), tok.clone()
+    bad_bt[1, 3], bad_bt[2, 0] = blocks, -1
+    bad_tok[3] = -1
+    status = i32([9] * 5)
+    out = sess.decode_sparse(cache, bad_bt, seq, bad_tok, 4, seq_status=status)
+    assert status.tolist() == [0, B.LLM42_SEQ_BAD_BLOCK, B.LLM42_SEQ_BAD_BLOCK, B.LLM42_SEQ_BAD_TOKEN, 0] and out[1:4].tolist() == [-1] * 3
+    after = cache.bounds.view(shape.n_layers, blocks, -1)
+    moved = (after != before).any(-1)
+    assert bool(moved[:, [whole[0], whole[4]]].all()) and int(moved.sum()) == 2 * shape.n_layers
+    changed = (kv != start).any(-1).any(-1).any(0).any(0).nonzero().flatten().tolist()
+    assert sorted(changed) == sorted([whole[0], whole[4]])
+    sess.close()
