@@ -171,8 +171,10 @@ __device__ inline bool bad_block(const Rows& r, int s, int len, int n, int lane,
 }
 
 // The launch's first workgroups take a (sequence, block, kv head) of K or of V per wave, the others a row and some heads of Q per HD / 8 lanes: its position's
-// cos and sin are read once for them.  Bound by memory where rows are many: 8 x 512 rows of 32 + 2 x 8 heads of 128 with norms, 103 MB, take 29 us, 3.5 TB/s (a head at a
-// time 47, four 33, sixteen 37); by launch and two trips where they are few: one row 3.8, 128 4.8.
+// cos and sin are read once for them.  8 x 512 rows of 32 + 2 x 8 heads of 128 with norms, 103 MB, take 29 us (a head at a time 47, four 33, sixteen 37), of which memory is
+// 21, as a copy of as many bytes takes: without norms and rotation the launch takes 24.5, without norms 27.6, without rotation 25.6, so a sixth is arithmetic and the loads of cos and sin, which
+// wait behind the rows.  K and V alone take 12.4, 9.6 without norms and rotation; from fp32 all takes 36.8, and with the bounds kept up 30.6.  (Three sets of inputs in turn;
+// one, part of which the caches hold, 22.6, and a copy 15.6.)  Few rows: launch and two trips, one row 3.8, 128 4.8, with bounds 5.9.
 template <int HD, typename T>
 __global__ __launch_bounds__(256) void append_kernel(Append a, Pairs pairs, int slots, unsigned kv_groups, int q_heads) {
   constexpr int LANES = HD / 8, UNITS = 64 / LANES, N = HD / 32, PAD = HD + 4;

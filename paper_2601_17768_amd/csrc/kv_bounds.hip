@@ -9,9 +9,10 @@ using namespace paged;
 namespace {
 
 // One wave per (block of 16 positions, kv head) and L layers (blockIdx.y), the next layer's keys asked for before this one's are looked at; four waves to a
-// workgroup.  Bound by memory: the keys of 4 x 1500 - 2048 tokens of 32 layers of 8 heads of 128, 461 MB, and their bounds take 109 us, 4.5 TB/s
-// (a layer to a wave 130: three loads that wait for each other stand before every 4 KiB; where there are few waves that costs less than
-// four layers in turn, 24 x 1 - 32 tokens 12.2 / 14.6).
+// workgroup.  Bound by memory where blocks are many: the keys of 4 x 1500 - 2048 tokens of 32 layers of 8 heads of 128, 461 MB, and their bounds take 102 us,
+// 4.8 TB/s (a copy of as many bytes runs at 5.3; a layer to a wave 130: three loads that wait for each other stand before every 4 KiB).  Where there are
+// few waves those trips are the time, and cost less than four layers in turn: 24 x 1 - 32 tokens, 30 MB, 14.6 / 16.6.
+// MANY: a wave takes some blocks in turn (see the launch).
 template <int HD, int L, bool MANY>
 __global__ __launch_bounds__(256) void bounds_store_kernel(const uint16_t* __restrict__ k_plane, int64_t layer_stride, char* __restrict__ bounds,
                                                            const int32_t* __restrict__ table, int width, int64_t num_blocks, int n_kv_heads,

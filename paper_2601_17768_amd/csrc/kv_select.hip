@@ -536,7 +536,7 @@ __global__ __launch_bounds__(kPickThreads) void pick_kernel(Select a, int64_t st
 int64_t keys_of(int max_context) { return ((int64_t)max_context + 255) / 256 * 16; }
 int cols_of(int group) { return group > 8 ? 16 : group > 4 ? 8 : group > 2 ? 4 : group; }
 int tile_rows_of(int group, int window) { return std::min(16 / cols_of(group), window); }
-constexpr int64_t kMostLdsKeys = 12288;      // 48 KiB
+constexpr int64_t kMostLdsKeys = 12288;      // 48 KiB, beside 8 or 16 for the records that are turned and 2 of counts: two workgroups to a CU
 // Scores that wait in the workspace at once, unless one sequence alone has more: a call of more goes through it some sequences at a time.
 constexpr size_t kMostScores = 256u << 20;
 size_t scores_of(int window, int n_kv_heads, int max_context) { return 4ull * window * n_kv_heads * keys_of(max_context); }   // (of a sequence)
