@@ -273,8 +273,8 @@ llm42_status llm42_kv_bounds_store(const llm42_heads* heads, int32_t layer, cons
   if (!kv_bounds || !first || !count) return fail(LLM42_EINVAL, "%s: null argument", who);
   if ((uintptr_t)kv_bounds % 16) return fail(LLM42_EINVAL, "%s: bounds must be 16-byte aligned", who);
   if (num_seqs < 1 || max_count < 1) return fail(LLM42_EINVAL, "%s: num_seqs and max_count must be positive", who);
-  // (four of them are a workgroup of 256 threads, of which a launch takes fewer than 2^32)
-  if ((int64_t)num_seqs * (((int64_t)max_count + 14) / 16 + 1) * heads->n_kv_heads >= (1 << 26))
+  // (below 2^26 waves: four of them are a workgroup of 256 threads, of which a launch takes fewer than 2^32)
+  if ((int64_t)num_seqs * (((int64_t)max_count + 14) / 16 + 1) > ((1 << 26) - 1) / heads->n_kv_heads)
     return fail(LLM42_EINVAL, "%s: num_seqs * max_count too large", who);
   const int from = layer < 0 ? 0 : layer;
   launch_bounds_store(layer < 0 ? heads->n_layers : 1, heads->n_kv_heads, heads->head_dim, k_plane_of(heads, kv, from),
