@@ -40,7 +40,7 @@ def test_bounds_store_refuses_what_is_more_threads_than_a_launch_takes(seqs, mos
     assert B.load_library().llm42_kv_bounds_store(ctypes.byref(heads), -1, ctypes.byref(kv), 4096, 4096, 4096, seqs, most, None, None) == B.LLM42_EINVAL
 
 
-@pytest.mark.parametrize("seqs,most,kv_heads", [(2 ** 31 - 1, 2 ** 31 - 1, 1024), (2 ** 27, 2 ** 31 - 1, 1024), (2 ** 31 - 1, 1, 1), (1, 2 ** 31 - 1, 1)])
+@pytest.mark.parametrize("seqs,most,kv_heads", [(2 ** 30, 2 ** 31 - 30, 1024), (2 ** 31 - 1, 2 ** 31 - 1, 1024), (2 ** 31 - 1, 1, 1), (1, 2 ** 31 - 1, 1)])
 def test_bounds_store_refuses_sizes_whose_product_passes_64_bits(seqs, most, kv_heads):
     heads, kv = B.Heads(2, kv_heads, kv_heads, 64), B.KVCache(4096, 4, 4096, 4)
     assert B.load_library().llm42_kv_bounds_store(ctypes.byref(heads), -1, ctypes.byref(kv), 4096, 4096, 4096, seqs, most, None, None) == B.LLM42_EINVAL
